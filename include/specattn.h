@@ -345,6 +345,161 @@ specattn_status specattn_stream_read(const void *src, size_t bytes, uint32_t *si
  */
 specattn_status specattn_init(void);
 
+/*
+ * Key/value cache in 4 bits.
+ *
+ * A row of keys (or values) of d elements is held in blocks of 32 consecutive elements: one power-of-two scale per
+ * block and one 4-bit floating-point code per element.  Code c stands for (c & 8 ? -1 : 1) * {0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6}[c & 7], scale byte x for 2^(x - 127); byte 255 makes the block NaN (the OCP microscaling format MXFP4).  A
+ * position of a kv head takes d bytes of codes - d/2 of its keys, then d/2 of its values, element 2i in the low half of
+ * byte i - and d/16 bytes of scales, those of the keys first: 136 bytes at d = 128, where bf16 takes 512.
+ *
+ * Contiguous: codes [B][H_kv][n_max][d], scales [B][H_kv][n_max][d/16].  Paged: pools [num_pages][H_kv][page_size][d]
+ * and [num_pages][H_kv][page_size][d/16] under one page table.  Strides are in bytes; the d (d/16) bytes of a position
+ * are contiguous.  codes and its strides are multiples of 16 bytes, scales and its strides of 4 (SPECATTN_EALIGN).  A
+ * page number outside [0, num_pages) or a slot outside [0, n_max) never leads outside the cache: rows to be written or
+ * moved there are left out, rows to be read there come from a page or slot that exists.
+ */
+typedef struct specattn_mx_cache {
+    uint8_t *codes, *scales;
+    int64_t codes_stride_b, codes_stride_h, codes_stride_n, codes_stride_page;       /* _b contiguous, _page paged */
+    int64_t scales_stride_b, scales_stride_h, scales_stride_n, scales_stride_page;
+    const int32_t *page_table;   /* [B][max_pages_per_seq] page ids, or NULL = contiguous */
+    int32_t page_size, max_pages_per_seq, num_pages;     /* page_size: a power of two */
+    int32_t B, H_kv, n_max, d;   /* n_max: slots per sequence; d: 64 or 128 */
+} specattn_mx_cache;
+
+/* Rows going into the cache, or coming out of it: row t of sequence b is slot starts[b] + t. */
+typedef struct specattn_mx_rows_args {
+    specattn_mx_cache cache;
+    void *k, *v;                 /* [B][H_kv][T][d]; read by specattn_mx_store, written by specattn_mx_load */
+    specattn_dtype dtype;        /* of k and v */
+    int32_t T;                   /* rows per sequence */
+    int64_t stride_b, stride_h, stride_t;                /* elements, of k and v alike; last dim contiguous; 16-byte multiples */
+    const int32_t *starts;       /* [B] first slot of each sequence, or NULL for 0 */
+    const int32_t *counts;       /* [B] rows of each sequence (at most T are taken), or NULL for T */
+} specattn_mx_rows_args;
+
+/*
+ * specattn_mx_store: rows into the cache (Algorithm 1 updates the caches with every accepted token; a prompt's rows all at
+ * once).  The scale of a block is 2^X with X = floor(log2(largest magnitude)) - 2, between -127 and 125, and each element goes to
+ * the nearest of its block's values (ties to the even code, magnitudes beyond 6 to 6, signs kept, of zeros too); a block of
+ * zeros gets scale byte 0, one with an infinity or NaN scale byte 255.  Slots that no row goes to are left as they were.
+ * Rows that lie beyond n_max or in a page outside the pool are left out.  Two rows must not go to the same slot.
+ *
+ * specattn_mx_load: the values of slots in the type of k and v (rounded to nearest even where it cannot hold them; a
+ * magnitude that fp16 cannot hold becomes infinite).  Rows at and beyond counts[b] are left as they were, and so are rows of
+ * slots beyond n_max or in a page outside the pool.
+ */
+specattn_status specattn_mx_store(const specattn_mx_rows_args *args, void *stream);
+specattn_status specattn_mx_load(const specattn_mx_rows_args *args, void *stream);
+
+/*
+ * Sparse decode attention (Section 3.1.2, Eq. 2-3; Section 3.5) over a cache in 4 bits: the same computation, lists and
+ * results as specattn_sparse_decode_attn on the values the cache stands for.  Products are exact, accumulation and the
+ * softmax are fp32, and repeated calls give bit-identical results.  q, k_new and v_new are bf16 or fp16.  Lists of
+ * positions, lists of chunks (chunk_size), pool slots (indices_are_physical) or, with indices == counts == NULL, every
+ * position below seq_lens[b].  A row with nothing to attend to gives out = 0 and lse = -inf.  Any number of query heads
+ * per kv head (up to 64 query rows G*T per pass over the cache).  A list entry outside the cache is read as the nearest
+ * slot inside it.  The codes a kv head's rows lie in have to be within 64 GiB of its first one (SPECATTN_ESHAPE).
+ */
+typedef struct specattn_mx_attn_args {
+    specattn_mx_cache cache;
+    const void *q;               /* [B][H_q][T][d]; H_q a multiple of cache.H_kv */
+    specattn_dtype dtype;        /* of q, k_new, v_new and out_lowp: SPECATTN_BF16 or SPECATTN_F16 */
+    int32_t H_q, T;
+    float sm_scale;              /* <= 0 selects 1/sqrt(d) */
+    int64_t q_stride_b, q_stride_h, q_stride_t;          /* elements; last dim contiguous; 16-byte multiples */
+    const int32_t *seq_lens;     /* [B] or NULL; used by dense calls and chunk lists */
+    const int32_t *indices;      /* [B*H_kv][idx_stride_row] */
+    int64_t idx_stride_row;
+    const int32_t *counts;       /* [B*H_kv]; values above idx_capacity are clamped to it */
+    int32_t idx_capacity;
+    int32_t chunk_size;          /* 0 or 1: positions; a power of two up to 1024: chunk numbers */
+    int32_t indices_are_physical;/* 1: entries are pool slots page * page_size + offset (a pool; no page table needed) */
+    const void *k_new, *v_new;   /* optional: [B][H_kv][T][d], contiguous, seen causally behind the cache */
+    float *out;                  /* [B][H_q][T][d] fp32, contiguous; optional if out_lowp is given */
+    void *out_lowp;              /* [B][H_q][T][d] in dtype, contiguous; optional if out is given */
+    float *lse;                  /* [B][H_q][T]; optional */
+    void *workspace;             /* specattn_mx_workspace_size(args) bytes, 256-byte aligned */
+    size_t workspace_bytes;
+} specattn_mx_attn_args;
+
+specattn_status specattn_mx_decode_attn(const specattn_mx_attn_args *args, void *stream);
+size_t specattn_mx_workspace_size(const specattn_mx_attn_args *args);      /* 0 for invalid arguments */
+
+/*
+ * Eviction by accumulated attention weight: the draft model's attention rows, which choose the positions that a verify step
+ * reads (Section 3.4), also say over many steps which ones are hardly ever read; those can leave the cache for good.
+ *
+ * specattn_evict_select, for every row (sequence b, score row h of H; with H = 1 all heads of a sequence share one
+ * choice) and the slots j < len = seq_lens[b]:
+ *   score'[j] = decay * scores[j] + the sum of probs[b][x][s][j] over the steps s and the draft heads x that speak for the row
+ *               (heads h*H_draft/H .. (h+1)*H_draft/H - 1, as in the union), added up in fp64 and rounded once to fp32;
+ *   kept      = min(len, budget) slots: first those whose token is one of the first `sinks` or of the last `recent` of the
+ *               text (positions[j] < sinks or positions[j] >= next_positions[b] - recent), then by score' from the largest
+ *               down, NaN last; among equals the lowest slot first.
+ * Kept slots beyond the new length move into the dropped slots below it, both in ascending order: move i of the row goes from
+ * move_src[i] to move_dst[i].  No slot is both, so that moves may run in any order, and what stays where it is costs
+ * nothing.  scores_out and positions_out get the new state: slots below the new length hold the kept slots' scores and positions,
+ * those from there up to len hold 0 and -1, the others are left as they were.  Both may be the input arrays themselves.
+ * Slots are thus in no order; positions tells which token a slot holds.
+ *
+ * specattn_evict_move applies the moves to the rows of any caches of the sequences, in place: keys and values in any type,
+ * codes and scales, the draft model's cache.  The kv heads h*H_kv/H .. (h+1)*H_kv/H - 1 of a plane follow row h.  Moves that
+ * lead outside [0, n_max) or into a page outside the pool are left out.
+ */
+typedef struct specattn_evict_args {
+    const float *probs;          /* [B][H_draft][S][n_max] fp32: row (b, x, s) starts at b*probs_stride_b +
+                                    (x*S + s)*probs_stride_row; NULL (with H_draft = S = 0) = nothing to add */
+    int64_t probs_stride_b, probs_stride_row;            /* elements */
+    int32_t B, H, n_max;         /* score rows: B * H; n_max <= SPECATTN_MAX_N slots each */
+    int32_t H_draft, S;          /* H_draft % H == 0 */
+    const float *scores;         /* [B][H][n_max] fp32, last dim contiguous */
+    const int32_t *positions;    /* [B][H][n_max] place in the text of the token in each slot; same strides */
+    float *scores_out;           /* may be `scores` */
+    int32_t *positions_out;      /* may be `positions` */
+    int64_t row_stride_b, row_stride_h;                  /* elements, of the four arrays above */
+    const int32_t *seq_lens;     /* [B] occupied slots, or NULL for n_max */
+    const int32_t *next_positions;   /* [B] place in the text of the sequence's next token */
+    double decay;                /* in [0, 1] */
+    int32_t budget;              /* slots kept per row, >= 1 */
+    int32_t sinks, recent;       /* sinks + recent <= budget */
+    int32_t *move_src, *move_dst;    /* out [B*H][move_stride_row] */
+    int64_t move_stride_row;     /* elements, >= move_capacity */
+    int32_t move_capacity;       /* >= min(budget, n_max - budget): no row has more moves */
+    int32_t *move_counts;        /* out [B*H] */
+    int32_t *new_lens;           /* out [B] min(len, budget); not seq_lens itself */
+    uint32_t *row_flags;         /* out [B*H], optional: SPECATTN_ROW_INVALID if one of the row's new scores is NaN */
+} specattn_evict_args;
+
+/* workspace: specattn_evict_workspace_size(args) bytes, 256-byte aligned */
+specattn_status specattn_evict_select(const specattn_evict_args *args, void *workspace, size_t workspace_bytes,
+                                      void *stream);
+size_t specattn_evict_workspace_size(const specattn_evict_args *args);     /* 0 for invalid arguments */
+
+#define SPECATTN_MAX_PLANES 8
+typedef struct specattn_move_plane {
+    void *data;                  /* contiguous [B][H_kv][n_max][row_bytes] or pool [num_pages][H_kv][page_size][row_bytes] */
+    int64_t stride_b, stride_h, stride_n, stride_page;   /* bytes; _b contiguous, _page paged */
+    int32_t row_bytes;           /* a multiple of 4 up to 8192; data and strides are multiples of the largest of 16, 8, 4 dividing it */
+    int32_t H_kv;                /* a multiple of H */
+    int32_t num_pages;           /* paged: pages of this pool */
+} specattn_move_plane;
+
+typedef struct specattn_move_args {
+    const int32_t *move_src, *move_dst, *move_counts;    /* as written by specattn_evict_select */
+    int64_t move_stride_row;
+    int32_t move_capacity;
+    int32_t B, H, n_max;
+    const int32_t *page_table;   /* [B][max_pages_per_seq] for all planes, or NULL = all contiguous */
+    int32_t page_size, max_pages_per_seq;
+    int32_t num_planes;          /* 1 .. SPECATTN_MAX_PLANES */
+    specattn_move_plane planes[SPECATTN_MAX_PLANES];
+} specattn_move_args;
+
+specattn_status specattn_evict_move(const specattn_move_args *args, void *stream);
+
 /* Text of the calling thread's last error ("" if none).  Never NULL. */
 const char *specattn_last_error(void);
 

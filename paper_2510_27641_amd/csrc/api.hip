@@ -1,6 +1,7 @@
 // C ABI of the library: host-side argument checks and dispatch.  Nothing here touches device
 // memory; every check runs before the first launch so that a failing call writes nothing.
 #include "common.h"
+#include "mx.h"
 
 #include <algorithm>
 #include <cmath>
@@ -217,6 +218,191 @@ AttnLaunch make_attn(const specattn_attn_args *a)
     l.workspace_bytes = a->workspace_bytes;
     l.seq_lens = a->seq_lens;
     return l;
+}
+
+// ---- the 4-bit cache and the eviction --------------------------------------------------------
+specattn_status check_pages(const int32_t *page_table, int page_size, int max_pages, int n_max)
+{
+    if (!is_pow2(page_size)) { set_error("page_size must be a power of two"); return SPECATTN_ESHAPE; }
+    if (page_table && (int64_t)max_pages * page_size < n_max) { set_error("page table is shorter than n_max"); return SPECATTN_ESHAPE; }
+    return SPECATTN_OK;
+}
+
+specattn_status check_mx_cache(const specattn_mx_cache *c, bool pool)
+{
+    if (!c->codes || !c->scales) { set_error("codes and scales must not be NULL"); return SPECATTN_EINVAL; }
+    if (c->B <= 0 || c->H_kv <= 0 || c->n_max <= 0 || c->d <= 0) { set_error("the cache's sizes must be positive"); return SPECATTN_EINVAL; }
+    if (c->d != 64 && c->d != 128) { set_error("d must be 64 or 128"); return SPECATTN_ESHAPE; }
+    if ((int64_t)c->B * c->H_kv > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
+    if (pool) {
+        const specattn_status st = check_pages(c->page_table, c->page_size, c->max_pages_per_seq, c->n_max);
+        if (st != SPECATTN_OK) return st;
+        if (c->num_pages <= 0) { set_error("num_pages must be positive"); return SPECATTN_EINVAL; }
+        if (c->codes_stride_page <= 0 || c->scales_stride_page <= 0) { set_error("page strides must be positive"); return SPECATTN_ESHAPE; }
+    }
+    if (c->codes_stride_n < c->d || c->scales_stride_n < c->d / 16) { set_error("codes_stride_n and scales_stride_n must not be smaller than d and d / 16"); return SPECATTN_ESHAPE; }
+    if (c->codes_stride_h < 0 || c->scales_stride_h < 0 || (!pool && (c->codes_stride_b < 0 || c->scales_stride_b < 0))) { set_error("strides must not be negative"); return SPECATTN_ESHAPE; }
+    const int64_t codes[] = {c->codes_stride_h, c->codes_stride_n, pool ? c->codes_stride_page : c->codes_stride_b};
+    const int64_t scales[] = {c->scales_stride_h, c->scales_stride_n, pool ? c->scales_stride_page : c->scales_stride_b};
+    for (int i = 0; i < 3; ++i)
+        if (codes[i] % 16 || scales[i] % 4) { set_error("strides of the codes must be multiples of 16 bytes, of the scales of 4"); return SPECATTN_EALIGN; }
+    if (!aligned(c->codes, 16) || !aligned(c->scales, 4)) { set_error("codes must be 16-byte, scales 4-byte aligned"); return SPECATTN_EALIGN; }
+    return SPECATTN_OK;
+}
+
+MxCache make_mx_cache(const specattn_mx_cache *c, bool pool)
+{
+    MxCache m{};
+    m.codes = c->codes; m.scales = c->scales;
+    m.codes_b = c->codes_stride_b; m.codes_h = c->codes_stride_h; m.codes_n = c->codes_stride_n; m.codes_page = c->codes_stride_page;
+    m.scales_b = c->scales_stride_b; m.scales_h = c->scales_stride_h; m.scales_n = c->scales_stride_n; m.scales_page = c->scales_stride_page;
+    m.page_table = c->page_table;
+    m.page_shift = pool ? log2i(c->page_size) : 0;
+    m.max_pages = c->max_pages_per_seq;
+    m.num_pages = c->num_pages;
+    m.B = c->B; m.H_kv = c->H_kv; m.n_max = c->n_max; m.d = c->d;
+    return m;
+}
+
+specattn_status check_mx_rows(const specattn_mx_rows_args *r)
+{
+    if (!r) { set_error("rows args are NULL"); return SPECATTN_EINVAL; }
+    const specattn_status st = check_mx_cache(&r->cache, r->cache.page_table != nullptr);
+    if (st != SPECATTN_OK) return st;
+    if (!r->k || !r->v) { set_error("k and v must not be NULL"); return SPECATTN_EINVAL; }
+    if (r->T <= 0) { set_error("T must be positive"); return SPECATTN_EINVAL; }
+    if (r->dtype != SPECATTN_F32 && r->dtype != SPECATTN_BF16 && r->dtype != SPECATTN_F16) { set_error("unknown dtype %d", (int)r->dtype); return SPECATTN_EUNSUPPORTED; }
+    if (!aligned(r->k, 16) || !aligned(r->v, 16)) { set_error("k and v must be 16-byte aligned"); return SPECATTN_EALIGN; }
+    const int64_t es = r->dtype == SPECATTN_F32 ? 4 : 2;
+    if ((r->stride_b * es) % 16 || (r->stride_h * es) % 16 || (r->stride_t * es) % 16) { set_error("strides must be multiples of 16 bytes"); return SPECATTN_EALIGN; }
+    return SPECATTN_OK;
+}
+
+MxRowsLaunch make_mx_rows(const specattn_mx_rows_args *r)
+{
+    MxRowsLaunch l{};
+    l.c = make_mx_cache(&r->cache, r->cache.page_table != nullptr);
+    l.k = r->k; l.v = r->v;
+    l.dtype = (int)r->dtype;
+    l.T = r->T;
+    l.stride_b = r->stride_b; l.stride_h = r->stride_h; l.stride_t = r->stride_t;
+    l.starts = r->starts; l.counts = r->counts;
+    return l;
+}
+
+specattn_status check_mx_attn(const specattn_mx_attn_args *a)
+{
+    if (!a) { set_error("attention args are NULL"); return SPECATTN_EINVAL; }
+    const specattn_mx_cache *c = &a->cache;
+    const bool pool = c->page_table != nullptr || a->indices_are_physical;
+    const specattn_status st = check_mx_cache(c, pool);
+    if (st != SPECATTN_OK) return st;
+    if (!a->q || (!a->out && !a->out_lowp)) { set_error("q and one of out and out_lowp must not be NULL"); return SPECATTN_EINVAL; }
+    const bool dense = !a->indices && !a->counts;
+    if (!dense && (!a->indices || !a->counts)) { set_error("indices and counts must both be given, or both be NULL (dense)"); return SPECATTN_EINVAL; }
+    if (dense && a->indices_are_physical) { set_error("indices_are_physical without an index list"); return SPECATTN_EINVAL; }
+    if (a->H_q <= 0 || a->T <= 0) { set_error("sizes must be positive"); return SPECATTN_EINVAL; }
+    if (a->dtype != SPECATTN_BF16 && a->dtype != SPECATTN_F16) { set_error("queries of a 4-bit cache are bf16 or fp16"); return SPECATTN_EUNSUPPORTED; }
+    if (a->H_q % c->H_kv) { set_error("H_q is not a multiple of H_kv"); return SPECATTN_ESHAPE; }
+    if (a->T > SPECATTN_MAX_T) { set_error("T exceeds %d", SPECATTN_MAX_T); return SPECATTN_ESHAPE; }
+    if (!dense && a->idx_capacity < 1) { set_error("idx_capacity must be at least 1"); return SPECATTN_ESHAPE; }
+    if (!dense && a->idx_stride_row < a->idx_capacity) { set_error("idx_stride_row is smaller than idx_capacity"); return SPECATTN_ESHAPE; }
+    if (a->chunk_size < 0 || (a->chunk_size > 1 && (!is_pow2(a->chunk_size) || a->chunk_size > 1024))) { set_error("chunk_size must be 0, 1 or a power of two up to 1024"); return SPECATTN_ESHAPE; }
+    if (a->chunk_size > 1 && (dense || a->indices_are_physical)) { set_error("chunk lists are not available with dense calls or physical indices"); return SPECATTN_EUNSUPPORTED; }
+    // positions of a row count in 31 bits, and row offsets go to the kernel in units of 16 (codes) and 4 bytes (scales) in 32 bits
+    if (a->chunk_size > 1 && (int64_t)a->idx_capacity * a->chunk_size > INT32_MAX - 65536) { set_error("idx_capacity * chunk_size is too large"); return SPECATTN_ESHAPE; }
+    if ((dense ? c->n_max : a->idx_capacity) > INT32_MAX - 65536) { set_error("too many positions per row"); return SPECATTN_ESHAPE; }
+    const __int128 reach = pool ? (__int128)(c->num_pages - 1) * c->codes_stride_page + (__int128)(c->page_size - 1) * c->codes_stride_n : (__int128)(c->n_max - 1) * c->codes_stride_n;
+    const __int128 scales_reach = pool ? (__int128)(c->num_pages - 1) * c->scales_stride_page + (__int128)(c->page_size - 1) * c->scales_stride_n : (__int128)(c->n_max - 1) * c->scales_stride_n;
+    if (reach >= ((__int128)1 << 36) || scales_reach >= ((__int128)1 << 34)) { set_error("the rows of a kv head must lie within 64 GiB of its first one (their scales within 16 GiB)"); return SPECATTN_ESHAPE; }
+    if ((a->k_new == nullptr) != (a->v_new == nullptr)) { set_error("k_new and v_new must both be given or both be NULL"); return SPECATTN_EINVAL; }
+    if (!aligned(a->q, 16) || !aligned(a->k_new, 16) || !aligned(a->v_new, 16) || !aligned(a->out, 16) || !aligned(a->out_lowp, 16)) { set_error("q, k_new, v_new, out and out_lowp must be 16-byte aligned"); return SPECATTN_EALIGN; }
+    if (a->q_stride_b % 8 || a->q_stride_h % 8 || a->q_stride_t % 8) { set_error("strides must be multiples of 16 bytes"); return SPECATTN_EALIGN; }
+    return SPECATTN_OK;
+}
+
+MxAttnLaunch make_mx_attn(const specattn_mx_attn_args *a)
+{
+    const specattn_mx_cache *c = &a->cache;
+    const bool pool = c->page_table != nullptr || a->indices_are_physical;
+    MxAttnLaunch m{};
+    m.c = make_mx_cache(c, pool);
+    if (a->indices_are_physical) m.c.page_table = nullptr;
+    AttnLaunch &l = m.a;
+    l.q = a->q;
+    l.dtype = (int)a->dtype;
+    l.B = c->B; l.H_q = a->H_q; l.H_kv = c->H_kv; l.T = a->T; l.d = c->d; l.n_max = c->n_max;
+    l.sm_scale = a->sm_scale > 0.0f ? a->sm_scale : 1.0f / std::sqrt((float)c->d);
+    l.q_stride_b = a->q_stride_b; l.q_stride_h = a->q_stride_h; l.q_stride_t = a->q_stride_t;
+    l.page_table = m.c.page_table;
+    l.page_shift = m.c.page_shift;
+    l.max_pages = c->max_pages_per_seq;
+    l.indices = a->indices;
+    l.idx_stride = a->idx_stride_row;
+    l.counts = a->counts;
+    l.idx_capacity = a->idx_capacity;
+    l.indices_are_physical = a->indices_are_physical;
+    l.chunk_shift = a->chunk_size > 1 ? log2i(a->chunk_size) : 0;
+    l.dense = (!a->indices && !a->counts) ? 1 : 0;
+    l.k_new = a->k_new;
+    l.v_new = a->v_new;
+    l.out = a->out;
+    l.out_lowp = a->out_lowp;
+    l.lse = a->lse;
+    l.workspace = a->workspace;
+    l.workspace_bytes = a->workspace_bytes;
+    l.seq_lens = a->seq_lens;
+    return m;
+}
+
+specattn_status check_evict(const specattn_evict_args *e)
+{
+    if (!e) { set_error("evict args are NULL"); return SPECATTN_EINVAL; }
+    if (!e->scores || !e->positions || !e->scores_out || !e->positions_out || !e->next_positions || !e->move_src || !e->move_dst || !e->move_counts || !e->new_lens) { set_error("scores, positions, their outputs, next_positions, the moves and new_lens must not be NULL"); return SPECATTN_EINVAL; }
+    if (e->B <= 0 || e->H <= 0 || e->n_max <= 0 || e->budget <= 0) { set_error("B, H, n_max and budget must be positive"); return SPECATTN_EINVAL; }
+    if (!(e->decay >= 0.0 && e->decay <= 1.0)) { set_error("decay must lie in [0, 1]"); return SPECATTN_EINVAL; }
+    if (e->new_lens == e->seq_lens) { set_error("new_lens must not be seq_lens"); return SPECATTN_EINVAL; }
+    if (e->n_max > SPECATTN_MAX_N) { set_error("n_max %d exceeds %d", e->n_max, SPECATTN_MAX_N); return SPECATTN_ESHAPE; }
+    if (e->probs) {
+        if (e->H_draft <= 0 || e->S <= 0) { set_error("H_draft and S must be positive"); return SPECATTN_EINVAL; }
+        if (e->H_draft % e->H) { set_error("H_draft is not a multiple of H"); return SPECATTN_ESHAPE; }
+        if ((int64_t)e->B * e->H_draft * e->S > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
+        if (e->probs_stride_row < e->n_max) { set_error("probs_stride_row is smaller than n_max"); return SPECATTN_ESHAPE; }
+    }
+    if ((int64_t)e->B * e->H > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
+    if (e->row_stride_h < e->n_max || e->row_stride_b < e->n_max) { set_error("row strides are smaller than n_max"); return SPECATTN_ESHAPE; }
+    if (e->sinks < 0 || e->recent < 0 || (int64_t)e->sinks + e->recent > e->budget) { set_error("sinks and recent must not be negative, nor exceed the budget together"); return SPECATTN_ESHAPE; }
+    if (e->move_capacity < 1 || e->move_capacity < std::min(e->budget, e->n_max - e->budget)) { set_error("move_capacity must be at least 1 and hold min(budget, n_max - budget) moves"); return SPECATTN_ESHAPE; }
+    if (e->move_stride_row < e->move_capacity) { set_error("move_stride_row is smaller than move_capacity"); return SPECATTN_ESHAPE; }
+    return SPECATTN_OK;
+}
+
+specattn_status check_move(const specattn_move_args *m)
+{
+    if (!m) { set_error("move args are NULL"); return SPECATTN_EINVAL; }
+    if (!m->move_src || !m->move_dst || !m->move_counts) { set_error("the moves must not be NULL"); return SPECATTN_EINVAL; }
+    if (m->B <= 0 || m->H <= 0 || m->n_max <= 0) { set_error("B, H and n_max must be positive"); return SPECATTN_EINVAL; }
+    if (m->n_max > SPECATTN_MAX_N) { set_error("n_max %d exceeds %d", m->n_max, SPECATTN_MAX_N); return SPECATTN_ESHAPE; }
+    if (m->move_capacity < 1 || m->move_capacity > m->n_max) { set_error("move_capacity must lie in 1..n_max"); return SPECATTN_ESHAPE; }
+    if (m->move_stride_row < m->move_capacity) { set_error("move_stride_row is smaller than move_capacity"); return SPECATTN_ESHAPE; }
+    if (m->num_planes < 1 || m->num_planes > SPECATTN_MAX_PLANES) { set_error("num_planes must lie in 1..%d", SPECATTN_MAX_PLANES); return SPECATTN_ESHAPE; }
+    if (m->page_table) {
+        const specattn_status st = check_pages(m->page_table, m->page_size, m->max_pages_per_seq, m->n_max);
+        if (st != SPECATTN_OK) return st;
+    }
+    for (int i = 0; i < m->num_planes; ++i) {
+        const specattn_move_plane *p = &m->planes[i];
+        if (!p->data) { set_error("plane %d has no data", i); return SPECATTN_EINVAL; }
+        if (p->H_kv <= 0 || p->H_kv % m->H) { set_error("H_kv of plane %d is not a positive multiple of H", i); return SPECATTN_ESHAPE; }
+        if ((int64_t)m->B * p->H_kv > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
+        if (p->row_bytes < 4 || p->row_bytes > 8192 || p->row_bytes % 4) { set_error("row_bytes of plane %d must be a multiple of 4 up to 8192", i); return SPECATTN_ESHAPE; }
+        if (p->stride_n < p->row_bytes) { set_error("stride_n of plane %d is smaller than row_bytes", i); return SPECATTN_ESHAPE; }
+        if (m->page_table && (p->num_pages <= 0 || p->stride_page <= 0)) { set_error("plane %d needs num_pages and a page stride", i); return SPECATTN_ESHAPE; }
+        const int unit = p->row_bytes % 16 == 0 ? 16 : p->row_bytes % 8 == 0 ? 8 : 4;
+        const int64_t outer = m->page_table ? p->stride_page : p->stride_b;
+        if (!aligned(p->data, unit) || p->stride_h % unit || p->stride_n % unit || outer % unit) { set_error("data and strides of plane %d must be multiples of %d bytes", i, unit); return SPECATTN_EALIGN; }
+    }
+    return SPECATTN_OK;
 }
 
 }  // namespace
@@ -487,6 +673,63 @@ size_t specattn_workspace_size(const specattn_select_args *sel, const specattn_a
     return workspace_bytes(sel, attn, true);
 }
 
+specattn_status specattn_mx_store(const specattn_mx_rows_args *args, void *stream)
+{
+    clear_error();
+    const specattn_status st = check_mx_rows(args);
+    if (st != SPECATTN_OK) return st;
+    return launch_mx_store(make_mx_rows(args), static_cast<hipStream_t>(stream));
+}
+
+specattn_status specattn_mx_load(const specattn_mx_rows_args *args, void *stream)
+{
+    clear_error();
+    const specattn_status st = check_mx_rows(args);
+    if (st != SPECATTN_OK) return st;
+    return launch_mx_load(make_mx_rows(args), static_cast<hipStream_t>(stream));
+}
+
+size_t specattn_mx_workspace_size(const specattn_mx_attn_args *a)
+{
+    if (!a || a->cache.B <= 0 || a->cache.H_kv <= 0 || a->H_q <= 0 || a->T <= 0 || a->T > SPECATTN_MAX_T || a->H_q % a->cache.H_kv) return 0;
+    if ((a->cache.d != 64 && a->cache.d != 128) || (int64_t)a->cache.B * a->cache.H_kv > (1 << 24)) return 0;
+    return mx_attn_workspace_bytes(a->cache.B * a->cache.H_kv, a->H_q / a->cache.H_kv, a->T, a->cache.d);
+}
+
+specattn_status specattn_mx_decode_attn(const specattn_mx_attn_args *args, void *stream)
+{
+    clear_error();
+    specattn_status st = check_mx_attn(args);
+    if (st != SPECATTN_OK) return st;
+    st = check_workspace(args->workspace, args->workspace_bytes, specattn_mx_workspace_size(args));
+    if (st != SPECATTN_OK) return st;
+    return launch_mx_attn(make_mx_attn(args), static_cast<hipStream_t>(stream));
+}
+
+size_t specattn_evict_workspace_size(const specattn_evict_args *e)
+{
+    if (!e || e->B <= 0 || e->H <= 0 || e->n_max <= 0 || e->n_max > SPECATTN_MAX_N || (int64_t)e->B * e->H > (1 << 24)) return 0;
+    return evict_workspace_bytes(e);
+}
+
+specattn_status specattn_evict_select(const specattn_evict_args *args, void *workspace, size_t workspace_bytes, void *stream)
+{
+    clear_error();
+    specattn_status st = check_evict(args);
+    if (st != SPECATTN_OK) return st;
+    st = check_workspace(workspace, workspace_bytes, evict_workspace_bytes(args));
+    if (st != SPECATTN_OK) return st;
+    return launch_evict_select(args, workspace, static_cast<hipStream_t>(stream));
+}
+
+specattn_status specattn_evict_move(const specattn_move_args *args, void *stream)
+{
+    clear_error();
+    const specattn_status st = check_move(args);
+    if (st != SPECATTN_OK) return st;
+    return launch_evict_move(args, static_cast<hipStream_t>(stream));
+}
+
 // Device address of this GPU's copy of `scratch`, looked up once per device (any thread may call).
 static specattn_status static_scratch(void **out)
 {
@@ -547,11 +790,13 @@ specattn_status specattn_init(void)
     if (sg != SPECATTN_OK) return sg;
     const specattn_status sm = layer_map_configure();
     if (sm != SPECATTN_OK) return sm;
+    const specattn_status sx = mx_attn_configure();
+    if (sx != SPECATTN_OK) return sx;
     return attn_mfma_configure();
 }
 
 const char *specattn_last_error(void) { return g_error; }
 
-int specattn_version(void) { return 1009; }
+int specattn_version(void) { return 1010; }
 
 }  // extern "C"
