@@ -49,7 +49,8 @@ template <int D> struct Geo {
 
 // What a wave holds of a tile between request and use.
 template <int D> struct Tile {
-    uint32_t k[2][Geo<D>::KW], k_scale[2], v[8], v_scale[8];
+    uint32_t k[2][Geo<D>::KW], v[8];
+    uint32_t scale[D / 64];               // all scales of position lane % 32
 };
 
 template <int D, int NQ, int QP> struct Lds {
@@ -58,7 +59,9 @@ template <int D, int NQ, int QP> struct Lds {
     int prefix[MAX_ROWS + 1];
     int count[MAX_ROWS];
     int red[2][NW];
-    uint32_t codes_at[NW][TILE], scales_at[NW][TILE];                         // row offsets of a wave's next tile
+    uint32_t codes_at[NW][TILE];                                              // row offsets of a wave's next tile
+    uint32_t k_scale[NW][TILE];                                               // [position][block]
+    uint8_t v_scale[NW][4][TILE];                                             // [block][position]
     float ml[NW][16][2];
     uint8_t q[Q_BYTES] __attribute__((aligned(16)));
     float o[NW][16][Geo<D>::PITCH] __attribute__((aligned(16)));
@@ -243,10 +246,11 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
         };
         auto request = [&](Tile<D> &x, int slot, int page) {
             const uint32_t in = paged ? (uint32_t)slot & ((1u << a.page_shift) - 1) : (uint32_t)slot;
+            const uint8_t *from = scales + ((uint64_t)(in * scales_n + (uint32_t)page * scales_page) << 2);
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) x.scale[i] = reinterpret_cast<const uint32_t *>(from)[i];
             lds.codes_at[wave][lane % TILE] = in * codes_n + (uint32_t)page * codes_page;
-            lds.scales_at[wave][lane % TILE] = in * scales_n + (uint32_t)page * scales_page;
             const uint8_t *kc = codes + (D / 8) * g, *vc = codes + D / 2 + (D / 32) * low;
-            const uint8_t *ks = scales + (D == 128 ? g : g / 2), *vs = scales + D / 32 + low / (D == 128 ? 4 : 8);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint8_t *src = kc + ((uint64_t)lds.codes_at[wave][16 * i + low] << 4);
@@ -259,26 +263,29 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
                     x.k[i][0] = w[0];
                     x.k[i][1] = w[1];
                 }
-                x.k_scale[i] = ks[(uint64_t)lds.scales_at[wave][16 * i + low] << 2];
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const u32x4 at = *reinterpret_cast<const u32x4 *>(&lds.codes_at[wave][16 * i + 4 * g]);
-                const u32x4 sat = *reinterpret_cast<const u32x4 *>(&lds.scales_at[wave][16 * i + 4 * g]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint8_t *src = vc + ((uint64_t)at[j] << 4);
                     if constexpr (D == 128) x.v[4 * i + j] = *reinterpret_cast<const uint32_t *>(src);
                     else x.v[4 * i + j] = *reinterpret_cast<const uint16_t *>(src);
-                    x.v_scale[4 * i + j] = vs[(uint64_t)sat[j] << 2];
                 }
             }
         };
         auto use = [&](const Tile<D> &x, int t) {
+            {
+                const uint32_t of_values = D == 128 ? x.scale[D / 64 - 1] : x.scale[0] >> 16;
+                lds.k_scale[wave][lane % TILE] = x.scale[0];
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) lds.v_scale[wave][i][lane % TILE] = (uint8_t)(of_values >> (8 * i));
+            }
             f32x4 s[NQ][2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float scale = scale_of(x.k_scale[i]);
+                const float scale = scale_of(reinterpret_cast<const uint8_t *>(&lds.k_scale[wave][16 * i + low])[D == 128 ? g : g / 2]);
 #pragma unroll
                 for (int qt = 0; qt < NQ; ++qt) s[qt][i] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -307,6 +314,7 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
             uint32_t w[NQ][PARTS][4];
 #pragma unroll
             for (int qt = 0; qt < NQ; ++qt) {
+                __builtin_amdgcn_sched_barrier(0);
                 float most = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -338,11 +346,17 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
                     }
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
             float scale[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) scale[j] = scale_of(x.v_scale[j]);
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t four = *reinterpret_cast<const uint32_t *>(&lds.v_scale[wave][low / (D == 128 ? 4 : 8)][16 * i + 4 * g]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) scale[4 * i + j] = scale_of((four >> (8 * j)) & 255);
+            }
             auto columns = [&](auto which) {                      // elements 2B and 2B + 1 of the lane's eight (four)
                 constexpr int B = decltype(which)::value;
+                __builtin_amdgcn_sched_barrier(0);
                 uint32_t even[4], odd[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -374,17 +388,12 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
             // (tiles past the share's end are found, clamped to the row, and not used)
             slot = slot_of(t + NW, list_word(t + NW));
             int page = page_of(slot), word = list_word(t + 2 * NW);
-            while (true) {
+            for (; t < t1; t += NW) {
                 request(y, slot, page);
                 slot = slot_of(t + 2 * NW, word); page = page_of(slot); word = list_word(t + 3 * NW);
+                __builtin_amdgcn_sched_barrier(0);
                 use(x, t);
-                t += NW;
-                if (t >= t1) break;
-                request(x, slot, page);
-                slot = slot_of(t + 2 * NW, word); page = page_of(slot); word = list_word(t + 3 * NW);
-                use(y, t);
-                t += NW;
-                if (t >= t1) break;
+                x = y;
             }
         }
 
