@@ -6,10 +6,14 @@
 // in slot share + row; mx_merge_kernel combines a row's partials in share order.  Inside a share tile k goes to wave k mod 8,
 // so every sum is taken in a fixed order.
 //
-// Per wave and tile, everything from memory goes straight into the registers of the lane that needs it:
-//   keys     lane (p, g) = (lane % 16, lane / 16) takes a quarter (d = 64: of 32 bytes) of the codes of positions p and 16 + p,
-//            d/4 elements that lie in one block, so one scale serves all of a lane's conversions.  The contraction runs over
-//            the elements in the order the lanes hold them; the queries are laid out to match.
+// Per wave and tile, codes and scales go from memory straight into LDS (global_load_lds): d/16 lanes fetch the d bytes of a
+// position as one piece, 1 KiB per instruction, and the list words and page numbers that tell where they lie come the same way, two and
+// four tiles earlier.  A wave holds three tiles: one in use, two on their way, 68 KiB per CU at d = 128, and waits by the
+// number of requests behind the ones it needs.  (Requests straight into registers, one tile ahead: a tile took as long as a trip
+// to memory; 8 dense sequences of up to 32768 positions 45 us.)  From LDS,
+//   keys     lane (p, g) = (lane % 16, lane / 16) takes a quarter of the codes of positions p and 16 + p, d/4 elements that lie
+//            in one block, so one scale serves all of a lane's conversions.  The contraction runs over the elements in the order
+//            the lanes hold them; the queries are laid out to match.
 //   values   lane (c, g) takes d/16 consecutive elements of the eight positions 4g .. 4g+3 and 16+4g .. 16+4g+3: what a
 //            column tile of the second product needs of those positions, for d/16 column tiles
 //   S^T = K Q^T, O^T += V^T P^T on mfma 16x16x32 in bf16.  The codes times their scales are exact in bf16, bf16 queries are
@@ -45,27 +49,59 @@ template <int D> struct Geo {
     static constexpr int KW = D / 32;     // words of key codes per lane and position: k-steps of the first product
     static constexpr int DT = D / 16;     // column tiles of the output, and value elements per lane and position
     static constexpr int PITCH = D + 4;   // floats of a row in the merge buffer
+    static constexpr int LPR = D / 16;    // lanes that fetch the codes of one position
+    static constexpr int RPI = 64 / LPR;  // positions per instruction
+    static constexpr int CI = TILE / RPI; // instructions per tile: position CI * j + k is the j-th of instruction k
+    static constexpr int CODES = TILE * D;
+    // 16-byte piece c of the codes of position `pos` lies in place c ^ swz(pos), so that both reads spread over all banks: keys, one piece
+    // of each of 16 positions, and values, 64 (32) bytes of the positions 4g + i of four g.
+    static __device__ __forceinline__ int swz(int pos) { return D == 128 ? (pos & 3) | ((pos >> 3 & 1) << 2) : (pos & 1) | (pos >> 3 & 1) << 1; }
+    static __device__ __forceinline__ int piece(int pos, int c) { return (pos % CI) * 1024 + (pos / CI) * D + ((c ^ swz(pos)) * 16); }
 };
 
-// What a wave holds of a tile between request and use.
-template <int D> struct Tile {
-    uint32_t k[2][Geo<D>::KW], v[8];
-    uint32_t scale[D / 64];               // all scales of position lane % 32
+constexpr int DEPTH = 3;                  // tiles of a wave: in use and on their way
+
+// A wave's part of the LDS.
+template <int D> struct WaveLds {
+    uint8_t codes[DEPTH][Geo<D>::CODES];
+    uint32_t scales[DEPTH][64];           // d = 128: of the keys of the 32 positions, then of the values; d = 64: of both
+    uint32_t words[DEPTH][64];            // list words
+    int32_t pages[DEPTH][64];             // page numbers
+    uint32_t codes_at[TILE];              // row offsets of the tile that is requested next
+};
+
+template <int D> struct MergeLds {
+    float o[NW][16][Geo<D>::PITCH];
+    float ml[NW][16][2];
 };
 
 template <int D, int NQ, int QP> struct Lds {
     static constexpr bool Q = NQ * QP > 2;                                    // queries wait in LDS, else in registers
     static constexpr int Q_BYTES = Q ? NQ * QP * Geo<D>::KW * 1024 : 16;
+    union {
+        WaveLds<D> wave[NW];
+        MergeLds<D> merge;
+    };
+    uint8_t q[Q_BYTES] __attribute__((aligned(16)));
     int prefix[MAX_ROWS + 1];
     int count[MAX_ROWS];
     int red[2][NW];
-    uint32_t codes_at[NW][TILE];                                              // row offsets of a wave's next tile
-    uint32_t k_scale[NW][TILE];                                               // [position][block]
-    uint8_t v_scale[NW][4][TILE];                                             // [block][position]
-    float ml[NW][16][2];
-    uint8_t q[Q_BYTES] __attribute__((aligned(16)));
-    float o[NW][16][Geo<D>::PITCH] __attribute__((aligned(16)));
 };
+static_assert(sizeof(Lds<128, 4, 2>) <= 160 * 1024, "a workgroup must fit a CU's LDS");
+
+// Requests 16 or 4 bytes per lane from `src` to `to` + 16 or 4 * lane in LDS.  Counts as one request of the wave in order; nobody but
+// wait_requests waits for it.
+__device__ __forceinline__ void request16(const void *src, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(src), "s"(to) : "memory", "m0");
+}
+__device__ __forceinline__ void request4(const void *src, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(to) : "memory", "m0");
+}
+// Waits until at most N of the wave's requests are under way.
+template <int N> __device__ __forceinline__ void wait_requests() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
+__device__ __forceinline__ uint32_t lds_offset(const void *p) { return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p); }
 
 __device__ __forceinline__ uint32_t bits(bf16x2 x) { return __builtin_bit_cast(uint32_t, x); }
 __device__ __forceinline__ uint32_t to_bf16(float a, float b) { return bits(__builtin_convertvector(f32x2{a, b}, bf16x2)); }
@@ -77,7 +113,7 @@ __device__ __forceinline__ f32x4 mfma(const uint32_t (&a)[4], const uint32_t (&b
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
-// Elements 2B and 2B + 1 of eight codes.
+// Elements 2B and 2B + 1 of eight codes.  (The conversion takes a scale's exponent alone.)
 template <int B> __device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale) { return bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, B)); }
 __device__ __forceinline__ float shuffle_xor(float x, int mask) { return __shfl_xor(x, mask, 64); }
 
@@ -96,7 +132,7 @@ __device__ __forceinline__ void sum_two(int a, int b, int (&red)[2][NW], int &ta
 
 struct Share { int size, head; };         // units of the line per workgroup, and ahead of a row's tiles
 
-template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void mx_attn_kernel(MxAttnLaunch p, int row0, int rows, int heads)
+template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS) void mx_attn_kernel(MxAttnLaunch p, int row0, int rows, int heads)
 {
     typedef Geo<D> G;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_bytes[];
@@ -229,68 +265,62 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
         const uint32_t codes_page = (uint32_t)(p.c.codes_page >> 4), scales_page = (uint32_t)(p.c.scales_page >> 2);
         const int last_slot = a.indices_are_physical ? INT32_MAX : a.n_max - 1;
 
-        // A tile's positions are found in three steps, each an iteration ahead of the next: list word, page, offsets.
-        auto list_rank = [&](int t) { return min(t * TILE + lane % TILE, n - 1); };
-        auto list_word = [&](int t) -> int {
-            const int jj = list_rank(t);
-            return a.dense ? jj : list[jj >> a.chunk_shift];
-        };
-        auto slot_of = [&](int t, int word) -> int {
-            if (a.chunk_shift) word = (word << a.chunk_shift) | (list_rank(t) & ((1 << a.chunk_shift) - 1));
+        // A tile goes through three steps, each two tiles ahead of the next: its list words are requested; its pages; its codes and
+        // scales.  Tiles are counted per wave: the wave's tile i is tile t0 + wave + i * NW of the row.  (Tiles past the share's end are
+        // requested like others, clamped to the row, and not used.)
+        WaveLds<D> &mine = lds.wave[wave];
+        const uint32_t codes_lds = lds_offset(mine.codes), scales_lds = lds_offset(mine.scales), words_lds = lds_offset(mine.words), pages_lds = lds_offset(mine.pages);
+        const bool listed = !a.dense, looked_up = pages != nullptr;
+        const int base_tile = t0 + wave;
+        auto list_rank = [&](int i) { return min((base_tile + i * NW) * TILE + lane % TILE, n - 1); };
+        auto list_at = [&](int i) { return list + (list_rank(i) >> a.chunk_shift); };
+        auto slot_of = [&](int i, int word) -> int {
+            if (!listed) return list_rank(i);                     // (below the length: inside the cache)
+            if (a.chunk_shift) word = (word << a.chunk_shift) | (list_rank(i) & ((1 << a.chunk_shift) - 1));
             return min(max(word, 0), last_slot);
         };
-        auto page_of = [&](int slot) -> int {
-            if (!paged) return 0;
-            const int page = pages ? pages[slot >> a.page_shift] : slot >> a.page_shift;
-            return min(max(page, 0), p.c.num_pages - 1);
+        auto request_words = [&](int i, int at) { if (listed) request4(list_at(i), words_lds + at * 256); };
+        auto request_pages = [&](int slot, int at) { if (looked_up) request4(pages + (slot >> a.page_shift), pages_lds + at * 256); };
+        auto request_codes = [&](int slot, int page, int at) {
+            uint32_t in = (uint32_t)slot;
+            if (paged) {
+                if (!looked_up) page = slot >> a.page_shift;
+                page = min(max(page, 0), p.c.num_pages - 1);
+                in &= (1u << a.page_shift) - 1;
+            } else page = 0;
+            mine.codes_at[lane % TILE] = in * codes_n + (uint32_t)page * codes_page;
+            const uint8_t *from = scales + ((uint64_t)(in * scales_n + (uint32_t)page * scales_page) << 2) + (D == 128 ? lane / 32 * 4 : 0);
+            uint32_t off[G::CI];
+#pragma unroll
+            for (int k = 0; k < G::CI; ++k) off[k] = mine.codes_at[lane / G::LPR * G::CI + k];
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // (what was read of the buffer that is written now has arrived)
+#pragma unroll
+            for (int k = 0; k < G::CI; ++k)
+                request16(codes + ((uint64_t)off[k] << 4) + ((lane % G::LPR) ^ G::swz(lane / G::LPR * G::CI + k)) * 16, codes_lds + at * G::CODES + k * 1024);
+            request4(from, scales_lds + at * 256);
         };
-        auto request = [&](Tile<D> &x, int slot, int page) {
-            const uint32_t in = paged ? (uint32_t)slot & ((1u << a.page_shift) - 1) : (uint32_t)slot;
-            const uint8_t *from = scales + ((uint64_t)(in * scales_n + (uint32_t)page * scales_page) << 2);
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) x.scale[i] = reinterpret_cast<const uint32_t *>(from)[i];
-            lds.codes_at[wave][lane % TILE] = in * codes_n + (uint32_t)page * codes_page;
-            const uint8_t *kc = codes + (D / 8) * g, *vc = codes + D / 2 + (D / 32) * low;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint8_t *src = kc + ((uint64_t)lds.codes_at[wave][16 * i + low] << 4);
-                if constexpr (D == 128) {
-                    const u32x4 w = *reinterpret_cast<const u32x4 *>(src);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) x.k[i][k] = w[k];
-                } else {
-                    const u32x2 w = *reinterpret_cast<const u32x2 *>(src);
-                    x.k[i][0] = w[0];
-                    x.k[i][1] = w[1];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const u32x4 at = *reinterpret_cast<const u32x4 *>(&lds.codes_at[wave][16 * i + 4 * g]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint8_t *src = vc + ((uint64_t)at[j] << 4);
-                    if constexpr (D == 128) x.v[4 * i + j] = *reinterpret_cast<const uint32_t *>(src);
-                    else x.v[4 * i + j] = *reinterpret_cast<const uint16_t *>(src);
-                }
-            }
-        };
-        auto use = [&](const Tile<D> &x, int t) {
-            {
-                const uint32_t of_values = D == 128 ? x.scale[D / 64 - 1] : x.scale[0] >> 16;
-                lds.k_scale[wave][lane % TILE] = x.scale[0];
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) lds.v_scale[wave][i][lane % TILE] = (uint8_t)(of_values >> (8 * i));
-            }
+        auto use = [&](int at, int t) {
+            const uint8_t *codes_in = mine.codes[at];
+            const uint8_t *scales_in = reinterpret_cast<const uint8_t *>(mine.scales[at]);
             f32x4 s[NQ][2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float scale = scale_of(reinterpret_cast<const uint8_t *>(&lds.k_scale[wave][16 * i + low])[D == 128 ? g : g / 2]);
+                const float scale = scale_of(scales_in[4 * (16 * i + low) + (D == 128 ? g : g / 2)]);
+                uint32_t key_codes[G::KW];
+                if constexpr (D == 128) {
+                    const u32x4 w = *reinterpret_cast<const u32x4 *>(codes_in + G::piece(16 * i + low, g));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) key_codes[k] = w[k];
+                } else {
+                    const u32x2 w = *reinterpret_cast<const u32x2 *>(codes_in + G::piece(16 * i + low, g / 2) + g % 2 * 8);
+                    key_codes[0] = w[0];
+                    key_codes[1] = w[1];
+                }
 #pragma unroll
                 for (int qt = 0; qt < NQ; ++qt) s[qt][i] = f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int k = 0; k < G::KW; ++k) {
-                    const uint32_t w = x.k[i][k];
+                    const uint32_t w = key_codes[k];
                     const uint32_t key[4] = {pair_of<0>(w, scale), pair_of<1>(w, scale), pair_of<2>(w, scale), pair_of<3>(w, scale)};
 #pragma unroll
                     for (int q = 0; q < QP * NQ; ++q) {
@@ -347,12 +377,20 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
+            uint32_t v[8];
             float scale[8];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t four = *reinterpret_cast<const uint32_t *>(&lds.v_scale[wave][low / (D == 128 ? 4 : 8)][16 * i + 4 * g]);
+                const u32x4 four = *reinterpret_cast<const u32x4 *>(scales_in + (D == 128 ? 128 : 0) + 4 * (16 * i + 4 * g));
+                const int block = D == 128 ? low / 4 : 2 + low / 8;        // byte of a position's word
 #pragma unroll
-                for (int j = 0; j < 4; ++j) scale[4 * i + j] = scale_of((four >> (8 * j)) & 255);
+                for (int j = 0; j < 4; ++j) {
+                    const int pos = 16 * i + 4 * g + j;
+                    scale[4 * i + j] = __uint_as_float(__builtin_amdgcn_alignbit(four[j], four[j], 8 * block + 9));    // the byte goes to the exponent's place
+                    const uint8_t *src = codes_in + G::piece(pos, D == 128 ? 4 + low / 4 : 2 + low / 8);
+                    if constexpr (D == 128) v[4 * i + j] = *reinterpret_cast<const uint32_t *>(src + low % 4 * 4);
+                    else v[4 * i + j] = *reinterpret_cast<const uint16_t *>(src + low % 8 * 2);
+                }
             }
             auto columns = [&](auto which) {                      // elements 2B and 2B + 1 of the lane's eight (four)
                 constexpr int B = decltype(which)::value;
@@ -360,7 +398,7 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
                 uint32_t even[4], odd[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t first = pair_of<B>(x.v[2 * j], scale[2 * j]), second = pair_of<B>(x.v[2 * j + 1], scale[2 * j + 1]);
+                    const uint32_t first = pair_of<B>(v[2 * j], scale[2 * j]), second = pair_of<B>(v[2 * j + 1], scale[2 * j + 1]);
                     even[j] = __builtin_amdgcn_perm(second, first, 0x05040100);
                     odd[j] = __builtin_amdgcn_perm(second, first, 0x07060302);
                 }
@@ -380,22 +418,36 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
             }
         };
 
-        int t = t0 + wave;
-        if (t < t1) {
-            Tile<D> x, y;
-            int slot = slot_of(t, list_word(t));
-            request(x, slot, page_of(slot));
-            // (tiles past the share's end are found, clamped to the row, and not used)
-            slot = slot_of(t + NW, list_word(t + NW));
-            int page = page_of(slot), word = list_word(t + 2 * NW);
-            for (; t < t1; t += NW) {
-                request(y, slot, page);
-                slot = slot_of(t + 2 * NW, word); page = page_of(slot); word = list_word(t + 3 * NW);
-                __builtin_amdgcn_sched_barrier(0);
-                use(x, t);
-                x = y;
+        if (base_tile < t1) {
+            int slot[2 * (DEPTH - 1)], page[DEPTH - 1] = {};
+            static_assert(DEPTH == 3, "the requests below are two tiles apart");
+            for (int i = 0; i < 4; ++i) slot[i] = slot_of(i, listed ? *list_at(i) : 0);
+            if (looked_up) for (int i = 0; i < 2; ++i) page[i] = pages[slot[i] >> a.page_shift];
+            for (int i = 0; i < 2; ++i) {
+                request_codes(slot[i], page[i], i);
+                request_pages(slot[2 + i], (2 + i) % DEPTH);
+                request_words(4 + i, (4 + i) % DEPTH);
             }
+            int ready = slot[2], next = slot[3], at = 0;          // slots of tiles i + 2 and i + 3; tile i lies in buffer `at`
+            for (int i = 0, t = base_tile; t < t1; ++i, t += NW) {
+                // all but what the last iteration requested
+                constexpr int R = G::CI + 1;
+                if (listed && looked_up) wait_requests<R + 2>();
+                else if (listed || looked_up) wait_requests<R + 1>();
+                else wait_requests<R>();
+                const int prev = at == 0 ? DEPTH - 1 : at - 1, after = at == DEPTH - 1 ? 0 : at + 1;      // buffers of tiles i + 2, i + 1 (i + 4)
+                const int word = listed ? (int)mine.words[after][lane] : 0, in_page = looked_up ? mine.pages[prev][lane] : 0;
+                request_codes(ready, in_page, prev);
+                ready = next;
+                next = slot_of(i + 4, word);
+                request_pages(next, after);
+                request_words(i + 6, at);
+                use(at, t);
+                at = after;
+            }
+            wait_requests<0>();                                   // (the buffers are used for other things next)
         }
+        __syncthreads();
 
         // The eight waves' states, one query tile at a time.
         const bool tail = a.k_new != nullptr, alone = t0 == 0 && t1 == row_tiles && !tail;
@@ -405,24 +457,24 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS, 2) void m
             float l = sum[qt];
             l += shuffle_xor(l, 16);
             l += shuffle_xor(l, 32);
-            if (g == 0) { lds.ml[wave][low][0] = ref[qt]; lds.ml[wave][low][1] = l; }
+            if (g == 0) { lds.merge.ml[wave][low][0] = ref[qt]; lds.merge.ml[wave][low][1] = l; }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int d = 0; d < G::DT; d += 4)
-                    *reinterpret_cast<f32x4 *>(&lds.o[wave][low][G::DT * (4 * g + i) + d]) = f32x4{acc[qt][d][i], acc[qt][d + 1][i], acc[qt][d + 2][i], acc[qt][d + 3][i]};
+                    *reinterpret_cast<f32x4 *>(&lds.merge.o[wave][low][G::DT * (4 * g + i) + d]) = f32x4{acc[qt][d][i], acc[qt][d + 1][i], acc[qt][d + 2][i], acc[qt][d + 3][i]};
             __syncthreads();
             const int q = tid / (D / 4), at = tid % (D / 4) * 4;
             if (q < 16) {
                 float top = -INFINITY, all = 0.0f, m[NW];
 #pragma unroll
-                for (int w = 0; w < NW; ++w) { m[w] = lds.ml[w][q][0]; top = fmaxf(top, m[w]); }
+                for (int w = 0; w < NW; ++w) { m[w] = lds.merge.ml[w][q][0]; top = fmaxf(top, m[w]); }
                 f32x4 o = {0, 0, 0, 0};
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
                     const float f = m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[w] - top);
-                    all += f * lds.ml[w][q][1];
-                    o += f * *reinterpret_cast<const f32x4 *>(&lds.o[w][q][at]);
+                    all += f * lds.merge.ml[w][q][1];
+                    o += f * *reinterpret_cast<const f32x4 *>(&lds.merge.o[w][q][at]);
                 }
                 const int i = qt * 16 + q;
                 if (!alone) {
