@@ -34,7 +34,6 @@ specattn_status launch_mx_load(const MxRowsLaunch &a, hipStream_t stream);
 struct MxAttnLaunch {
     AttnLaunch a;
     MxCache c;
-    FastDivisor per_h, per_t;
 };
 size_t mx_attn_workspace_bytes(int rows, int G, int T, int d);
 specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream);

@@ -16,10 +16,10 @@
 //            the lanes hold them; the queries are laid out to match.
 //   values   lane (c, g) takes d/16 consecutive elements of the eight positions 4g .. 4g+3 and 16+4g .. 16+4g+3: what a
 //            column tile of the second product needs of those positions, for d/16 column tiles
-//   S^T = K Q^T, O^T += V^T P^T on mfma 16x16x32 in bf16.  The codes times their scales are exact in bf16, bf16 queries are
-//   exact, fp16 queries go in two exact parts.  The first product leaves the weights of a query in the lanes that hold the
-//   values' positions, so weights never leave their lane.  A weight goes in three bf16 parts, 24 significant bits: two leave 2^-17 of
-//   it, more than the fp32 sums do.
+//   S^T = K Q^T on mfma 16x16x32 in bf16: codes times scales are exact, and so are bf16 queries; fp16 queries go in two exact parts.
+//   O^T += V^T P^T in fp16: a weight goes in two parts, 22 significant bits (bf16 took three: a third more matrix and twice the vector
+//   instructions), and the scales in units that follow the largest one of a block, since fp16 has not their range.  The first product
+//   leaves the weights of a query in the lanes that hold the values' positions, so weights never leave their lane.
 // (The matrix instructions that take 4-bit operands and scales directly, with the queries in two 8-bit parts, measured 2e-5 of
 // the sum of magnitudes on random operands, far from fp32: their sums are aligned in few bits.)
 #include "mx.h"
@@ -36,14 +36,23 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int NW = 8;                     // waves per workgroup
-constexpr int THREADS = NW * 64;
+// Waves per workgroup, and tiles of a wave in use and on their way.
+template <int NQ> struct Waves {
+    static constexpr int N = NQ <= 0 ? 12 : 8, DEPTH = NQ <= 0 ? 2 : 3, THREADS = N * 64;
+};
 constexpr int TILE = 32;                  // positions per tile
-constexpr int MAX_ROWS = 1024;            // rows per launch: two to a thread
+constexpr int MAX_ROWS = 1024;            // rows per launch
 constexpr int SEG_COST = 6;               // cost of picking a row up, in tiles
-constexpr int PARTS = 3;                  // bf16 parts of a weight
-constexpr float RANGE = 8.0f;             // weights are taken in units of 2^ref; ref moves when one exceeds 2^RANGE
+constexpr int PARTS = 2;                  // fp16 parts of a weight
+// Weights are taken in units of 2^ref.  ref puts the largest weight so far at 2^HEAD and moves when one exceeds 2^RANGE: fp16 ends at 2^16
+// and, downwards, at 2^-24, so that a weight 2^-36 below the largest still counts.
+constexpr float HEAD = 12.0f, RANGE = 15.0f;
+// Values are taken in units of 2^(unit - 127), a byte per block that follows the largest scale of the wave's positions up.  Codes times
+// scales are exact in fp16 down to 2^-FAR of that; values under smaller scales are rounded to multiples of 2^-24 of it.
+constexpr int FAR = 22;
 
 template <int D> struct Geo {
     static constexpr int KW = D / 32;     // words of key codes per lane and position: k-steps of the first product
@@ -59,10 +68,8 @@ template <int D> struct Geo {
     static __device__ __forceinline__ int piece(int pos, int c) { return (pos % CI) * 1024 + (pos / CI) * D + ((c ^ swz(pos)) * 16); }
 };
 
-constexpr int DEPTH = 3;                  // tiles of a wave: in use and on their way
-
 // A wave's part of the LDS.
-template <int D> struct WaveLds {
+template <int D, int DEPTH> struct WaveLds {
     uint8_t codes[DEPTH][Geo<D>::CODES];
     uint32_t scales[DEPTH][64];           // d = 128: of the keys of the 32 positions, then of the values; d = 64: of both
     uint32_t words[DEPTH][64];            // list words
@@ -70,17 +77,18 @@ template <int D> struct WaveLds {
     uint32_t codes_at[TILE];              // row offsets of the tile that is requested next
 };
 
-template <int D> struct MergeLds {
+template <int D, int NW> struct MergeLds {
     float o[NW][16][Geo<D>::PITCH];
     float ml[NW][16][2];
 };
 
 template <int D, int NQ, int QP> struct Lds {
-    static constexpr bool Q = NQ * QP > 2;                                    // queries wait in LDS, else in registers
+    static constexpr int NW = Waves<NQ>::N;
+    static constexpr bool Q = NQ * QP > 1;                                    // queries wait in LDS, else in registers
     static constexpr int Q_BYTES = Q ? NQ * QP * Geo<D>::KW * 1024 : 16;
     union {
-        WaveLds<D> wave[NW];
-        MergeLds<D> merge;
+        WaveLds<D, Waves<NQ>::DEPTH> wave[NW];
+        MergeLds<D, NW> merge;
     };
     uint8_t q[Q_BYTES] __attribute__((aligned(16)));
     int prefix[MAX_ROWS + 1];
@@ -112,107 +120,168 @@ __device__ __forceinline__ f32x4 mfma(const uint32_t (&a)[4], const uint32_t (&b
     const u32x4 x = {a[0], a[1], a[2], a[3]}, y = {b[0], b[1], b[2], b[3]};
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ f32x4 mfma_f16(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c)
+{
+    const u32x4 x = {a[0], a[1], a[2], a[3]}, y = {b[0], b[1], b[2], b[3]};
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+}
+__device__ __forceinline__ float f16_low(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[0]; }
+__device__ __forceinline__ float f16_high(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[1]; }
 // Elements 2B and 2B + 1 of eight codes.  (The conversion takes a scale's exponent alone.)
-template <int B> __device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale) { return bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, B)); }
+__device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int B)
+{
+    return bits(B == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0) : B == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)
+              : B == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+}
+__device__ __forceinline__ uint32_t half_pair_of(uint32_t codes, float scale, int B)
+{
+    const f16x2 x = B == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0) : B == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1)
+                  : B == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3);
+    return __builtin_bit_cast(uint32_t, x);
+}
 __device__ __forceinline__ float shuffle_xor(float x, int mask) { return __shfl_xor(x, mask, 64); }
 
-// Reduction over a workgroup: sums of a and b.
-__device__ __forceinline__ void sum_two(int a, int b, int (&red)[2][NW], int &ta, int &tb)
+// What the kernels need of a call.  Row offsets of codes in units of 16 bytes, of scales in units of 4.
+struct MxArgs {
+    const int32_t *counts, *seq_lens, *indices;
+    const uint8_t *codes, *scales;
+    const int32_t *page_table;
+    const uint16_t *q;
+    float *out, *lse;
+    void *out_lowp;
+    uint16_t *row_parts;                  // [rows][2]: first and last share of a row
+    float *slots;                         // partial (row, share) in slot share + row: [16 NQ][D] o, [16 NQ][2] m and l
+    int64_t idx_stride, codes_b, codes_h, scales_b, scales_h, q_b, q_h, q_t;
+    uint32_t codes_n, codes_page, scales_n, scales_page;
+    FastDivisor per_h, per_t;
+    int max_pages, page_shift, last_page, last_slot;
+    int H_q, H_kv, T, first_head, heads, queries, row0, rows, n_max, capacity, chunk_shift;
+    int dense, paged, tail, dtype;        // paged: 1 by a page table, 2 by the list itself
+    float to_log2;
+    const uint16_t *k_new, *v_new;        // (the merge alone)
+};
+
+// Positions that row r of sequence b attends to.
+__device__ __forceinline__ int positions_of(const MxArgs &a, int r, int b)
 {
-    const int wave = threadIdx.x / 64;
-    a = __builtin_amdgcn_readlane(wave_inclusive_sum(a), 63);
-    b = __builtin_amdgcn_readlane(wave_inclusive_sum(b), 63);
-    if (threadIdx.x % 64 == 0) { red[0][wave] = a; red[1][wave] = b; }
-    __syncthreads();
-    ta = tb = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) { ta += red[0][w]; tb += red[1][w]; }
+    int len = a.n_max;
+    if (a.seq_lens && (a.dense || a.chunk_shift)) len = min(max(a.seq_lens[b], 0), a.n_max);
+    if (a.dense) return len;
+    const int c = min(max(a.counts[r], 0), a.capacity);
+    if (!a.chunk_shift || c == 0) return c;
+    // ascending chunks: only the last can reach past the sequence's length
+    const int over = (int)min((int64_t)1 << a.chunk_shift, max((int64_t)0, (((int64_t)a.indices[r * a.idx_stride + c - 1] + 1) << a.chunk_shift) - len));
+    return (c << a.chunk_shift) - over;
 }
 
-struct Share { int size, head; };         // units of the line per workgroup, and ahead of a row's tiles
+// How the line is cut: shares of `size` units, a row's tiles behind `head` units.  Few tiles: shares of at most 32 tiles, whole rounds
+// of the waves, each of one row (a row's units are rounded up to whole shares), so that no workgroup has to pick up a second one.
+struct Share { int size, head; };
+__device__ __forceinline__ Share share_of(int tiles, int filled, int workgroups, int waves)
+{
+    if (filled < workgroups) {
+        const int least = (tiles + workgroups - filled - 1) / (workgroups - filled);
+        const int size = max((least + waves - 1) / waves, 1) * waves;
+        if (size <= 32) return {size, 0};
+    }
+    return {(tiles + SEG_COST * filled + workgroups - 1) / workgroups, SEG_COST};
+}
+__device__ __forceinline__ int units_of(int tiles, Share s)
+{
+    return tiles == 0 ? 0 : s.head ? tiles + s.head : (tiles + s.size - 1) / s.size * s.size;
+}
+__device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
-template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS) void mx_attn_kernel(MxAttnLaunch p, int row0, int rows, int heads)
+// FEW: up to 64 rows, which every wave holds one to a lane; otherwise up to MAX_ROWS in tables, two to a thread.
+template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ>::THREADS) void mx_attn_kernel(MxArgs a)
 {
     typedef Geo<D> G;
+    constexpr int NW = Waves<NQ>::N, DEPTH = Waves<NQ>::DEPTH, AHEAD = DEPTH - 1, THREADS = Waves<NQ>::THREADS;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_bytes[];
     Lds<D, NQ, QP> &lds = *reinterpret_cast<Lds<D, NQ, QP> *>(lds_bytes);
-    const AttnLaunch &a = p.a;
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, low = lane % 16, g = lane / 16;
+    const int tid = threadIdx.x, lane = tid % 64, low = lane % 16, g = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int me = blockIdx.x;
+    SPECATTN_PRELOAD(a.counts); SPECATTN_PRELOAD(a.indices); SPECATTN_PRELOAD(a.codes); SPECATTN_PRELOAD(a.scales); SPECATTN_PRELOAD(a.page_table); SPECATTN_PRELOAD(a.q);
+    SPECATTN_PRELOAD(a.idx_stride); SPECATTN_PRELOAD(a.codes_h); SPECATTN_PRELOAD(a.scales_h); SPECATTN_PRELOAD(a.q_h); SPECATTN_PRELOAD(a.q_t); SPECATTN_PRELOAD(a.codes_n);
+    SPECATTN_PRELOAD(a.per_h.mul); SPECATTN_PRELOAD(a.per_t.mul); SPECATTN_PRELOAD(a.max_pages); SPECATTN_PRELOAD(a.H_q); SPECATTN_PRELOAD(a.first_head); SPECATTN_PRELOAD(a.dense);
 
     // The line: every workgroup works it out for itself.
-    int cnt[2], tiles = 0, filled = 0;
+    int my_n = 0, my_prefix = 0, total;                           // FEW: of row `lane`
+    Share share;
+    if constexpr (FEW) {
+        const int r = a.row0 + min(lane, a.rows - 1), n = positions_of(a, r, a.per_h.divide(r));
+        my_n = lane < a.rows ? n : 0;
+        const int tiles = (my_n + TILE - 1) / TILE;
+        share = share_of(wave_last(wave_inclusive_sum(tiles)), __popcll(__ballot(my_n > 0)), gridDim.x, NW);
+        const int units = units_of(tiles, share), upto = wave_inclusive_sum(units);
+        my_prefix = upto - units;
+        total = wave_last(upto);
+    } else {
+        int n[2], tiles = 0, filled = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = 2 * tid + i;
-        cnt[i] = r < rows ? attn_row_count(a, row0 + r, p.per_h.divide(row0 + r)) : 0;
-        lds.count[r] = cnt[i];
-        tiles += (cnt[i] + TILE - 1) / TILE;
-        filled += cnt[i] > 0;
-    }
-    int all_tiles, all_rows;
-    sum_two(tiles, filled, lds.red, all_tiles, all_rows);
-    const int W = gridDim.x;
-    // Few tiles: shares of 8, 16, 24 or 32 tiles, each of one row, so that no workgroup has to pick up a second one.
-    Share share = {0, 0};
-    if (all_rows < W) {
-        const int least = (all_tiles + W - all_rows - 1) / (W - all_rows);
-        const int size = max((least + NW - 1) / NW, 1) * NW;
-        if (size <= 4 * NW) share.size = size;
-    }
-    const bool whole = share.size > 0;
-    if (!whole) { share.head = SEG_COST; share.size = (all_tiles + SEG_COST * all_rows + W - 1) / W; }
-    int cost[2];
+        for (int i = 0; i < 2; ++i) {
+            const int r = 2 * tid + i;
+            n[i] = tid < MAX_ROWS / 2 && r < a.rows ? positions_of(a, a.row0 + r, a.per_h.divide(a.row0 + r)) : 0;
+            if (tid < MAX_ROWS / 2) lds.count[r] = n[i];
+            tiles += (n[i] + TILE - 1) / TILE;
+            filled += n[i] > 0;
+        }
+        tiles = wave_last(wave_inclusive_sum(tiles));
+        filled = wave_last(wave_inclusive_sum(filled));
+        if (lane == 0) { lds.red[0][wave] = tiles; lds.red[1][wave] = filled; }
+        __syncthreads();
+        tiles = filled = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int t = (cnt[i] + TILE - 1) / TILE;
-        cost[i] = t == 0 ? 0 : whole ? (t + share.size - 1) / share.size * share.size : t + SEG_COST;
+        for (int w = 0; w < NW; ++w) { tiles += lds.red[0][w]; filled += lds.red[1][w]; }
+        share = share_of(tiles, filled, gridDim.x, NW);
+        const int first = units_of((n[0] + TILE - 1) / TILE, share), second = units_of((n[1] + TILE - 1) / TILE, share);
+        const int upto = wave_inclusive_sum(first + second);
+        __syncthreads();                                          // (red is used again)
+        if (lane == 63) lds.red[0][wave] = upto;
+        __syncthreads();
+        int before = upto - first - second;
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w < wave) before += lds.red[0][w];
+            total += lds.red[0][w];
+        }
+        if (tid < MAX_ROWS / 2) {
+            lds.prefix[2 * tid] = before;
+            lds.prefix[2 * tid + 1] = before + first;
+        }
+        if (tid == THREADS - 1) lds.prefix[MAX_ROWS] = total;
+        // the thread whose rows hold this workgroup's first unit says so
+        const int u = me * share.size;
+        if (u >= before && u < before + first + second) lds.red[1][0] = u < before + first ? 2 * tid : 2 * tid + 1;
+        __syncthreads();
     }
-    __syncthreads();                                              // (red is used again)
-    const int upto = wave_inclusive_sum(cost[0] + cost[1]);
-    if (lane == 63) lds.red[0][wave] = upto;
-    __syncthreads();
-    int before = upto - cost[0] - cost[1];
-    for (int w = 0; w < wave; ++w) before += lds.red[0][w];
-    lds.prefix[2 * tid] = before;
-    lds.prefix[2 * tid + 1] = before + cost[0];
-    if (tid == THREADS - 1) lds.prefix[MAX_ROWS] = before + cost[0] + cost[1];
-    __syncthreads();
+    auto prefix_of = [&](int r) { return FEW ? __builtin_amdgcn_readlane(my_prefix, r) : __builtin_amdgcn_readfirstlane(lds.prefix[r]); };
+    auto end_of = [&](int r) { return FEW ? r < 63 ? __builtin_amdgcn_readlane(my_prefix, r + 1) : total : __builtin_amdgcn_readfirstlane(lds.prefix[r + 1]); };
+    auto count_of = [&](int r) { return FEW ? __builtin_amdgcn_readlane(my_n, r) : __builtin_amdgcn_readfirstlane(lds.count[r]); };
 
-    const int total = lds.prefix[MAX_ROWS];
     int u = me * share.size;
     const int u_end = min(u + share.size, total);
     if (u >= u_end) return;
-    int r = 0;                                                    // the row that holds unit u
-    {
-        int lo = 0, hi = MAX_ROWS;                                // prefix[lo] <= u < prefix[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (lds.prefix[mid] <= u) lo = mid; else hi = mid;
-        }
-        r = lo;
-    }
-    uint16_t *row_parts = static_cast<uint16_t *>(a.workspace);                // [rows][2]: first and last share of a row
-    float *slots = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + (((size_t)rows * 4 + 255) & ~(size_t)255));
-    const int queries = heads * a.T;
-    const float to_log2 = a.sm_scale * 1.44269504088896340736f;
+    // the last row that starts at or ahead of unit u (empty rows ahead of it start there too)
+    int r = FEW ? 63 - __builtin_clzll(__ballot(my_prefix <= u && my_n > 0)) : __builtin_amdgcn_readfirstlane(lds.red[1][0]);
 
-    for (; u < u_end; u = lds.prefix[r + 1], ++r) {
-        const int row_start = lds.prefix[r], n = lds.count[r], row_tiles = (n + TILE - 1) / TILE;
+    for (; u < u_end; u = end_of(r), ++r) {
+        const int row_start = prefix_of(r), n = count_of(r), row_tiles = (n + TILE - 1) / TILE;
         const int t0 = max(0, u - row_start - share.head), t1 = min(row_tiles, u_end - row_start - share.head);
         if (t1 <= t0) continue;                                   // (an empty row, or the share ends ahead of the row's first tile)
-        const int row = row0 + r, b = p.per_h.divide(row), h = row - b * a.H_kv;
+        const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
+        const int head0 = h * (a.H_q / a.H_kv) + a.first_head;
 
         // queries: element j of k-step s in lane (q, g) is element (d/4) g + 8 s + j of query 16 qt + q
         uint32_t qf[Lds<D, NQ, QP>::Q ? 1 : NQ * QP][G::KW][4];
         {
-            auto fetch = [&](int qt, int s, uint32_t (&part)[QP][4]) {
-                const int i = qt * 16 + low, gh = p.per_t.divide(i), t = i - gh * a.T;
-                u32x4 w = {0, 0, 0, 0};
-                if (i < queries)
-                    w = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) + b * a.q_stride_b + (int64_t)(h * (a.H_q / a.H_kv) + a.g_first + gh) * a.q_stride_h
-                                                        + t * a.q_stride_t + (D / 4) * g + 8 * s);
+            auto query = [&](int qt) {
+                const int i = min(qt * 16 + low, a.queries - 1), gh = a.per_t.divide(i), t = i - gh * a.T;      // (behind the last query: that one again)
+                return a.q + b * a.q_b + (head0 + gh) * a.q_h + t * a.q_t + (D / 4) * g;
+            };
+            auto split = [&](u32x4 w, uint32_t (&part)[QP][4]) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     if constexpr (QP == 1) part[0][k] = w[k];
@@ -226,23 +295,25 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS) void mx_a
             if constexpr (Lds<D, NQ, QP>::Q) {
                 for (int k = wave; k < NQ * G::KW; k += NW) {
                     uint32_t part[QP][4];
-                    fetch(k / G::KW, k % G::KW, part);
+                    split(*reinterpret_cast<const u32x4 *>(query(k / G::KW) + 8 * (k % G::KW)), part);
 #pragma unroll
                     for (int q = 0; q < QP; ++q) *reinterpret_cast<u32x4 *>(lds.q + ((q * NQ * G::KW + k) * 64 + lane) * 16) = u32x4{part[q][0], part[q][1], part[q][2], part[q][3]};
                 }
                 __syncthreads();
             } else {
 #pragma unroll
-                for (int qt = 0; qt < NQ; ++qt)
+                for (int qt = 0; qt < NQ; ++qt) {
+                    const uint16_t *from = query(qt);
 #pragma unroll
                     for (int s = 0; s < G::KW; ++s) {
                         uint32_t part[QP][4];
-                        fetch(qt, s, part);
+                        split(*reinterpret_cast<const u32x4 *>(from + 8 * s), part);
 #pragma unroll
                         for (int q = 0; q < QP; ++q)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) qf[q * NQ + qt][s][k] = part[q][k];
                     }
+                }
             }
         }
 
@@ -256,202 +327,228 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS) void mx_a
             for (int t = 0; t < G::DT; ++t) acc[qt][t] = f32x4{0, 0, 0, 0};
         }
 
-        const int32_t *list = a.dense ? nullptr : a.indices + (int64_t)row * a.idx_stride;
-        const int32_t *pages = p.c.page_table ? p.c.page_table + (int64_t)b * p.c.max_pages : nullptr;
-        const bool paged = pages || a.indices_are_physical;
-        const uint8_t *codes = p.c.codes + (paged ? 0 : b * p.c.codes_b) + h * p.c.codes_h;
-        const uint8_t *scales = p.c.scales + (paged ? 0 : b * p.c.scales_b) + h * p.c.scales_h;
-        const uint32_t codes_n = (uint32_t)(p.c.codes_n >> 4), scales_n = (uint32_t)(p.c.scales_n >> 2);
-        const uint32_t codes_page = (uint32_t)(p.c.codes_page >> 4), scales_page = (uint32_t)(p.c.scales_page >> 2);
-        const int last_slot = a.indices_are_physical ? INT32_MAX : a.n_max - 1;
-
-        // A tile goes through three steps, each two tiles ahead of the next: its list words are requested; its pages; its codes and
+        // A tile goes through three steps, each AHEAD of the wave's tiles ahead of the next: its list words are requested; its pages; its codes and
         // scales.  Tiles are counted per wave: the wave's tile i is tile t0 + wave + i * NW of the row.  (Tiles past the share's end are
         // requested like others, clamped to the row, and not used.)
-        WaveLds<D> &mine = lds.wave[wave];
+        WaveLds<D, DEPTH> &mine = lds.wave[wave];
         const uint32_t codes_lds = lds_offset(mine.codes), scales_lds = lds_offset(mine.scales), words_lds = lds_offset(mine.words), pages_lds = lds_offset(mine.pages);
-        const bool listed = !a.dense, looked_up = pages != nullptr;
-        const int base_tile = t0 + wave;
-        auto list_rank = [&](int i) { return min((base_tile + i * NW) * TILE + lane % TILE, n - 1); };
+        const int32_t *list = a.indices + row * a.idx_stride, *pages = a.page_table + (int64_t)b * a.max_pages;
+        const uint8_t *codes = a.codes + (a.paged ? 0 : b * a.codes_b) + h * a.codes_h;
+        const uint8_t *scales = a.scales + (a.paged ? 0 : b * a.scales_b) + h * a.scales_h + (D == 128 ? lane / 32 * 4 : 0);
+        const bool listed = !a.dense, looked_up = a.paged == 1;
+        const int base_tile = t0 + wave, in_tile = lane % TILE;
+        const int lane_piece = (lane % G::LPR) ^ G::swz(lane / G::LPR * G::CI);      // (of instruction 0; of instruction k: ^ k)
+        auto list_rank = [&](int i) { return min((base_tile + i * NW) * TILE + in_tile, n - 1); };
         auto list_at = [&](int i) { return list + (list_rank(i) >> a.chunk_shift); };
         auto slot_of = [&](int i, int word) -> int {
             if (!listed) return list_rank(i);                     // (below the length: inside the cache)
             if (a.chunk_shift) word = (word << a.chunk_shift) | (list_rank(i) & ((1 << a.chunk_shift) - 1));
-            return min(max(word, 0), last_slot);
+            return min(max(word, 0), a.last_slot);
         };
         auto request_words = [&](int i, int at) { if (listed) request4(list_at(i), words_lds + at * 256); };
         auto request_pages = [&](int slot, int at) { if (looked_up) request4(pages + (slot >> a.page_shift), pages_lds + at * 256); };
         auto request_codes = [&](int slot, int page, int at) {
-            uint32_t in = (uint32_t)slot;
-            if (paged) {
+            uint32_t code_at, scale_at;
+            if (a.paged) {
                 if (!looked_up) page = slot >> a.page_shift;
-                page = min(max(page, 0), p.c.num_pages - 1);
-                in &= (1u << a.page_shift) - 1;
-            } else page = 0;
-            mine.codes_at[lane % TILE] = in * codes_n + (uint32_t)page * codes_page;
-            const uint8_t *from = scales + ((uint64_t)(in * scales_n + (uint32_t)page * scales_page) << 2) + (D == 128 ? lane / 32 * 4 : 0);
+                page = min(max(page, 0), a.last_page);
+                const uint32_t in = (uint32_t)slot & ((1u << a.page_shift) - 1);
+                code_at = in * a.codes_n + (uint32_t)page * a.codes_page;
+                scale_at = in * a.scales_n + (uint32_t)page * a.scales_page;
+            } else {
+                code_at = (uint32_t)slot * a.codes_n;
+                scale_at = (uint32_t)slot * a.scales_n;
+            }
+            mine.codes_at[in_tile] = code_at;
             uint32_t off[G::CI];
 #pragma unroll
             for (int k = 0; k < G::CI; ++k) off[k] = mine.codes_at[lane / G::LPR * G::CI + k];
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // (what was read of the buffer that is written now has arrived)
+            request4(scales + ((uint64_t)scale_at << 2), scales_lds + at * 256);
 #pragma unroll
             for (int k = 0; k < G::CI; ++k)
-                request16(codes + ((uint64_t)off[k] << 4) + ((lane % G::LPR) ^ G::swz(lane / G::LPR * G::CI + k)) * 16, codes_lds + at * G::CODES + k * 1024);
-            request4(from, scales_lds + at * 256);
+                request16(codes + ((uint64_t)(off[k] + (lane_piece ^ k)) << 4), codes_lds + at * G::CODES + k * 1024);
         };
-        auto use = [&](int at, int t) {
-            const uint8_t *codes_in = mine.codes[at];
-            const uint8_t *scales_in = reinterpret_cast<const uint8_t *>(mine.scales[at]);
-            f32x4 s[NQ][2];
+
+        uint32_t w[NQ][PARTS][4], v[8];
+        int v_scale[8], unit = 0;                                 // scale bytes of the lane's block; unit: of the same block
+        auto add_values = [&]() {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float scale = scale_of(scales_in[4 * (16 * i + low) + (D == 128 ? g : g / 2)]);
-                uint32_t key_codes[G::KW];
-                if constexpr (D == 128) {
-                    const u32x4 w = *reinterpret_cast<const u32x4 *>(codes_in + G::piece(16 * i + low, g));
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) key_codes[k] = w[k];
-                } else {
-                    const u32x2 w = *reinterpret_cast<const u32x2 *>(codes_in + G::piece(16 * i + low, g / 2) + g % 2 * 8);
-                    key_codes[0] = w[0];
-                    key_codes[1] = w[1];
-                }
-#pragma unroll
-                for (int qt = 0; qt < NQ; ++qt) s[qt][i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < G::KW; ++k) {
-                    const uint32_t w = key_codes[k];
-                    const uint32_t key[4] = {pair_of<0>(w, scale), pair_of<1>(w, scale), pair_of<2>(w, scale), pair_of<3>(w, scale)};
-#pragma unroll
-                    for (int q = 0; q < QP * NQ; ++q) {
-                        if constexpr (Lds<D, NQ, QP>::Q) {
-                            const u32x4 v = *reinterpret_cast<const u32x4 *>(lds.q + ((q * G::KW + k) * 64 + lane) * 16);
-                            const uint32_t f[4] = {v[0], v[1], v[2], v[3]};
-                            s[q % NQ][i] = mfma(key, f, s[q % NQ][i]);
-                        } else s[q % NQ][i] = mfma(key, qf[q][k], s[q % NQ][i]);
-                    }
-                }
-            }
-            const int left = n - t * TILE;
-            if (left < TILE) {                                    // a row's last tile: what lies behind it repeats its last position
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int qt = 0; qt < NQ; ++qt) s[qt][i][k] = 16 * i + 4 * g + k < left ? s[qt][i][k] : -INFINITY;
-            }
-            uint32_t w[NQ][PARTS][4];
-#pragma unroll
-            for (int qt = 0; qt < NQ; ++qt) {
-                __builtin_amdgcn_sched_barrier(0);
-                float most = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) { s[qt][i][k] *= to_log2; most = fmaxf(most, s[qt][i][k]); }
-                if (__any(most > ref[qt] + RANGE)) {
-                    most = fmaxf(most, shuffle_xor(most, 16));
-                    most = fmaxf(most, shuffle_xor(most, 32));
-                    const float now = fmaxf(ref[qt], most), shrink = __builtin_amdgcn_exp2f(ref[qt] - now);
-                    const float factor = ref[qt] == -INFINITY ? 0.0f : shrink;
-                    ref[qt] = now;
-                    sum[qt] *= factor;
-#pragma unroll
-                    for (int d = 0; d < G::DT; ++d) acc[qt][d] *= factor;
-                }
-                float e[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    e[k] = __builtin_amdgcn_exp2f(s[qt][k / 4][k % 4] - ref[qt]);
-                    sum[qt] += e[k];
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float x0 = e[2 * k], x1 = e[2 * k + 1];
-#pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
-                        w[qt][part][k] = to_bf16(x0, x1);
-                        if (part + 1 < PARTS) { x0 -= low_half(w[qt][part][k]); x1 -= high_half(w[qt][part][k]); }
-                    }
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            uint32_t v[8];
-            float scale[8];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const u32x4 four = *reinterpret_cast<const u32x4 *>(scales_in + (D == 128 ? 128 : 0) + 4 * (16 * i + 4 * g));
-                const int block = D == 128 ? low / 4 : 2 + low / 8;        // byte of a position's word
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int pos = 16 * i + 4 * g + j;
-                    scale[4 * i + j] = __uint_as_float(__builtin_amdgcn_alignbit(four[j], four[j], 8 * block + 9));    // the byte goes to the exponent's place
-                    const uint8_t *src = codes_in + G::piece(pos, D == 128 ? 4 + low / 4 : 2 + low / 8);
-                    if constexpr (D == 128) v[4 * i + j] = *reinterpret_cast<const uint32_t *>(src + low % 4 * 4);
-                    else v[4 * i + j] = *reinterpret_cast<const uint16_t *>(src + low % 8 * 2);
-                }
-            }
-            auto columns = [&](auto which) {                      // elements 2B and 2B + 1 of the lane's eight (four)
-                constexpr int B = decltype(which)::value;
-                __builtin_amdgcn_sched_barrier(0);
+            for (int B = 0; B < G::DT / 2; ++B) {                 // elements 2B and 2B + 1 of the lane's
                 uint32_t even[4], odd[4];
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t first = pair_of<B>(v[2 * j], scale[2 * j]), second = pair_of<B>(v[2 * j + 1], scale[2 * j + 1]);
+                    const uint32_t first = half_pair_of(v[2 * j], __int_as_float(v_scale[2 * j]), B), second = half_pair_of(v[2 * j + 1], __int_as_float(v_scale[2 * j + 1]), B);
                     even[j] = __builtin_amdgcn_perm(second, first, 0x05040100);
                     odd[j] = __builtin_amdgcn_perm(second, first, 0x07060302);
                 }
 #pragma unroll
-                for (int qt = 0; qt < NQ; ++qt)
+                for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
-                        acc[qt][2 * B] = mfma(even, w[qt][part], acc[qt][2 * B]);
-                        acc[qt][2 * B + 1] = mfma(odd, w[qt][part], acc[qt][2 * B + 1]);
+                    for (int qt = 0; qt < NQ; ++qt) {
+                        acc[qt][2 * B] = mfma_f16(even, w[qt][part], acc[qt][2 * B]);
+                        acc[qt][2 * B + 1] = mfma_f16(odd, w[qt][part], acc[qt][2 * B + 1]);
                     }
-            };
-            columns(std::integral_constant<int, 0>{});
-            columns(std::integral_constant<int, 1>{});
-            if constexpr (D == 128) {
-                columns(std::integral_constant<int, 2>{});
-                columns(std::integral_constant<int, 3>{});
             }
         };
-
         if (base_tile < t1) {
-            int slot[2 * (DEPTH - 1)], page[DEPTH - 1] = {};
-            static_assert(DEPTH == 3, "the requests below are two tiles apart");
-            for (int i = 0; i < 4; ++i) slot[i] = slot_of(i, listed ? *list_at(i) : 0);
-            if (looked_up) for (int i = 0; i < 2; ++i) page[i] = pages[slot[i] >> a.page_shift];
-            for (int i = 0; i < 2; ++i) {
+            int slot[2 * AHEAD], page[AHEAD] = {};
+#pragma unroll
+            for (int i = 0; i < 2 * AHEAD; ++i) slot[i] = listed ? *list_at(i) : 0;
+#pragma unroll
+            for (int i = 0; i < 2 * AHEAD; ++i) slot[i] = slot_of(i, slot[i]);
+            if (looked_up)
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) page[i] = pages[slot[i] >> a.page_shift];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
                 request_codes(slot[i], page[i], i);
-                request_pages(slot[2 + i], (2 + i) % DEPTH);
-                request_words(4 + i, (4 + i) % DEPTH);
+                request_pages(slot[AHEAD + i], (AHEAD + i) % DEPTH);
+                request_words(2 * AHEAD + i, (2 * AHEAD + i) % DEPTH);
+                slot[i] = slot[AHEAD + i];
             }
-            int ready = slot[2], next = slot[3], at = 0;          // slots of tiles i + 2 and i + 3; tile i lies in buffer `at`
+            int at = 0;                                           // tile i lies in buffer `at`; slot[]: of tiles i + AHEAD ...
             for (int i = 0, t = base_tile; t < t1; ++i, t += NW) {
-                // all but what the last iteration requested
+                // all but what the last AHEAD - 1 iterations requested
                 constexpr int R = G::CI + 1;
-                if (listed && looked_up) wait_requests<R + 2>();
-                else if (listed || looked_up) wait_requests<R + 1>();
-                else wait_requests<R>();
-                const int prev = at == 0 ? DEPTH - 1 : at - 1, after = at == DEPTH - 1 ? 0 : at + 1;      // buffers of tiles i + 2, i + 1 (i + 4)
-                const int word = listed ? (int)mine.words[after][lane] : 0, in_page = looked_up ? mine.pages[prev][lane] : 0;
-                request_codes(ready, in_page, prev);
-                ready = next;
-                next = slot_of(i + 4, word);
-                request_pages(next, after);
-                request_words(i + 6, at);
-                use(at, t);
+                if (listed && looked_up) wait_requests<(AHEAD - 1) * (R + 2)>();
+                else if (listed || looked_up) wait_requests<(AHEAD - 1) * (R + 1)>();
+                else wait_requests<(AHEAD - 1) * R>();
+                const int prev = at == 0 ? DEPTH - 1 : at - 1, after = at == DEPTH - 1 ? 0 : at + 1;
+                const int word_at = DEPTH == 2 ? at : after;      // of tile i + 2 AHEAD, like its pages
+                const uint8_t *codes_in = mine.codes[at], *scales_in = reinterpret_cast<const uint8_t *>(mine.scales[at]);
+                const int word = listed ? (int)mine.words[word_at][lane] : 0, in_page = looked_up ? mine.pages[prev][lane] : 0;
+                uint32_t key[2][G::KW], key_scale[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    key_scale[k] = scales_in[4 * (16 * k + low) + (D == 128 ? g : g / 2)];
+                    if constexpr (D == 128) {
+                        const u32x4 x = *reinterpret_cast<const u32x4 *>(codes_in + G::piece(16 * k + low, g));
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) key[k][s] = x[s];
+                    } else {
+                        const u32x2 x = *reinterpret_cast<const u32x2 *>(codes_in + G::piece(16 * k + low, g / 2) + g % 2 * 8);
+                        key[k][0] = x[0];
+                        key[k][1] = x[1];
+                    }
+                }
+                request_codes(slot[0], in_page, prev);
+#pragma unroll
+                for (int k = 0; k + 1 < AHEAD; ++k) slot[k] = slot[k + 1];
+                slot[AHEAD - 1] = slot_of(i + 2 * AHEAD, word);
+                request_pages(slot[AHEAD - 1], word_at);
+                request_words(i + 3 * AHEAD, DEPTH == 2 ? after : at);
+
+                f32x4 s[NQ][2];
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) s[qt][0] = s[qt][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float scale = __uint_as_float(key_scale[k] << 23);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int step = 0; step < G::KW; ++step) {
+                        uint32_t f[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f[j] = pair_of(key[k][step], scale, j);
+#pragma unroll
+                        for (int q = 0; q < QP * NQ; ++q) {
+                            if constexpr (Lds<D, NQ, QP>::Q) {
+                                const u32x4 x = *reinterpret_cast<const u32x4 *>(lds.q + ((q * G::KW + step) * 64 + lane) * 16);
+                                const uint32_t y[4] = {x[0], x[1], x[2], x[3]};
+                                s[q % NQ][k] = mfma(f, y, s[q % NQ][k]);
+                            } else s[q % NQ][k] = mfma(f, qf[q][step], s[q % NQ][k]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const u32x4 four = *reinterpret_cast<const u32x4 *>(scales_in + (D == 128 ? 128 : 0) + 4 * (16 * k + 4 * g));
+                    const int block = D == 128 ? low / 4 : 2 + low / 8;        // byte of a position's word
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        v_scale[4 * k + j] = (int)__builtin_amdgcn_ubfe(four[j], 8 * block, 8);
+                        const uint8_t *src = codes_in + G::piece(16 * k + 4 * g + j, D == 128 ? 4 + low / 4 : 2 + low / 8);
+                        if constexpr (D == 128) v[4 * k + j] = *reinterpret_cast<const uint32_t *>(src + low % 4 * 4);
+                        else v[4 * k + j] = *reinterpret_cast<const uint16_t *>(src + low % 8 * 2);
+                    }
+                }
+                const int left = n - t * TILE;
+                if (__builtin_expect(left < TILE, 0)) {                                // a row's last tile: what lies behind it repeats its last position
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll
+                        for (int qt = 0; qt < NQ; ++qt) s[qt][k / 4][k % 4] = 16 * (k / 4) + 4 * g + k % 4 < left ? s[qt][k / 4][k % 4] : -INFINITY;
+                }
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    float most = fmaxf(s[qt][0][0], s[qt][1][0]);
+#pragma unroll
+                    for (int k = 1; k < 4; ++k) most = fmaxf(most, fmaxf(s[qt][0][k], s[qt][1][k]));
+                    most *= a.to_log2;
+                    if (__builtin_expect(__any(most > ref[qt] + RANGE), 0)) {
+                        most = fmaxf(most, shuffle_xor(most, 16));
+                        most = fmaxf(most, shuffle_xor(most, 32));
+                        const float now = fmaxf(ref[qt], most - HEAD), factor = ref[qt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[qt] - now);
+                        ref[qt] = now;
+                        sum[qt] *= factor;
+#pragma unroll
+                        for (int d = 0; d < G::DT; ++d) acc[qt][d] *= factor;
+                    }
+                    float e[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][k / 4][k % 4], a.to_log2, -ref[qt]));
+                    sum[qt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        w[qt][0][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[2 * k], e[2 * k + 1]));
+                        w[qt][1][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[2 * k] - f16_low(w[qt][0][k]), e[2 * k + 1] - f16_high(w[qt][0][k])));
+                    }
+                }
+                // scales in units of 2^(unit - 127)
+                int most_v = v_scale[0], least_v = v_scale[0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) { most_v = max(most_v, v_scale[j]); least_v = min(least_v, v_scale[j]); }
+                if (__builtin_expect(__any(most_v > unit || least_v < unit - FAR), 0)) {
+                    int top = 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) top = max(top, v_scale[j] == 255 ? 0 : v_scale[j]);
+                    top = max(top, __shfl_xor(top, 16, 64));      // (the lanes of a block hold the same positions but for g)
+                    top = max(top, __shfl_xor(top, 32, 64));
+                    if (__any(top > unit)) {
+                        const int now = max(unit, top), down = __shfl(unit - now, D == 128 ? 4 * g : 8 * (g / 2), 64);     // (lane group g sums up columns of that lane's block)
+                        unit = now;
+#pragma unroll
+                        for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+                            for (int d = 0; d < G::DT; ++d)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) acc[qt][d][k] = __builtin_ldexpf(acc[qt][d][k], down);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v_scale[j] = v_scale[j] == 255 ? unit + 128 : max(v_scale[j], unit - 100);    // (NaN; zero)
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v_scale[j] = (v_scale[j] - unit + 127) << 23;
+                add_values();
                 at = after;
             }
             wait_requests<0>();                                   // (the buffers are used for other things next)
+            const int up = __shfl(unit, D == 128 ? 4 * g : 8 * (g / 2), 64) - 127;
+#pragma unroll
+            for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+                for (int d = 0; d < G::DT; ++d)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[qt][d][k] = __builtin_ldexpf(acc[qt][d][k], up);
         }
         __syncthreads();
 
         // The eight waves' states, one query tile at a time.
-        const bool tail = a.k_new != nullptr, alone = t0 == 0 && t1 == row_tiles && !tail;
-        float *slot_o = slots + (size_t)(me + r) * NQ * 16 * (D + 2), *slot_ml = slot_o + NQ * 16 * D;
+        const bool alone = t0 == 0 && t1 == row_tiles && !a.tail;
+        float *slot_o = a.slots + (size_t)(me + r) * NQ * 16 * (D + 2), *slot_ml = slot_o + NQ * 16 * D;
 #pragma unroll
         for (int qt = 0; qt < NQ; ++qt) {
             float l = sum[qt];
@@ -464,36 +561,36 @@ template <int D, int NQ, int QP> __global__ __launch_bounds__(THREADS) void mx_a
                 for (int d = 0; d < G::DT; d += 4)
                     *reinterpret_cast<f32x4 *>(&lds.merge.o[wave][low][G::DT * (4 * g + i) + d]) = f32x4{acc[qt][d][i], acc[qt][d + 1][i], acc[qt][d + 2][i], acc[qt][d + 3][i]};
             __syncthreads();
-            const int q = tid / (D / 4), at = tid % (D / 4) * 4;
+            const int q = tid / (D / 4), col = tid % (D / 4) * 4;
             if (q < 16) {
                 float top = -INFINITY, all = 0.0f, m[NW];
 #pragma unroll
-                for (int w = 0; w < NW; ++w) { m[w] = lds.merge.ml[w][q][0]; top = fmaxf(top, m[w]); }
+                for (int x = 0; x < NW; ++x) { m[x] = lds.merge.ml[x][q][0]; top = fmaxf(top, m[x]); }
                 f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    const float f = m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[w] - top);
-                    all += f * lds.merge.ml[w][q][1];
-                    o += f * *reinterpret_cast<const f32x4 *>(&lds.merge.o[w][q][at]);
+                for (int x = 0; x < NW; ++x) {
+                    const float f = m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[x] - top);
+                    all += f * lds.merge.ml[x][q][1];
+                    o += f * *reinterpret_cast<const f32x4 *>(&lds.merge.o[x][q][col]);
                 }
                 const int i = qt * 16 + q;
                 if (!alone) {
-                    *reinterpret_cast<f32x4 *>(slot_o + i * D + at) = o;
-                    if (at == 0) { slot_ml[2 * i] = top; slot_ml[2 * i + 1] = all; }
-                } else if (i < queries) {
-                    const int gh = p.per_t.divide(i), tq = i - gh * a.T;
-                    const int64_t orow = ((int64_t)b * a.H_q + h * (a.H_q / a.H_kv) + a.g_first + gh) * a.T + tq;
+                    *reinterpret_cast<f32x4 *>(slot_o + i * D + col) = o;
+                    if (col == 0) { slot_ml[2 * i] = top; slot_ml[2 * i + 1] = all; }
+                } else if (i < a.queries) {
+                    const int gh = a.per_t.divide(i), tq = i - gh * a.T;
+                    const int64_t orow = ((int64_t)b * a.H_q + head0 + gh) * a.T + tq;
                     o = o / all;
-                    if (a.out) *reinterpret_cast<f32x4 *>(a.out + orow * D + at) = o;
+                    if (a.out) *reinterpret_cast<f32x4 *>(a.out + orow * D + col) = o;
                     if (a.out_lowp)
-                        for (int k = 0; k < 4; ++k) st_lowp(a.out_lowp, orow * D + at + k, o[k], a.dtype);
-                    if (a.lse && at == 0) a.lse[orow] = (top + __builtin_amdgcn_logf(all)) * 0.69314718055994530942f;
+                        for (int k = 0; k < 4; ++k) st_lowp(a.out_lowp, orow * D + col + k, o[k], a.dtype);
+                    if (a.lse && col == 0) a.lse[orow] = (top + __builtin_amdgcn_logf(all)) * 0.69314718055994530942f;
                 }
             }
             __syncthreads();
         }
-        if (tid == 0 && t0 == 0) row_parts[2 * r] = (uint16_t)me;
-        if (tid == 0 && t1 == row_tiles) row_parts[2 * r + 1] = (uint16_t)me;
+        if (tid == 0 && t0 == 0) a.row_parts[2 * r] = (uint16_t)me;
+        if (tid == 0 && t1 == row_tiles) a.row_parts[2 * r + 1] = (uint16_t)me;
     }
 }
 
@@ -506,26 +603,23 @@ __device__ __forceinline__ float wave_sum(float x)
 }
 
 // One wave per (row, query): the row's partials in share order, then the new tokens behind the cache up to the query's own.
-template <int D> __global__ __launch_bounds__(256) void mx_merge_kernel(MxAttnLaunch p, int row0, int rows, int heads, int padded)
+template <int D> __global__ __launch_bounds__(256) void mx_merge_kernel(MxArgs a, int padded)
 {
     constexpr int E = D / 64;                                     // elements per lane
-    const AttnLaunch &a = p.a;
-    const int lane = threadIdx.x % 64, queries = heads * a.T;
+    const int lane = threadIdx.x % 64;
     const int r = blockIdx.y, i = blockIdx.x * 4 + threadIdx.x / 64;
-    if (i >= queries) return;
-    const int row = row0 + r, b = p.per_h.divide(row), h = row - b * a.H_kv;
-    const uint16_t *row_parts = static_cast<const uint16_t *>(a.workspace);
-    const float *slots = reinterpret_cast<const float *>(static_cast<const char *>(a.workspace) + (((size_t)rows * 4 + 255) & ~(size_t)255));
-    const int gh = p.per_t.divide(i), t = i - gh * a.T, head = h * (a.H_q / a.H_kv) + a.g_first + gh;
+    if (i >= a.queries) return;
+    const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
+    const int gh = a.per_t.divide(i), t = i - gh * a.T, head = h * (a.H_q / a.H_kv) + a.first_head + gh;
     const int64_t orow = ((int64_t)b * a.H_q + head) * a.T + t;
     float m = -INFINITY, l = 0.0f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.0f;
-    if (attn_row_count(a, row, b) > 0) {
-        const int first = row_parts[2 * r], last = row_parts[2 * r + 1];
-        if (first == last && !a.k_new) return;                    // finished by its only workgroup
+    if (positions_of(a, row, b) > 0) {
+        const int first = a.row_parts[2 * r], last = a.row_parts[2 * r + 1];
+        if (first == last && !a.tail) return;                     // finished by its only workgroup
         for (int w = first; w <= last; ++w) {
-            const float *slot = slots + (size_t)(w + r) * padded * (D + 2);
+            const float *slot = a.slots + (size_t)(w + r) * padded * (D + 2);
             const float mw = slot[padded * D + 2 * i], lw = slot[padded * D + 2 * i + 1];
             const float now = fmaxf(m, mw);
             const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now), fw = __builtin_amdgcn_exp2f(mw - now);
@@ -535,20 +629,17 @@ template <int D> __global__ __launch_bounds__(256) void mx_merge_kernel(MxAttnLa
             m = now;
         }
     }
-    if (a.k_new) {
-        auto value = [&](const void *x, int64_t at) {
-            const uint16_t w = static_cast<const uint16_t *>(x)[at];
-            return a.dtype == SPECATTN_F16 ? (float)__builtin_bit_cast(_Float16, w) : __uint_as_float((uint32_t)w << 16);
-        };
+    if (a.tail) {
+        auto value = [&](const uint16_t *x, int64_t at) { return a.dtype == SPECATTN_F16 ? (float)__builtin_bit_cast(_Float16, x[at]) : __uint_as_float((uint32_t)x[at] << 16); };
         float q[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) q[e] = value(a.q, b * a.q_stride_b + (int64_t)head * a.q_stride_h + t * a.q_stride_t + E * lane + e);
+        for (int e = 0; e < E; ++e) q[e] = value(a.q, b * a.q_b + head * a.q_h + t * a.q_t + E * lane + e);
         for (int j = 0; j <= t; ++j) {
             const int64_t at = ((int64_t)row * a.T + j) * D + E * lane;
             float dot = 0.0f;
 #pragma unroll
             for (int e = 0; e < E; ++e) dot += q[e] * value(a.k_new, at + e);
-            const float s = wave_sum(dot) * (a.sm_scale * 1.44269504088896340736f), now = fmaxf(m, s);
+            const float s = wave_sum(dot) * a.to_log2, now = fmaxf(m, s);
             const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now), fw = __builtin_amdgcn_exp2f(s - now);
             l = l * f + fw;
 #pragma unroll
@@ -566,15 +657,16 @@ template <int D> __global__ __launch_bounds__(256) void mx_merge_kernel(MxAttnLa
     if (a.lse && lane == 0) a.lse[orow] = any ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
 }
 
-template <int D, int NQ> const void *variant(bool f16)
+template <int D, int NQ> const void *variant(bool f16, bool few)
 {
-    return f16 ? reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 2>) : reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 1>);
+    return f16 ? few ? reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 2, true>) : reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 2, false>)
+               : few ? reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 1, true>) : reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 1, false>);
 }
-template <int D> const void *variant(int nq, bool f16)
+template <int D> const void *variant(int nq, bool f16, bool few)
 {
-    return nq == 1 ? variant<D, 1>(f16) : nq == 2 ? variant<D, 2>(f16) : nq == 3 ? variant<D, 3>(f16) : variant<D, 4>(f16);
+    return nq == 1 ? variant<D, 1>(f16, few) : nq == 2 ? variant<D, 2>(f16, few) : nq == 3 ? variant<D, 3>(f16, few) : variant<D, 4>(f16, few);
 }
-const void *variant(int d, int nq, bool f16) { return d == 128 ? variant<128>(nq, f16) : variant<64>(nq, f16); }
+const void *variant(int d, int nq, bool f16, bool few) { return d == 128 ? variant<128>(nq, f16, few) : variant<64>(nq, f16, few); }
 template <int D, int NQ> size_t lds_size(bool f16) { return f16 ? sizeof(Lds<D, NQ, 2>) : sizeof(Lds<D, NQ, 1>); }
 template <int D> size_t lds_size(int nq, bool f16) { return nq == 1 ? lds_size<D, 1>(f16) : nq == 2 ? lds_size<D, 2>(f16) : nq == 3 ? lds_size<D, 3>(f16) : lds_size<D, 4>(f16); }
 size_t lds_size(int d, int nq, bool f16) { return d == 128 ? lds_size<128>(nq, f16) : lds_size<64>(nq, f16); }
@@ -607,10 +699,10 @@ specattn_status mx_attn_configure()
     }
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return SPECATTN_OK;
-    for (int k = 0; k < 16; ++k) {
+    for (int k = 0; k < 32; ++k) {
         const int d = k & 1 ? 128 : 64, nq = (k >> 1 & 3) + 1;
-        const bool f16 = k & 8;
-        if (hipFuncSetAttribute(variant(d, nq, f16), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_size(d, nq, f16)) != hipSuccess) {
+        const bool f16 = k & 8, few = k & 16;
+        if (hipFuncSetAttribute(variant(d, nq, f16, few), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_size(d, nq, f16)) != hipSuccess) {
             (void)hipGetLastError();
             set_error("cannot reserve %zu bytes of LDS", lds_size(d, nq, f16));
             return SPECATTN_EHIP;
@@ -624,23 +716,44 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
 {
     specattn_status st = mx_attn_configure();
     if (st != SPECATTN_OK) return st;
-    const int rows = l.a.B * l.a.H_kv, G = l.a.H_q / l.a.H_kv, per = heads_per_launch(G, l.a.T);
+    const AttnLaunch &c = l.a;
+    const int rows = c.B * c.H_kv, G = c.H_q / c.H_kv, per = heads_per_launch(G, c.T);
+    MxArgs a{};
+    a.counts = c.counts; a.seq_lens = c.seq_lens; a.indices = c.indices;
+    a.codes = l.c.codes; a.scales = l.c.scales; a.page_table = l.c.page_table;
+    a.q = static_cast<const uint16_t *>(c.q);
+    a.out = c.out; a.lse = c.lse; a.out_lowp = c.out_lowp;
+    a.idx_stride = c.idx_stride;
+    a.codes_b = l.c.codes_b; a.codes_h = l.c.codes_h; a.scales_b = l.c.scales_b; a.scales_h = l.c.scales_h;
+    a.q_b = c.q_stride_b; a.q_h = c.q_stride_h; a.q_t = c.q_stride_t;
+    a.codes_n = (uint32_t)(l.c.codes_n >> 4); a.codes_page = (uint32_t)(l.c.codes_page >> 4);
+    a.scales_n = (uint32_t)(l.c.scales_n >> 2); a.scales_page = (uint32_t)(l.c.scales_page >> 2);
+    a.per_h = FastDivisor(c.H_kv); a.per_t = FastDivisor(c.T);
+    a.max_pages = l.c.max_pages; a.page_shift = l.c.page_shift; a.last_page = l.c.num_pages - 1;
+    a.last_slot = c.indices_are_physical ? INT32_MAX : c.n_max - 1;
+    a.H_q = c.H_q; a.H_kv = c.H_kv; a.T = c.T;
+    a.n_max = c.n_max; a.capacity = c.idx_capacity; a.chunk_shift = c.chunk_shift;
+    a.dense = c.dense; a.paged = l.c.page_table ? 1 : c.indices_are_physical ? 2 : 0; a.tail = c.k_new != nullptr; a.dtype = c.dtype;
+    a.to_log2 = c.sm_scale * 1.44269504088896340736f;
+    a.k_new = static_cast<const uint16_t *>(c.k_new); a.v_new = static_cast<const uint16_t *>(c.v_new);
     for (int first = 0; first < G; first += per) {
-        const int heads = std::min(per, G - first), nq = (heads * l.a.T + 15) / 16;
-        MxAttnLaunch part = l;
-        part.a.g_first = first;
-        part.per_h = FastDivisor(l.a.H_kv);
-        part.per_t = FastDivisor(l.a.T);
+        a.first_head = first;
+        a.heads = std::min(per, G - first);
+        a.queries = a.heads * c.T;
+        const int nq = (a.queries + 15) / 16;
         for (int row0 = 0; row0 < rows; row0 += MAX_ROWS) {
-            int here = std::min(MAX_ROWS, rows - row0), at = row0, h = heads;
-            void *args[] = {&part, &at, &here, &h};
-            const bool f16 = l.a.dtype == SPECATTN_F16;
-            if (hipLaunchKernel(variant(l.a.d, nq, f16), dim3(cu_count()), dim3(THREADS), args, lds_size(l.a.d, nq, f16), stream) != hipSuccess) return check_launch("mx_attn_kernel");
+            a.row0 = row0;
+            a.rows = std::min(MAX_ROWS, rows - row0);
+            a.row_parts = static_cast<uint16_t *>(c.workspace);
+            a.slots = reinterpret_cast<float *>(static_cast<char *>(c.workspace) + (((size_t)a.rows * 4 + 255) & ~(size_t)255));
+            void *args[] = {&a};
+            const bool f16 = c.dtype == SPECATTN_F16;
+            if (hipLaunchKernel(variant(c.d, nq, f16, a.rows <= 64), dim3(cu_count()), dim3(nq <= 0 ? Waves<1>::THREADS : Waves<4>::THREADS), args, lds_size(c.d, nq, f16), stream) != hipSuccess) return check_launch("mx_attn_kernel");
             st = check_launch("mx_attn_kernel");
             if (st != SPECATTN_OK) return st;
-            const dim3 grid((heads * l.a.T + 3) / 4, here);
-            if (l.a.d == 128) mx_merge_kernel<128><<<grid, 256, 0, stream>>>(part, row0, here, heads, nq * 16);
-            else mx_merge_kernel<64><<<grid, 256, 0, stream>>>(part, row0, here, heads, nq * 16);
+            const dim3 grid((a.queries + 3) / 4, a.rows);
+            if (c.d == 128) mx_merge_kernel<128><<<grid, 256, 0, stream>>>(a, nq * 16);
+            else mx_merge_kernel<64><<<grid, 256, 0, stream>>>(a, nq * 16);
             st = check_launch("mx_merge_kernel");
             if (st != SPECATTN_OK) return st;
         }
