@@ -309,9 +309,9 @@ specattn_status check_mx_attn(const specattn_mx_attn_args *a)
     if (!dense && a->idx_stride_row < a->idx_capacity) { set_error("idx_stride_row is smaller than idx_capacity"); return SPECATTN_ESHAPE; }
     if (a->chunk_size < 0 || (a->chunk_size > 1 && (!is_pow2(a->chunk_size) || a->chunk_size > 1024))) { set_error("chunk_size must be 0, 1 or a power of two up to 1024"); return SPECATTN_ESHAPE; }
     if (a->chunk_size > 1 && (dense || a->indices_are_physical)) { set_error("chunk lists are not available with dense calls or physical indices"); return SPECATTN_EUNSUPPORTED; }
-    // positions of a row count in 31 bits, and row offsets go to the kernel in units of 16 (codes) and 4 bytes (scales) in 32 bits
-    if (a->chunk_size > 1 && (int64_t)a->idx_capacity * a->chunk_size > INT32_MAX - 65536) { set_error("idx_capacity * chunk_size is too large"); return SPECATTN_ESHAPE; }
-    if ((dense ? c->n_max : a->idx_capacity) > INT32_MAX - 65536) { set_error("too many positions per row"); return SPECATTN_ESHAPE; }
+    // the tiles of a launch are counted in 31 bits, and row offsets go to the kernel in units of 16 (codes) and 4 bytes (scales) in 32 bits
+    const int64_t most = dense ? c->n_max : (int64_t)a->idx_capacity * (a->chunk_size > 1 ? a->chunk_size : 1);
+    if (most > (1 << 24)) { set_error("more than 2^24 positions per row"); return SPECATTN_ESHAPE; }
     const __int128 reach = pool ? (__int128)(c->num_pages - 1) * c->codes_stride_page + (__int128)(c->page_size - 1) * c->codes_stride_n : (__int128)(c->n_max - 1) * c->codes_stride_n;
     const __int128 scales_reach = pool ? (__int128)(c->num_pages - 1) * c->scales_stride_page + (__int128)(c->page_size - 1) * c->scales_stride_n : (__int128)(c->n_max - 1) * c->scales_stride_n;
     if (reach >= ((__int128)1 << 36) || scales_reach >= ((__int128)1 << 34)) { set_error("the rows of a kv head must lie within 64 GiB of its first one (their scales within 16 GiB)"); return SPECATTN_ESHAPE; }

@@ -41,11 +41,11 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // Waves per workgroup, and tiles of a wave in use and on their way.
 template <int NQ> struct Waves {
-    static constexpr int N = NQ <= 0 ? 12 : 8, DEPTH = NQ <= 0 ? 2 : 3, THREADS = N * 64;
+    static constexpr int N = 8, DEPTH = 3, THREADS = N * 64;
 };
 constexpr int TILE = 32;                  // positions per tile
 constexpr int MAX_ROWS = 1024;            // rows per launch
-constexpr int SEG_COST = 6;               // cost of picking a row up, in tiles
+constexpr int SEG_COST = 20;              // cost of picking a row up, in tiles
 constexpr int PARTS = 2;                  // fp16 parts of a weight
 // Weights are taken in units of 2^ref.  ref puts the largest weight so far at 2^HEAD and moves when one exceeds 2^RANGE: fp16 ends at 2^16
 // and, downwards, at 2^-24, so that a weight 2^-36 below the largest still counts.
@@ -84,7 +84,7 @@ template <int D, int NW> struct MergeLds {
 
 template <int D, int NQ, int QP> struct Lds {
     static constexpr int NW = Waves<NQ>::N;
-    static constexpr bool Q = NQ * QP > 1;                                    // queries wait in LDS, else in registers
+    static constexpr bool Q = NQ * QP > 2;                                    // queries wait in LDS, else in registers
     static constexpr int Q_BYTES = Q ? NQ * QP * Geo<D>::KW * 1024 : 16;
     union {
         WaveLds<D, Waves<NQ>::DEPTH> wave[NW];
@@ -143,89 +143,114 @@ __device__ __forceinline__ float shuffle_xor(float x, int mask) { return __shfl_
 
 // What the kernels need of a call.  Row offsets of codes in units of 16 bytes, of scales in units of 4.
 struct MxArgs {
-    const int32_t *counts, *seq_lens, *indices;
+    const int32_t *indices;
     const uint8_t *codes, *scales;
     const int32_t *page_table;
     const uint16_t *q;
     float *out, *lse;
     void *out_lowp;
-    uint16_t *row_parts;                  // [rows][2]: first and last share of a row
+    uint32_t *row_parts;                  // [rows]: first and last share of a row, 16 bits each, or EMPTY
     float *slots;                         // partial (row, share) in slot share + row: [16 NQ][D] o, [16 NQ][2] m and l
     int64_t idx_stride, codes_b, codes_h, scales_b, scales_h, q_b, q_h, q_t;
     uint32_t codes_n, codes_page, scales_n, scales_page;
     FastDivisor per_h, per_t;
     int max_pages, page_shift, last_page, last_slot;
-    int H_q, H_kv, T, first_head, heads, queries, row0, rows, n_max, capacity, chunk_shift;
-    int dense, paged, tail, dtype;        // paged: 1 by a page table, 2 by the list itself
+    int H_q, H_kv, T, first_head, heads, queries, chunk_shift;
+    int paged, tail, dtype;               // paged: 1 by a page table, 2 by the list itself
     float to_log2;
     const uint16_t *k_new, *v_new;        // (the merge alone)
 };
 
-// Positions that row r of sequence b attends to.
-__device__ __forceinline__ int positions_of(const MxArgs &a, int r, int b)
+// What the line of tiles depends on: the kernels' leading arguments, which come in registers with the launch.
+struct Lengths {
+    const int32_t *counts, *seq_lens;
+    uint32_t per_h_mul;
+    int per_h_shift, rows, row0, n_max, capacity, dense, chunk_shift;
+};
+#define LENGTHS_PARAMS const int32_t *counts, const int32_t *seq_lens, uint32_t per_h_mul, int per_h_shift, int rows, int row0, int n_max, int capacity, int dense, int chunk_shift
+
+// Positions that row r of the call attends to.
+__device__ __forceinline__ int positions_of(const Lengths &c, const MxArgs &a, int r)
 {
-    int len = a.n_max;
-    if (a.seq_lens && (a.dense || a.chunk_shift)) len = min(max(a.seq_lens[b], 0), a.n_max);
-    if (a.dense) return len;
-    const int c = min(max(a.counts[r], 0), a.capacity);
-    if (!a.chunk_shift || c == 0) return c;
+    int len = c.n_max;
+    if (c.seq_lens && (c.dense || c.chunk_shift)) {
+        FastDivisor per_h;
+        per_h.mul = c.per_h_mul;
+        per_h.shift = c.per_h_shift;
+        len = min(max(c.seq_lens[per_h.divide(r)], 0), c.n_max);
+    }
+    if (c.dense) return len;
+    const int n = min(max(c.counts[r], 0), c.capacity);
+    if (!c.chunk_shift || n == 0) return n;
     // ascending chunks: only the last can reach past the sequence's length
-    const int over = (int)min((int64_t)1 << a.chunk_shift, max((int64_t)0, (((int64_t)a.indices[r * a.idx_stride + c - 1] + 1) << a.chunk_shift) - len));
-    return (c << a.chunk_shift) - over;
+    const int over = (int)min((int64_t)1 << c.chunk_shift, max((int64_t)0, (((int64_t)a.indices[r * a.idx_stride + n - 1] + 1) << c.chunk_shift) - len));
+    return (n << c.chunk_shift) - over;
 }
 
-// How the line is cut: shares of `size` units, a row's tiles behind `head` units.  Few tiles: shares of at most 32 tiles, whole rounds
-// of the waves, each of one row (a row's units are rounded up to whole shares), so that no workgroup has to pick up a second one.
-struct Share { int size, head; };
-__device__ __forceinline__ Share share_of(int tiles, int filled, int workgroups, int waves)
+// x / y rounded up, for quotients below 2^22
+__device__ __forceinline__ int divide_up(int x, int y)
 {
-    if (filled < workgroups) {
-        const int least = (tiles + workgroups - filled - 1) / (workgroups - filled);
-        const int size = max((least + waves - 1) / waves, 1) * waves;
-        if (size <= 32) return {size, 0};
-    }
-    return {(tiles + SEG_COST * filled + workgroups - 1) / workgroups, SEG_COST};
+    int q = (int)ceilf((float)x * __builtin_amdgcn_rcpf((float)y));
+    q -= (int64_t)(q - 1) * y >= x;
+    q += (int64_t)q * y < x;
+    return q;
 }
-__device__ __forceinline__ int units_of(int tiles, Share s)
-{
-    return tiles == 0 ? 0 : s.head ? tiles + s.head : (tiles + s.size - 1) / s.size * s.size;
-}
+constexpr uint32_t EMPTY = 0xffffffffu;   // the parts of a row that attends to nothing
+
 __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
-// FEW: up to 64 rows, which every wave holds one to a lane; otherwise up to MAX_ROWS in tables, two to a thread.
-template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ>::THREADS) void mx_attn_kernel(MxArgs a)
+// How the work is cut.  FEW, up to 64 rows, which every wave holds one to a lane: each row goes to whole workgroups, as many as its
+// tiles take at `size` tiles each, the smallest size at which the workgroups suffice (small ones in whole rounds of the waves); the
+// row's tiles are dealt to them evenly.  Otherwise the tiles of all rows form one line with SEG_COST ahead of every row, and every
+// workgroup takes an equal stretch of it.  Picking up a second row costs a workgroup about 8 us, the time of 20 tiles: 64 rows of 7500
+// positions 42 us in equal stretches / 36 in whole workgroups.
+template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ>::THREADS) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
 {
     typedef Geo<D> G;
     constexpr int NW = Waves<NQ>::N, DEPTH = Waves<NQ>::DEPTH, AHEAD = DEPTH - 1, THREADS = Waves<NQ>::THREADS;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_bytes[];
     Lds<D, NQ, QP> &lds = *reinterpret_cast<Lds<D, NQ, QP> *>(lds_bytes);
+    const Lengths lengths = {counts, seq_lens, per_h_mul, per_h_shift, rows, row0, n_max, capacity, dense, chunk_shift};
     const int tid = threadIdx.x, lane = tid % 64, low = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int me = blockIdx.x;
-    SPECATTN_PRELOAD(a.counts); SPECATTN_PRELOAD(a.indices); SPECATTN_PRELOAD(a.codes); SPECATTN_PRELOAD(a.scales); SPECATTN_PRELOAD(a.page_table); SPECATTN_PRELOAD(a.q);
+    int my_n = 0;                                                 // FEW: of row `lane`
+    if constexpr (FEW) my_n = positions_of(lengths, a, row0 + min(lane, rows - 1));
+    SPECATTN_PRELOAD(a.indices); SPECATTN_PRELOAD(a.codes); SPECATTN_PRELOAD(a.scales); SPECATTN_PRELOAD(a.page_table); SPECATTN_PRELOAD(a.q); SPECATTN_PRELOAD(a.row_parts);
     SPECATTN_PRELOAD(a.idx_stride); SPECATTN_PRELOAD(a.codes_h); SPECATTN_PRELOAD(a.scales_h); SPECATTN_PRELOAD(a.q_h); SPECATTN_PRELOAD(a.q_t); SPECATTN_PRELOAD(a.codes_n);
-    SPECATTN_PRELOAD(a.per_h.mul); SPECATTN_PRELOAD(a.per_t.mul); SPECATTN_PRELOAD(a.max_pages); SPECATTN_PRELOAD(a.H_q); SPECATTN_PRELOAD(a.first_head); SPECATTN_PRELOAD(a.dense);
+    SPECATTN_PRELOAD(a.per_h.mul); SPECATTN_PRELOAD(a.per_t.mul); SPECATTN_PRELOAD(a.max_pages); SPECATTN_PRELOAD(a.H_q); SPECATTN_PRELOAD(a.first_head); SPECATTN_PRELOAD(a.paged);
 
-    // The line: every workgroup works it out for itself.
-    int my_n = 0, my_prefix = 0, total;                           // FEW: of row `lane`
-    Share share;
+    int r, t0, t1, n, u = 0, u_end = 0, size = 0;                 // this workgroup's first row, its tiles of it, the row's positions
     if constexpr (FEW) {
-        const int r = a.row0 + min(lane, a.rows - 1), n = positions_of(a, r, a.per_h.divide(r));
-        my_n = lane < a.rows ? n : 0;
-        const int tiles = (my_n + TILE - 1) / TILE;
-        share = share_of(wave_last(wave_inclusive_sum(tiles)), __popcll(__ballot(my_n > 0)), gridDim.x, NW);
-        const int units = units_of(tiles, share), upto = wave_inclusive_sum(units);
-        my_prefix = upto - units;
-        total = wave_last(upto);
+        my_n = lane < rows ? my_n : 0;
+        const int tiles = (my_n + TILE - 1) / TILE, all = wave_last(wave_inclusive_sum(tiles)), W = gridDim.x;
+        int s = max((all + W - 1) / W, NW), groups, upto;
+        if (s <= 4 * NW) s = (s + NW - 1) / NW * NW;
+        while (true) {
+            groups = divide_up(tiles, s);
+            upto = wave_inclusive_sum(groups);
+            const int need = wave_last(upto);
+            if (need <= W) break;
+            s += s <= 4 * NW ? NW : max(1, s * (need - W) / W);
+        }
+        if (me == 0 && tid < rows) a.row_parts[tid] = my_n == 0 ? EMPTY : (uint32_t)(upto - groups) | (uint32_t)(upto - 1) << 16;
+        const uint64_t mine = __ballot(me >= upto - groups && me < upto);
+        if (mine == 0) return;
+        r = __builtin_ctzll(mine);
+        n = __builtin_amdgcn_readlane(my_n, r);
+        const int row_tiles = (n + TILE - 1) / TILE, parts = __builtin_amdgcn_readlane(groups, r), k = me - (__builtin_amdgcn_readlane(upto, r) - parts);
+        const int even = __builtin_amdgcn_readfirstlane(divide_up(row_tiles + 1, parts)) - 1, more = row_tiles - even * parts;       // (row_tiles / parts rounded down)
+        t0 = k * even + min(k, more);
+        t1 = t0 + even + (k < more);
     } else {
-        int n[2], tiles = 0, filled = 0;
+        int c[2], tiles = 0, filled = 0;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int r = 2 * tid + i;
-            n[i] = tid < MAX_ROWS / 2 && r < a.rows ? positions_of(a, a.row0 + r, a.per_h.divide(a.row0 + r)) : 0;
-            if (tid < MAX_ROWS / 2) lds.count[r] = n[i];
-            tiles += (n[i] + TILE - 1) / TILE;
-            filled += n[i] > 0;
+            const int x = 2 * tid + i;
+            c[i] = x < rows ? positions_of(lengths, a, row0 + x) : 0;
+            lds.count[x] = c[i];
+            tiles += (c[i] + TILE - 1) / TILE;
+            filled += c[i] > 0;
         }
         tiles = wave_last(wave_inclusive_sum(tiles));
         filled = wave_last(wave_inclusive_sum(filled));
@@ -234,44 +259,49 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
         tiles = filled = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) { tiles += lds.red[0][w]; filled += lds.red[1][w]; }
-        share = share_of(tiles, filled, gridDim.x, NW);
-        const int first = units_of((n[0] + TILE - 1) / TILE, share), second = units_of((n[1] + TILE - 1) / TILE, share);
+        size = max(1, (int)(((int64_t)tiles + (int64_t)SEG_COST * filled + gridDim.x - 1) / gridDim.x));
+        const int first = c[0] ? (c[0] + TILE - 1) / TILE + SEG_COST : 0, second = c[1] ? (c[1] + TILE - 1) / TILE + SEG_COST : 0;
         const int upto = wave_inclusive_sum(first + second);
         __syncthreads();                                          // (red is used again)
         if (lane == 63) lds.red[0][wave] = upto;
         __syncthreads();
-        int before = upto - first - second;
-        total = 0;
+        int before = upto - first - second, total = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             if (w < wave) before += lds.red[0][w];
             total += lds.red[0][w];
         }
-        if (tid < MAX_ROWS / 2) {
-            lds.prefix[2 * tid] = before;
-            lds.prefix[2 * tid + 1] = before + first;
-        }
+        lds.prefix[2 * tid] = before;
+        lds.prefix[2 * tid + 1] = before + first;
         if (tid == THREADS - 1) lds.prefix[MAX_ROWS] = total;
+        if (me == 0) {                                            // first and last share of every row
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int start = (i ? before + first : before) + SEG_COST;
+                if (2 * tid + i < rows)
+                    a.row_parts[2 * tid + i] = c[i] == 0 ? EMPTY : (uint32_t)(start / size) | (uint32_t)((start + (c[i] + TILE - 1) / TILE - 1) / size) << 16;
+            }
+        }
         // the thread whose rows hold this workgroup's first unit says so
-        const int u = me * share.size;
+        u = me * size;
         if (u >= before && u < before + first + second) lds.red[1][0] = u < before + first ? 2 * tid : 2 * tid + 1;
         __syncthreads();
+        u_end = min(u + size, total);
+        if (u >= u_end) return;
+        r = __builtin_amdgcn_readfirstlane(lds.red[1][0]);
     }
-    auto prefix_of = [&](int r) { return FEW ? __builtin_amdgcn_readlane(my_prefix, r) : __builtin_amdgcn_readfirstlane(lds.prefix[r]); };
-    auto end_of = [&](int r) { return FEW ? r < 63 ? __builtin_amdgcn_readlane(my_prefix, r + 1) : total : __builtin_amdgcn_readfirstlane(lds.prefix[r + 1]); };
-    auto count_of = [&](int r) { return FEW ? __builtin_amdgcn_readlane(my_n, r) : __builtin_amdgcn_readfirstlane(lds.count[r]); };
 
-    int u = me * share.size;
-    const int u_end = min(u + share.size, total);
-    if (u >= u_end) return;
-    // the last row that starts at or ahead of unit u (empty rows ahead of it start there too)
-    int r = FEW ? 63 - __builtin_clzll(__ballot(my_prefix <= u && my_n > 0)) : __builtin_amdgcn_readfirstlane(lds.red[1][0]);
-
-    for (; u < u_end; u = end_of(r), ++r) {
-        const int row_start = prefix_of(r), n = count_of(r), row_tiles = (n + TILE - 1) / TILE;
-        const int t0 = max(0, u - row_start - share.head), t1 = min(row_tiles, u_end - row_start - share.head);
-        if (t1 <= t0) continue;                                   // (an empty row, or the share ends ahead of the row's first tile)
-        const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
+    for (bool more = true; more; ++r) {
+        if constexpr (!FEW) {
+            const int row_start = __builtin_amdgcn_readfirstlane(lds.prefix[r]);
+            n = __builtin_amdgcn_readfirstlane(lds.count[r]);
+            t0 = max(0, u - row_start - SEG_COST);
+            t1 = min((n + TILE - 1) / TILE, u_end - row_start - SEG_COST);
+            u = __builtin_amdgcn_readfirstlane(lds.prefix[r + 1]);
+            more = u < u_end;
+            if (t1 <= t0) continue;                               // (an empty row, or the share ends ahead of the row's first tile)
+        } else more = false;
+        const int row_tiles = (n + TILE - 1) / TILE, row = row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
         const int head0 = h * (a.H_q / a.H_kv) + a.first_head;
 
         // queries: element j of k-step s in lane (q, g) is element (d/4) g + 8 s + j of query 16 qt + q
@@ -335,7 +365,7 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
         const int32_t *list = a.indices + row * a.idx_stride, *pages = a.page_table + (int64_t)b * a.max_pages;
         const uint8_t *codes = a.codes + (a.paged ? 0 : b * a.codes_b) + h * a.codes_h;
         const uint8_t *scales = a.scales + (a.paged ? 0 : b * a.scales_b) + h * a.scales_h + (D == 128 ? lane / 32 * 4 : 0);
-        const bool listed = !a.dense, looked_up = a.paged == 1;
+        const bool listed = !dense, looked_up = a.paged == 1;
         const int base_tile = t0 + wave, in_tile = lane % TILE;
         const int lane_piece = (lane % G::LPR) ^ G::swz(lane / G::LPR * G::CI);      // (of instruction 0; of instruction k: ^ k)
         auto list_rank = [&](int i) { return min((base_tile + i * NW) * TILE + in_tile, n - 1); };
@@ -401,12 +431,16 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
             if (looked_up)
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) page[i] = pages[slot[i] >> a.page_shift];
+#pragma unroll 1
+            for (int i = 0; i < AHEAD; ++i) {                     // (one copy of the code: a launch starts with none of it in the caches)
+                request_codes(slot[0], page[0], i);
+                request_pages(slot[AHEAD], i == 0 ? AHEAD % DEPTH : (AHEAD + 1) % DEPTH);
+                request_words(2 * AHEAD + i, i == 0 ? 2 * AHEAD % DEPTH : (2 * AHEAD + 1) % DEPTH);
+                const int first = slot[0];
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                request_codes(slot[i], page[i], i);
-                request_pages(slot[AHEAD + i], (AHEAD + i) % DEPTH);
-                request_words(2 * AHEAD + i, (2 * AHEAD + i) % DEPTH);
-                slot[i] = slot[AHEAD + i];
+                for (int k = 0; k + 1 < 2 * AHEAD; ++k) slot[k] = slot[k + 1];
+                slot[2 * AHEAD - 1] = first;
+                page[0] = page[AHEAD - 1];
             }
             int at = 0;                                           // tile i lies in buffer `at`; slot[]: of tiles i + AHEAD ...
             for (int i = 0, t = base_tile; t < t1; ++i, t += NW) {
@@ -473,6 +507,14 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
                         if constexpr (D == 128) v[4 * k + j] = *reinterpret_cast<const uint32_t *>(src + low % 4 * 4);
                         else v[4 * k + j] = *reinterpret_cast<const uint16_t *>(src + low % 8 * 2);
                     }
+                }
+                // The scores are read by the vector unit next, in another block of the program.  The compiler has been seen to leave the wait
+                // that a matrix result needs ahead of it out there: it is written out.
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int qt = 0; qt < NQ; ++qt) {
+                    if (qt == 0) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(s[qt][0]), "+v"(s[qt][1]));
+                    else asm volatile("" : "+v"(s[qt][0]), "+v"(s[qt][1]));
                 }
                 const int left = n - t * TILE;
                 if (__builtin_expect(left < TILE, 0)) {                                // a row's last tile: what lies behind it repeats its last position
@@ -589,8 +631,6 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
             }
             __syncthreads();
         }
-        if (tid == 0 && t0 == 0) a.row_parts[2 * r] = (uint16_t)me;
-        if (tid == 0 && t1 == row_tiles) a.row_parts[2 * r + 1] = (uint16_t)me;
     }
 }
 
@@ -602,30 +642,52 @@ __device__ __forceinline__ float wave_sum(float x)
     return x;
 }
 
-// One wave per (row, query): the row's partials in share order, then the new tokens behind the cache up to the query's own.
-template <int D> __global__ __launch_bounds__(256) void mx_merge_kernel(MxArgs a, int padded)
+// One wave per (row, query): the row's partials in share order, eight to a trip to memory, then the new tokens behind the cache up to
+// the query's own.
+template <int D> __global__ __launch_bounds__(256) void mx_merge_kernel(const uint32_t *row_parts, const float *slots, int row0, int padded, int queries, MxArgs a)
 {
-    constexpr int E = D / 64;                                     // elements per lane
+    constexpr int E = D / 64, TRIP = 8;                           // elements per lane
     const int lane = threadIdx.x % 64;
     const int r = blockIdx.y, i = blockIdx.x * 4 + threadIdx.x / 64;
-    if (i >= a.queries) return;
-    const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
+    if (i >= queries) return;
+    const uint32_t parts = row_parts[r];
+    SPECATTN_PRELOAD(a.out); SPECATTN_PRELOAD(a.lse); SPECATTN_PRELOAD(a.out_lowp); SPECATTN_PRELOAD(a.per_h.mul); SPECATTN_PRELOAD(a.per_t.mul); SPECATTN_PRELOAD(a.H_q);
+    const int row = row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
     const int gh = a.per_t.divide(i), t = i - gh * a.T, head = h * (a.H_q / a.H_kv) + a.first_head + gh;
     const int64_t orow = ((int64_t)b * a.H_q + head) * a.T + t;
     float m = -INFINITY, l = 0.0f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.0f;
-    if (positions_of(a, row, b) > 0) {
-        const int first = a.row_parts[2 * r], last = a.row_parts[2 * r + 1];
+    if (parts != EMPTY) {
+        const int first = parts & 0xffff, last = parts >> 16;
         if (first == last && !a.tail) return;                     // finished by its only workgroup
-        for (int w = first; w <= last; ++w) {
-            const float *slot = a.slots + (size_t)(w + r) * padded * (D + 2);
-            const float mw = slot[padded * D + 2 * i], lw = slot[padded * D + 2 * i + 1];
-            const float now = fmaxf(m, mw);
-            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now), fw = __builtin_amdgcn_exp2f(mw - now);
-            l = l * f + lw * fw;
+        for (int w = first; w <= last; w += TRIP) {
+            float mw[TRIP], lw[TRIP], ow[TRIP][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = o[e] * f + slot[i * D + E * lane + e] * fw;
+            for (int k = 0; k < TRIP; ++k) {                      // (behind the last: that one again)
+                const float *slot = slots + (size_t)(min(w + k, last) + r) * padded * (D + 2);
+                const f32x2 ml = *reinterpret_cast<const f32x2 *>(slot + padded * D + 2 * i);
+                mw[k] = ml[0];
+                lw[k] = ml[1];
+#pragma unroll
+                for (int e = 0; e < E; ++e) ow[k][e] = slot[i * D + E * lane + e];
+            }
+            __builtin_amdgcn_sched_barrier(0);                    // all requested before the first is used
+            float now = m;
+#pragma unroll
+            for (int k = 0; k < TRIP; ++k) now = fmaxf(now, w + k <= last ? mw[k] : -INFINITY);
+            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now);
+            l *= f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll
+            for (int k = 0; k < TRIP; ++k) {
+                if (w + k > last) break;
+                const float fw = __builtin_amdgcn_exp2f(mw[k] - now);
+                l += lw[k] * fw;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += ow[k][e] * fw;
+            }
             m = now;
         }
     }
@@ -719,7 +781,7 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
     const AttnLaunch &c = l.a;
     const int rows = c.B * c.H_kv, G = c.H_q / c.H_kv, per = heads_per_launch(G, c.T);
     MxArgs a{};
-    a.counts = c.counts; a.seq_lens = c.seq_lens; a.indices = c.indices;
+    a.indices = c.indices;
     a.codes = l.c.codes; a.scales = l.c.scales; a.page_table = l.c.page_table;
     a.q = static_cast<const uint16_t *>(c.q);
     a.out = c.out; a.lse = c.lse; a.out_lowp = c.out_lowp;
@@ -732,8 +794,8 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
     a.max_pages = l.c.max_pages; a.page_shift = l.c.page_shift; a.last_page = l.c.num_pages - 1;
     a.last_slot = c.indices_are_physical ? INT32_MAX : c.n_max - 1;
     a.H_q = c.H_q; a.H_kv = c.H_kv; a.T = c.T;
-    a.n_max = c.n_max; a.capacity = c.idx_capacity; a.chunk_shift = c.chunk_shift;
-    a.dense = c.dense; a.paged = l.c.page_table ? 1 : c.indices_are_physical ? 2 : 0; a.tail = c.k_new != nullptr; a.dtype = c.dtype;
+    a.chunk_shift = c.chunk_shift;
+    a.paged = l.c.page_table ? 1 : c.indices_are_physical ? 2 : 0; a.tail = c.k_new != nullptr; a.dtype = c.dtype;
     a.to_log2 = c.sm_scale * 1.44269504088896340736f;
     a.k_new = static_cast<const uint16_t *>(c.k_new); a.v_new = static_cast<const uint16_t *>(c.v_new);
     for (int first = 0; first < G; first += per) {
@@ -742,18 +804,18 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
         a.queries = a.heads * c.T;
         const int nq = (a.queries + 15) / 16;
         for (int row0 = 0; row0 < rows; row0 += MAX_ROWS) {
-            a.row0 = row0;
-            a.rows = std::min(MAX_ROWS, rows - row0);
-            a.row_parts = static_cast<uint16_t *>(c.workspace);
-            a.slots = reinterpret_cast<float *>(static_cast<char *>(c.workspace) + (((size_t)a.rows * 4 + 255) & ~(size_t)255));
-            void *args[] = {&a};
+            int here = std::min(MAX_ROWS, rows - row0), at = row0;
+            a.row_parts = static_cast<uint32_t *>(c.workspace);
+            a.slots = reinterpret_cast<float *>(static_cast<char *>(c.workspace) + (((size_t)here * 4 + 255) & ~(size_t)255));
+            Lengths n = {c.counts, c.seq_lens, a.per_h.mul, a.per_h.shift, here, at, c.n_max, c.idx_capacity, c.dense, c.chunk_shift};
+            void *args[] = {&n.counts, &n.seq_lens, &n.per_h_mul, &n.per_h_shift, &n.rows, &n.row0, &n.n_max, &n.capacity, &n.dense, &n.chunk_shift, &a};
             const bool f16 = c.dtype == SPECATTN_F16;
-            if (hipLaunchKernel(variant(c.d, nq, f16, a.rows <= 64), dim3(cu_count()), dim3(nq <= 0 ? Waves<1>::THREADS : Waves<4>::THREADS), args, lds_size(c.d, nq, f16), stream) != hipSuccess) return check_launch("mx_attn_kernel");
+            if (hipLaunchKernel(variant(c.d, nq, f16, here <= std::min(64, cu_count())), dim3(cu_count()), dim3(Waves<1>::THREADS), args, lds_size(c.d, nq, f16), stream) != hipSuccess) return check_launch("mx_attn_kernel");
             st = check_launch("mx_attn_kernel");
             if (st != SPECATTN_OK) return st;
-            const dim3 grid((a.queries + 3) / 4, a.rows);
-            if (c.d == 128) mx_merge_kernel<128><<<grid, 256, 0, stream>>>(a, nq * 16);
-            else mx_merge_kernel<64><<<grid, 256, 0, stream>>>(a, nq * 16);
+            const dim3 grid((a.queries + 3) / 4, here);
+            if (c.d == 128) mx_merge_kernel<128><<<grid, 256, 0, stream>>>(a.row_parts, a.slots, at, nq * 16, a.queries, a);
+            else mx_merge_kernel<64><<<grid, 256, 0, stream>>>(a.row_parts, a.slots, at, nq * 16, a.queries, a);
             st = check_launch("mx_merge_kernel");
             if (st != SPECATTN_OK) return st;
         }
