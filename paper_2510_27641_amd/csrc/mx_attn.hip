@@ -40,8 +40,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // Waves per workgroup, and tiles of a wave in use and on their way.
-template <int NQ> struct Waves {
-    static constexpr int N = 8, DEPTH = 3, THREADS = N * 64;
+template <int NQ, bool FEW> struct Waves {
+    static constexpr int N = FEW && NQ == 1 ? 12 : 8, DEPTH = N == 12 ? 2 : 3, THREADS = N * 64;
 };
 constexpr int TILE = 32;                  // positions per tile
 constexpr int MAX_ROWS = 1024;            // rows per launch
@@ -82,12 +82,12 @@ template <int D, int NW> struct MergeLds {
     float ml[NW][16][2];
 };
 
-template <int D, int NQ, int QP> struct Lds {
-    static constexpr int NW = Waves<NQ>::N;
-    static constexpr bool Q = NQ * QP > 2;                                    // queries wait in LDS, else in registers
+template <int D, int NQ, int QP, bool FEW> struct Lds {
+    static constexpr int NW = Waves<NQ, FEW>::N;
+    static constexpr bool Q = NQ * QP > 2;                                              // queries wait in LDS, else in registers
     static constexpr int Q_BYTES = Q ? NQ * QP * Geo<D>::KW * 1024 : 16;
     union {
-        WaveLds<D, Waves<NQ>::DEPTH> wave[NW];
+        WaveLds<D, Waves<NQ, FEW>::DEPTH> wave[NW];
         MergeLds<D, NW> merge;
     };
     uint8_t q[Q_BYTES] __attribute__((aligned(16)));
@@ -95,7 +95,7 @@ template <int D, int NQ, int QP> struct Lds {
     int count[MAX_ROWS];
     int red[2][NW];
 };
-static_assert(sizeof(Lds<128, 4, 2>) <= 160 * 1024, "a workgroup must fit a CU's LDS");
+static_assert(sizeof(Lds<128, 4, 2, false>) <= 160 * 1024, "a workgroup must fit a CU's LDS");
 
 // Requests 16 or 4 bytes per lane from `src` to `to` + 16 or 4 * lane in LDS.  Counts as one request of the wave in order; nobody but
 // wait_requests waits for it.
@@ -204,12 +204,12 @@ __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readla
 // row's tiles are dealt to them evenly.  Otherwise the tiles of all rows form one line with SEG_COST ahead of every row, and every
 // workgroup takes an equal stretch of it.  Picking up a second row costs a workgroup about 8 us, the time of 20 tiles: 64 rows of 7500
 // positions 42 us in equal stretches / 36 in whole workgroups.
-template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ>::THREADS) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
+template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<NQ, FEW>::THREADS)) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
 {
     typedef Geo<D> G;
-    constexpr int NW = Waves<NQ>::N, DEPTH = Waves<NQ>::DEPTH, AHEAD = DEPTH - 1, THREADS = Waves<NQ>::THREADS;
+    constexpr int NW = Waves<NQ, FEW>::N, DEPTH = Waves<NQ, FEW>::DEPTH, AHEAD = DEPTH - 1, THREADS = Waves<NQ, FEW>::THREADS;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_bytes[];
-    Lds<D, NQ, QP> &lds = *reinterpret_cast<Lds<D, NQ, QP> *>(lds_bytes);
+    Lds<D, NQ, QP, FEW> &lds = *reinterpret_cast<Lds<D, NQ, QP, FEW> *>(lds_bytes);
     const Lengths lengths = {counts, seq_lens, per_h_mul, per_h_shift, rows, row0, n_max, capacity, dense, chunk_shift};
     const int tid = threadIdx.x, lane = tid % 64, low = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -305,7 +305,7 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
         const int head0 = h * (a.H_q / a.H_kv) + a.first_head;
 
         // queries: element j of k-step s in lane (q, g) is element (d/4) g + 8 s + j of query 16 qt + q
-        uint32_t qf[Lds<D, NQ, QP>::Q ? 1 : NQ * QP][G::KW][4];
+        uint32_t qf[Lds<D, NQ, QP, FEW>::Q ? 1 : NQ * QP][G::KW][4];
         {
             auto query = [&](int qt) {
                 const int i = min(qt * 16 + low, a.queries - 1), gh = a.per_t.divide(i), t = i - gh * a.T;      // (behind the last query: that one again)
@@ -322,7 +322,7 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
                     }
                 }
             };
-            if constexpr (Lds<D, NQ, QP>::Q) {
+            if constexpr (Lds<D, NQ, QP, FEW>::Q) {
                 for (int k = wave; k < NQ * G::KW; k += NW) {
                     uint32_t part[QP][4];
                     split(*reinterpret_cast<const u32x4 *>(query(k / G::KW) + 8 * (k % G::KW)), part);
@@ -488,7 +488,7 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__(Waves<NQ
                         for (int j = 0; j < 4; ++j) f[j] = pair_of(key[k][step], scale, j);
 #pragma unroll
                         for (int q = 0; q < QP * NQ; ++q) {
-                            if constexpr (Lds<D, NQ, QP>::Q) {
+                            if constexpr (Lds<D, NQ, QP, FEW>::Q) {
                                 const u32x4 x = *reinterpret_cast<const u32x4 *>(lds.q + ((q * G::KW + step) * 64 + lane) * 16);
                                 const uint32_t y[4] = {x[0], x[1], x[2], x[3]};
                                 s[q % NQ][k] = mfma(f, y, s[q % NQ][k]);
@@ -729,9 +729,16 @@ template <int D> const void *variant(int nq, bool f16, bool few)
     return nq == 1 ? variant<D, 1>(f16, few) : nq == 2 ? variant<D, 2>(f16, few) : nq == 3 ? variant<D, 3>(f16, few) : variant<D, 4>(f16, few);
 }
 const void *variant(int d, int nq, bool f16, bool few) { return d == 128 ? variant<128>(nq, f16, few) : variant<64>(nq, f16, few); }
-template <int D, int NQ> size_t lds_size(bool f16) { return f16 ? sizeof(Lds<D, NQ, 2>) : sizeof(Lds<D, NQ, 1>); }
-template <int D> size_t lds_size(int nq, bool f16) { return nq == 1 ? lds_size<D, 1>(f16) : nq == 2 ? lds_size<D, 2>(f16) : nq == 3 ? lds_size<D, 3>(f16) : lds_size<D, 4>(f16); }
-size_t lds_size(int d, int nq, bool f16) { return d == 128 ? lds_size<128>(nq, f16) : lds_size<64>(nq, f16); }
+template <int D, int NQ> size_t lds_size(bool f16, bool few)
+{
+    return f16 ? few ? sizeof(Lds<D, NQ, 2, true>) : sizeof(Lds<D, NQ, 2, false>) : few ? sizeof(Lds<D, NQ, 1, true>) : sizeof(Lds<D, NQ, 1, false>);
+}
+template <int D> size_t lds_size(int nq, bool f16, bool few)
+{
+    return nq == 1 ? lds_size<D, 1>(f16, few) : nq == 2 ? lds_size<D, 2>(f16, few) : nq == 3 ? lds_size<D, 3>(f16, few) : lds_size<D, 4>(f16, few);
+}
+size_t lds_size(int d, int nq, bool f16, bool few) { return d == 128 ? lds_size<128>(nq, f16, few) : lds_size<64>(nq, f16, few); }
+int threads_of(int nq, bool few) { return few && nq == 1 ? Waves<1, true>::THREADS : Waves<1, false>::THREADS; }
 
 // Query heads of a kv head per launch: groups of more than 64 query rows go out in equal parts.
 int heads_per_launch(int G, int T)
@@ -764,9 +771,9 @@ specattn_status mx_attn_configure()
     for (int k = 0; k < 32; ++k) {
         const int d = k & 1 ? 128 : 64, nq = (k >> 1 & 3) + 1;
         const bool f16 = k & 8, few = k & 16;
-        if (hipFuncSetAttribute(variant(d, nq, f16, few), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_size(d, nq, f16)) != hipSuccess) {
+        if (hipFuncSetAttribute(variant(d, nq, f16, few), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_size(d, nq, f16, few)) != hipSuccess) {
             (void)hipGetLastError();
-            set_error("cannot reserve %zu bytes of LDS", lds_size(d, nq, f16));
+            set_error("cannot reserve %zu bytes of LDS", lds_size(d, nq, f16, few));
             return SPECATTN_EHIP;
         }
     }
@@ -810,7 +817,8 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
             Lengths n = {c.counts, c.seq_lens, a.per_h.mul, a.per_h.shift, here, at, c.n_max, c.idx_capacity, c.dense, c.chunk_shift};
             void *args[] = {&n.counts, &n.seq_lens, &n.per_h_mul, &n.per_h_shift, &n.rows, &n.row0, &n.n_max, &n.capacity, &n.dense, &n.chunk_shift, &a};
             const bool f16 = c.dtype == SPECATTN_F16;
-            if (hipLaunchKernel(variant(c.d, nq, f16, here <= std::min(64, cu_count())), dim3(cu_count()), dim3(Waves<1>::THREADS), args, lds_size(c.d, nq, f16), stream) != hipSuccess) return check_launch("mx_attn_kernel");
+            const bool few = here <= std::min(64, cu_count());
+            if (hipLaunchKernel(variant(c.d, nq, f16, few), dim3(cu_count()), dim3(threads_of(nq, few)), args, lds_size(c.d, nq, f16, few), stream) != hipSuccess) return check_launch("mx_attn_kernel");
             st = check_launch("mx_attn_kernel");
             if (st != SPECATTN_OK) return st;
             const dim3 grid((a.queries + 3) / 4, here);
