@@ -13,12 +13,24 @@ namespace specattn {
 namespace {
 
 constexpr int ADD_THREADS = 256, ADD_SLOTS = 4;               // a thread adds up slots j, j + 256, j + 512, j + 768
-constexpr int PICK_WAVES = 16, PICK_THREADS = PICK_WAVES * 64;
+constexpr int PICK_THREADS = 1024;                            // of a workgroup that holds a whole row
+constexpr int SLICE_THREADS = 512, SLICE_KEYS = 8, SLICE = SLICE_THREADS * SLICE_KEYS;       // and of one that holds a slice of it: keys per thread, slots
+constexpr int MAX_SLICES = SPECATTN_MAX_N / SLICE;
+// A key is found 12, 10 and 10 bits at a time: with 11 in the first pass, four bins per octave, the lanes that meet in one counter, which are
+// added one after the other, took most of it.
+constexpr int TOP_BITS = 12, MID_BITS = 10, LOW_BITS = 10;
+constexpr int TOP_BINS = 1 << TOP_BITS, MID_BINS = 1 << MID_BITS, LOW_BINS = 1 << LOW_BITS, TOP_SHIFT = 32 - TOP_BITS;
 constexpr uint32_t KEY_STAYS = 0xffffffffu, KEY_NAN = 0;
 
 struct EvictLaunch {
     specattn_evict_args e;
-    uint32_t *keys;                                           // [B*H][n_max]
+    uint32_t *keys;                                           // [B*H][stride]
+    int stride;                                               // n_max, rounded up to whole threads of either kind of workgroup
+    // rows that are cut up
+    uint32_t *hist;                                           // [B*H][TOP_BINS]
+    uint32_t *candidates;                                     // [B*H][stride]: of every slice, its keys in the bin of the K-th largest, in slot order
+    int32_t *info;                                            // [B*H][slices][4]: keys above that bin and in it, each below and beyond the new length
+    int slices;                                               // 0: rows are not cut up
     int members;                                              // rows of probs per score row
 };
 
@@ -41,6 +53,10 @@ __global__ __launch_bounds__(ADD_THREADS) void evict_add_kernel(EvictLaunch l)
         const int b = r / e.H, h = r - b * e.H, len = row_length(e, b);
         const int first = blockIdx.x * ADD_THREADS * ADD_SLOTS + threadIdx.x;
         const int64_t row = b * e.row_stride_b + h * e.row_stride_h;
+        if (l.slices && blockIdx.x == 0) {                    // (the launches behind this one add to these)
+            for (int i = threadIdx.x; i < TOP_BINS; i += ADD_THREADS) l.hist[(int64_t)r * TOP_BINS + i] = 0;
+            if (e.row_flags && threadIdx.x == 0) e.row_flags[r] = 0;
+        }
         const int next = e.next_positions[b];
         double sum[ADD_SLOTS];
         int at[ADD_SLOTS];
@@ -63,139 +79,343 @@ __global__ __launch_bounds__(ADD_THREADS) void evict_add_kernel(EvictLaunch l)
             const int64_t place = e.positions[row + j];
             const bool stays = place < e.sinks || place >= (int64_t)next - e.recent;
             e.scores_out[row + j] = score;
-            l.keys[(int64_t)r * e.n_max + j] = stays ? KEY_STAYS : key_of(score);
+            l.keys[(int64_t)r * l.stride + j] = stays ? KEY_STAYS : key_of(score);
         }
     }
 }
 
-struct Pick {
-    uint32_t bins[2048];
-    int wave_sum[PICK_WAVES][4];                              // above / equal to the K-th key, below / beyond the new length
+// Shared memory of a selecting workgroup.
+template <int THREADS> struct Pick {
+    uint32_t bins[TOP_BINS];
+    int wave_sum[THREADS / 64][2];
     int found[2];
+    uint32_t kept[THREADS];                                   // a bit per key of a thread
 };
 
-// The bin that holds the K-th largest of the counted entries, and how many lie above it.  Called by all threads.
-__device__ __forceinline__ void locate(Pick &s, int bins, int K, int &bin, int &above)
+__device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
+
+// The bin that holds the K-th largest of the counted entries (there are as many at least), and how many lie above it.  Called by all threads,
+// which take the bins from the highest down, BINS / THREADS each.
+template <int BINS, int THREADS> __device__ __forceinline__ void locate(Pick<THREADS> &s, int K, int &bin, int &above)
 {
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    constexpr int PER = BINS > THREADS ? BINS / THREADS : 1;
+    const int tid = threadIdx.x, wave = tid / 64;
     __syncthreads();
-    if (wave == 0) {                                          // lane i holds the i-th highest run of bins
-        const int run = bins / 64, top = bins - 1 - lane * run;
-        int mine = 0;
-        for (int i = 0; i < run; ++i) mine += s.bins[top - i];
-        const int upto = wave_inclusive_sum(mine);
-        if (upto - mine < K && K <= upto) {
-            int over = upto - mine;
-            for (int i = 0; i < run; ++i) {
-                const int c = s.bins[top - i];
-                if (over + c >= K) { s.found[0] = top - i; s.found[1] = over; break; }
-                over += c;
-            }
-        }
+    const int top = BINS - 1 - tid * PER;
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine += top >= 0 ? s.bins[top - (i + tid) % PER] : 0;       // (each thread from a place of its own: other banks)
+    int upto = wave_inclusive_sum(mine);
+    if (tid % 64 == 63) s.wave_sum[wave][0] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += s.wave_sum[w][0];
+    if (upto - mine < K && K <= upto) {
+        int over = upto - mine, at = top;
+        for (int c; over + (c = s.bins[at]) < K; --at) over += c;
+        s.found[0] = at;
+        s.found[1] = over;
     }
     __syncthreads();
     bin = s.found[0];
     above = s.found[1];
 }
-
-// One workgroup per row.
-__global__ __launch_bounds__(PICK_THREADS) void evict_pick_kernel(EvictLaunch l)
+template <int BINS, int THREADS> __device__ __forceinline__ void clear(Pick<THREADS> &s)
 {
-    __shared__ Pick s;
+    for (int i = threadIdx.x; i < BINS; i += THREADS) s.bins[i] = 0;
+    __syncthreads();
+}
+
+// A row's arrays.
+struct EvictRow {
+    int r, b, h, len, K;
+    float *scores;
+    const int32_t *from;
+    int32_t *to, *src, *dst;
+    __device__ __forceinline__ EvictRow(const specattn_evict_args &e, int row) : r(row), b(row / e.H)
+    {
+        h = row - b * e.H;
+        len = row_length(e, b);
+        K = min(len, e.budget);
+        const int64_t at = b * e.row_stride_b + h * e.row_stride_h;
+        scores = e.scores_out + at;
+        from = e.positions + at;
+        to = e.positions_out + at;
+        src = e.move_src + row * e.move_stride_row;
+        dst = e.move_dst + row * e.move_stride_row;
+    }
+};
+
+// A thread's keys: those of KEYS consecutive slots from `first`.
+template <int KEYS> struct Held {
+    uint32_t key[KEYS] __attribute__((aligned(16)));
+    int first;
+    __device__ __forceinline__ void load(const uint32_t *keys, int start, int len)
+    {
+        first = start + threadIdx.x * KEYS;
+        if (first >= len) return;                             // (what lies behind the row is not looked at)
+#pragma unroll
+        for (int k = 0; k < KEYS; k += 4) *reinterpret_cast<uint4 *>(key + k) = *reinterpret_cast<const uint4 *>(keys + first + k);
+    }
+};
+
+// Keys above `cut` and equal to it, below and beyond slot K; two counts to a word, the lower half that of the slots below K.
+struct Sides { uint32_t above = 0, equal = 0; };
+template <int KEYS> __device__ __forceinline__ Sides count_sides(const Held<KEYS> &x, uint32_t cut, int shift, int K, int len)
+{
+    Sides n;
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+        const int j = x.first + k;
+        const uint32_t key = x.key[k] >> shift, one = j >= len ? 0 : j < K ? 1 : 1 << 16;
+        n.above += key > cut ? one : 0;
+        n.equal += key == cut ? one : 0;
+    }
+    return n;
+}
+// The same of all slots ahead of this thread's in the workgroup, and in all of it.
+template <int THREADS> __device__ __forceinline__ Sides scan_sides(Pick<THREADS> &s, Sides n, Sides &all)
+{
+    const int wave = threadIdx.x / 64;
+    Sides upto;
+    upto.above = wave_inclusive_sum(n.above);
+    upto.equal = wave_inclusive_sum(n.equal);
+    __syncthreads();
+    if (threadIdx.x % 64 == 63) { s.wave_sum[wave][0] = upto.above; s.wave_sum[wave][1] = upto.equal; }
+    __syncthreads();
+    all = Sides();
+    upto.above -= n.above;
+    upto.equal -= n.equal;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        const uint32_t a = s.wave_sum[w][0], e = s.wave_sum[w][1];
+        if (w < wave) { upto.above += a; upto.equal += e; }
+        all.above += a;
+        all.equal += e;
+    }
+    return upto;
+}
+
+// What lies ahead of a slot in its row: keys above the cut and equal to it below K and beyond.  `need` of the equal keys stay, the lowest
+// slots first.
+struct Ahead {
+    int above_l = 0, equal_l = 0, above_r = 0, equal_r = 0;
+    __device__ __forceinline__ void add(Sides n)
+    {
+        above_l += n.above & 0xffff; equal_l += n.equal & 0xffff;
+        above_r += n.above >> 16; equal_r += n.equal >> 16;
+    }
+    // holes among `slots` slots below K, movers among those beyond
+    __device__ __forceinline__ int holes(int slots, int need) const { return slots - above_l - min(need, equal_l); }
+    __device__ __forceinline__ int movers(int need) const { return above_r + min(max(need - equal_l, 0), equal_r); }
+};
+
+// Writes a thread's part of the lists, and which of its slots stay.
+template <int KEYS, int THREADS> __device__ __forceinline__ void emit(const EvictRow &w, const Held<KEYS> &x, uint32_t cut, int need, const Ahead &ahead, Pick<THREADS> &s)
+{
+    int equals = ahead.equal_l + ahead.equal_r, hole = ahead.holes(min(x.first, w.K), need), mover = ahead.movers(need);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+        const int j = x.first + k;
+        const bool in = j < w.len, low = j < w.K, equal = in && x.key[k] == cut, kept = in && (x.key[k] > cut || (equal && equals < need));
+        equals += equal;
+        if (low && !kept) w.dst[hole++] = j;
+        if (!low && kept) w.src[mover++] = j;
+        bits |= (uint32_t)kept << k;
+    }
+    s.kept[threadIdx.x] = bits;
+}
+
+__device__ __forceinline__ bool nan_among(const float *scores, int from, int to, int threads)
+{
+    int bad = 0;
+    for (int j = from + threadIdx.x; j < to; j += threads) bad |= scores[j] != scores[j];
+    return __syncthreads_or(bad);
+}
+
+// One workgroup per row of up to 1024 KEYS slots, which are read once.
+template <int KEYS> __global__ __launch_bounds__(PICK_THREADS) void evict_pick_kernel(EvictLaunch l)
+{
+    __shared__ Pick<PICK_THREADS> s;
     const specattn_evict_args &e = l.e;
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
-    for (int r = blockIdx.x; r < e.B * e.H; r += gridDim.x) {
-        const int b = r / e.H, h = r - b * e.H, len = row_length(e, b), K = min(len, e.budget);
-        const int64_t row = b * e.row_stride_b + h * e.row_stride_h;
-        const uint32_t *keys = l.keys + (int64_t)r * e.n_max;
-        float *scores = e.scores_out + row;
-        const int32_t *from = e.positions + row;
-        int32_t *to = e.positions_out + row;
-        int32_t *src = e.move_src + r * e.move_stride_row, *dst = e.move_dst + r * e.move_stride_row;
-        if (tid == 0 && h == 0) e.new_lens[b] = K;
-        if (e.row_flags) {
-            int bad = 0;
-            for (int j = tid; j < len; j += PICK_THREADS) bad |= scores[j] != scores[j];
-            bad = __syncthreads_or(bad);
-            if (tid == 0) e.row_flags[r] = bad ? SPECATTN_ROW_INVALID : 0u;
+    const int tid = threadIdx.x;
+    const EvictRow w(e, blockIdx.x);
+    Held<KEYS> x;
+    if (w.len > w.K) x.load(l.keys + (int64_t)w.r * l.stride, 0, w.len);
+    if (tid == 0 && w.h == 0) e.new_lens[w.b] = w.K;
+    if (e.row_flags) {
+        const bool bad = nan_among(w.scores, 0, w.len, PICK_THREADS);
+        if (tid == 0) e.row_flags[w.r] = bad ? SPECATTN_ROW_INVALID : 0u;
+    }
+    if (w.from != w.to) for (int j = tid; j < w.K; j += PICK_THREADS) w.to[j] = w.from[j];
+    if (w.len == w.K) {                                       // nothing leaves
+        if (tid == 0) e.move_counts[w.r] = 0;
+        return;
+    }
+    int bin, above, need = w.K;
+    clear<TOP_BINS>(s);
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) if (x.first + k < w.len) atomicAdd(&s.bins[x.key[k] >> TOP_SHIFT], 1u);
+    locate<TOP_BINS>(s, need, bin, above);
+    uint32_t cut = bin;
+    need -= above;
+    clear<MID_BINS>(s);
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) if (x.first + k < w.len && x.key[k] >> TOP_SHIFT == cut) atomicAdd(&s.bins[x.key[k] >> LOW_BITS & (MID_BINS - 1)], 1u);
+    locate<MID_BINS>(s, need, bin, above);
+    cut = cut << MID_BITS | bin;
+    need -= above;
+    clear<LOW_BINS>(s);
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) if (x.first + k < w.len && x.key[k] >> LOW_BITS == cut) atomicAdd(&s.bins[x.key[k] & (LOW_BINS - 1)], 1u);
+    locate<LOW_BINS>(s, need, bin, above);
+    cut = cut << LOW_BITS | bin;                              // kept: every key above it, and the first `need` that equal it
+    need -= above;
+
+    Sides all;
+    Ahead ahead, row;
+    ahead.add(scan_sides(s, count_sides(x, cut, 0, w.K, w.len), all));
+    row.add(all);
+    emit(w, x, cut, need, ahead, s);
+    const int moves = row.movers(need);
+    if (tid == 0) e.move_counts[w.r] = moves;
+    __syncthreads();
+    for (int i = tid; i < moves; i += PICK_THREADS) {
+        const int a = w.src[i], d = w.dst[i];
+        w.scores[d] = w.scores[a];
+        w.to[d] = w.from[a];
+    }
+    __syncthreads();
+    for (int j = w.K + tid; j < w.len; j += PICK_THREADS) { w.scores[j] = 0.0f; w.to[j] = -1; }
+}
+
+// Rows that are cut into slices, one workgroup each, in four launches: the keys' highest bits are counted; the K-th largest key's bin
+// is located and the slice's keys in it set aside; the K-th largest is found among those of all slices and the lists are written; the
+// rows' own state moves.
+__global__ __launch_bounds__(SLICE_THREADS) void evict_count_kernel(EvictLaunch l)
+{
+    __shared__ Pick<SLICE_THREADS> s;
+    const EvictRow w(l.e, blockIdx.x);
+    const int start = blockIdx.y * SLICE;
+    if (w.len == w.K || start >= w.len) return;
+    Held<SLICE_KEYS> x;
+    x.load(l.keys + (int64_t)w.r * l.stride, start, w.len);
+    clear<TOP_BINS>(s);
+#pragma unroll
+    for (int k = 0; k < SLICE_KEYS; ++k) if (x.first + k < w.len) atomicAdd(&s.bins[x.key[k] >> TOP_SHIFT], 1u);
+    __syncthreads();
+    for (int i = threadIdx.x; i < TOP_BINS; i += SLICE_THREADS) if (s.bins[i]) atomicAdd(&l.hist[(int64_t)w.r * TOP_BINS + i], s.bins[i]);
+}
+
+__global__ __launch_bounds__(SLICE_THREADS) void evict_collect_kernel(EvictLaunch l)
+{
+    __shared__ Pick<SLICE_THREADS> s;
+    const specattn_evict_args &e = l.e;
+    const EvictRow w(e, blockIdx.x);
+    const int tid = threadIdx.x, start = blockIdx.y * SLICE;
+    if (start >= w.len) return;
+    if (e.row_flags && nan_among(w.scores, start, min(start + SLICE, w.len), SLICE_THREADS) && tid == 0) atomicOr(&e.row_flags[w.r], SPECATTN_ROW_INVALID);
+    if (w.len == w.K) return;
+    Held<SLICE_KEYS> x;
+    x.load(l.keys + (int64_t)w.r * l.stride, start, w.len);
+    for (int i = tid; i < TOP_BINS; i += SLICE_THREADS) s.bins[i] = l.hist[(int64_t)w.r * TOP_BINS + i];
+    int bin, above;
+    locate<TOP_BINS>(s, w.K, bin, above);
+    Sides all;
+    const Sides ahead = scan_sides(s, count_sides(x, (uint32_t)bin, TOP_SHIFT, w.K, w.len), all);
+    if (tid < 4) l.info[((int64_t)w.r * l.slices + blockIdx.y) * 4 + tid] = tid == 0 ? all.above & 0xffff : tid == 1 ? all.equal & 0xffff : tid == 2 ? all.above >> 16 : all.equal >> 16;
+    uint32_t *to = l.candidates + (int64_t)w.r * l.stride + start + (ahead.equal & 0xffff) + (ahead.equal >> 16);
+#pragma unroll
+    for (int k = 0; k < SLICE_KEYS; ++k) if (x.first + k < w.len && x.key[k] >> TOP_SHIFT == (uint32_t)bin) *to++ = x.key[k];
+}
+
+__global__ __launch_bounds__(SLICE_THREADS) void evict_emit_kernel(EvictLaunch l)
+{
+    constexpr int WAVES = SLICE_THREADS / 64;
+    __shared__ Pick<SLICE_THREADS> s;
+    __shared__ int info[MAX_SLICES][4];                       // above the bin of the K-th largest and in it; later above and equal to the K-th largest
+    const specattn_evict_args &e = l.e;
+    const EvictRow w(e, blockIdx.x);
+    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, slice = blockIdx.y, start = slice * SLICE, end = min(start + SLICE, w.len);
+    if (tid == 0 && w.h == 0 && slice == 0) e.new_lens[w.b] = w.K;
+    if (w.from != w.to) for (int j = start + tid; j < min(end, w.K); j += SLICE_THREADS) w.to[j] = w.from[j];
+    if (w.len == w.K) {
+        if (tid == 0 && slice == 0) e.move_counts[w.r] = 0;
+        return;
+    }
+    if (start >= w.len) return;
+    const int slices = (w.len + SLICE - 1) / SLICE;
+    Held<SLICE_KEYS> x;
+    x.load(l.keys + (int64_t)w.r * l.stride, start, w.len);
+    for (int i = tid; i < slices * 4; i += SLICE_THREADS) info[i / 4][i % 4] = l.info[(int64_t)w.r * l.slices * 4 + i];
+    for (int i = tid; i < TOP_BINS; i += SLICE_THREADS) s.bins[i] = l.hist[(int64_t)w.r * TOP_BINS + i];
+    int bin, above, need = w.K;
+    locate<TOP_BINS>(s, need, bin, above);
+    uint32_t cut = bin;
+    need -= above;
+    const uint32_t *candidates = l.candidates + (int64_t)w.r * l.stride;
+    // the waves are dealt to the slices
+    const int share = max(WAVES / slices, 1), step = 64 * share;
+    auto each = [&](auto &&f) {
+        if (wave >= share * slices) return;
+        for (int v = wave / share; v < slices; v += WAVES / share) {
+            const int all = info[v][1] + info[v][3];
+#pragma unroll 4
+            for (int i = wave % share * 64; i < all; i += step) f(v, i + lane, i + lane < all, candidates[v * SLICE + min(i + lane, all - 1)]);
         }
-        if (len == K) {                                       // nothing leaves
-            if (tid == 0) e.move_counts[r] = 0;
-            if (from != to) for (int j = tid; j < len; j += PICK_THREADS) to[j] = from[j];
-            continue;
-        }
-        // The K-th largest key: 11, 11 and 10 bits at a time.
-        uint32_t prefix = 0;
-        int need = K;
-#pragma unroll 1
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-            for (int i = tid; i < bins; i += PICK_THREADS) s.bins[i] = 0;
-            __syncthreads();
-            for (int j = tid; j < len; j += PICK_THREADS) {
-                const uint32_t key = keys[j];
-                if (pass == 0 || (key >> (shift + (pass == 2 ? 10 : 11))) == prefix) atomicAdd(&s.bins[(key >> shift) & (bins - 1)], 1u);
-            }
-            int bin, above;
-            locate(s, bins, need, bin, above);
-            prefix = (prefix << (pass == 2 ? 10 : 11)) | (uint32_t)bin;
-            need -= above;
-        }
-        const uint32_t cut = prefix;                          // kept: every key above it, and the first `need` that equal it
-        // Each wave takes a run of the row.
-        const int run = ((len + PICK_WAVES - 1) / PICK_WAVES + 63) & ~63, j0 = min(wave * run, len), j1 = min(j0 + run, len);
-        int above_l = 0, equal_l = 0, above_r = 0, equal_r = 0;
-        for (int j = j0; j < j1; j += 64) {
-            const uint32_t key = j + lane < j1 ? keys[j + lane] : 0;
-            const bool in = j + lane < j1;
-            const uint64_t below = __ballot(j + lane < K), above = __ballot(in && key > cut), equal = __ballot(in && key == cut);
-            above_l += __popcll(above & below);
-            equal_l += __popcll(equal & below);
-            above_r += __popcll(above & ~below);
-            equal_r += __popcll(equal & ~below);
-        }
+    };
+    clear<MID_BINS>(s);
+    each([&](int, int, bool in, uint32_t key) { if (in) atomicAdd(&s.bins[key >> LOW_BITS & (MID_BINS - 1)], 1u); });
+    locate<MID_BINS>(s, need, bin, above);
+    cut = cut << MID_BITS | bin;
+    need -= above;
+    clear<LOW_BINS>(s);
+    each([&](int, int, bool in, uint32_t key) { if (in && key >> LOW_BITS == cut) atomicAdd(&s.bins[key & (LOW_BINS - 1)], 1u); });
+    locate<LOW_BINS>(s, need, bin, above);
+    cut = cut << LOW_BITS | bin;
+    need -= above;
+    // what lies ahead of this slice: of the earlier ones what is above the bin, and their candidates above the cut and equal to it
+    int *ahead = reinterpret_cast<int *>(s.bins);
+    if (tid < 4) ahead[tid] = 0;
+    __syncthreads();
+    each([&](int v, int i, bool in, uint32_t key) {
+        if (v >= slice) return;
+        const uint64_t low = __ballot(i < info[v][1]), over = __ballot(in && key > cut), equal = __ballot(in && key == cut);
         if (lane == 0) {
-            s.wave_sum[wave][0] = above_l; s.wave_sum[wave][1] = equal_l;
-            s.wave_sum[wave][2] = above_r; s.wave_sum[wave][3] = equal_r;
+            if (over & low) atomicAdd(&ahead[0], __popcll(over & low));
+            if (equal & low) atomicAdd(&ahead[1], __popcll(equal & low));
+            if (over & ~low) atomicAdd(&ahead[2], __popcll(over & ~low));
+            if (equal & ~low) atomicAdd(&ahead[3], __popcll(equal & ~low));
         }
-        __syncthreads();
-        int equals = 0, hole = 0, mover = 0, all_movers = 0;  // ahead of this wave's run; of the row
-        int my_equals = 0, my_hole = 0, my_mover = 0;
-        for (int w = 0; w < PICK_WAVES; ++w) {
-            if (w == wave) { my_equals = equals; my_hole = hole; my_mover = all_movers; }
-            const int w0 = min(w * run, len), w1 = min(w0 + run, len);
-            const int ties_l = min(max(need - equals, 0), s.wave_sum[w][1]);
-            const int ties_r = min(max(need - equals - s.wave_sum[w][1], 0), s.wave_sum[w][3]);
-            hole += max(min(w1, K) - w0, 0) - s.wave_sum[w][0] - ties_l;
-            all_movers += s.wave_sum[w][2] + ties_r;
-            equals += s.wave_sum[w][1] + s.wave_sum[w][3];
-        }
-        equals = my_equals; hole = my_hole; mover = my_mover;
-        const uint64_t before = ((uint64_t)1 << lane) - 1;
-        for (int j = j0; j < j1; j += 64) {
-            const bool in = j + lane < j1;
-            const uint32_t key = in ? keys[j + lane] : 0;
-            const uint64_t equal = __ballot(in && key == cut);
-            const bool kept = in && (key > cut || (key == cut && equals + __popcll(equal & before) < need));
-            const bool low = j + lane < K;
-            const uint64_t holes = __ballot(in && low && !kept), movers = __ballot(in && !low && kept);
-            if (in && low && !kept) dst[hole + __popcll(holes & before)] = j + lane;
-            if (in && !low && kept) src[mover + __popcll(movers & before)] = j + lane;
-            if (kept && low && from != to) to[j + lane] = from[j + lane];
-            hole += __popcll(holes);
-            mover += __popcll(movers);
-            equals += __popcll(equal);
-        }
-        if (tid == 0) e.move_counts[r] = all_movers;
-        __syncthreads();
-        for (int i = tid; i < all_movers; i += PICK_THREADS) {
-            const int a = src[i], d = dst[i];
-            scores[d] = scores[a];
-            to[d] = from[a];
-        }
-        __syncthreads();
-        for (int j = K + tid; j < len; j += PICK_THREADS) { scores[j] = 0.0f; to[j] = -1; }
-        __syncthreads();                                      // (the bins are used again)
+    });
+    for (int v = tid; v < slice; v += SLICE_THREADS) {
+        atomicAdd(&ahead[0], info[v][0]);
+        atomicAdd(&ahead[2], info[v][2]);
+    }
+    __syncthreads();
+    Ahead mine;
+    mine.above_l = ahead[0]; mine.equal_l = ahead[1]; mine.above_r = ahead[2]; mine.equal_r = ahead[3];
+    Ahead upto = mine;
+    Sides all;
+    mine.add(scan_sides(s, count_sides(x, cut, 0, w.K, w.len), all));
+    upto.add(all);
+    emit(w, x, cut, need, mine, s);
+    if (slice == slices - 1 && tid == 0) e.move_counts[w.r] = upto.movers(need);
+    __syncthreads();
+    for (int j = max(start, w.K) + tid; j < end; j += SLICE_THREADS)
+        if (!(s.kept[(j - start) / SLICE_KEYS] >> (j - start) % SLICE_KEYS & 1)) { w.scores[j] = 0.0f; w.to[j] = -1; }
+}
+
+__global__ __launch_bounds__(256) void evict_state_kernel(EvictLaunch l)
+{
+    const EvictRow w(l.e, blockIdx.x);
+    const int n = l.e.move_counts[w.r];
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < n; i += gridDim.y * 256) {
+        const int a = w.src[i], d = w.dst[i];
+        w.scores[d] = w.scores[a];
+        w.to[d] = w.from[a];
+        w.scores[a] = 0.0f;
+        w.to[a] = -1;
     }
 }
 
@@ -206,7 +426,7 @@ struct MoveLaunch {
     FastDivisor per_row[SPECATTN_MAX_PLANES];                 // by the units of a row
 };
 
-constexpr int MOVE_THREADS = 256, MOVE_ITEMS = 4;
+constexpr int MOVE_THREADS = 256, MOVE_FLIGHT = 8;           // requests of a lane under way
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -221,31 +441,36 @@ __device__ __forceinline__ bool move_offset(const MoveLaunch &l, const specattn_
     return page >= 0 && page < p.num_pages;
 }
 
+// A wave takes 64 moves of one head: their slots and pages are looked up once, a lane each, then the lanes go through the rows' units together.
 template <typename V> __device__ __forceinline__ void move_rows(const MoveLaunch &l, const specattn_move_plane &p, const FastDivisor &per_row, int units)
 {
-    const int share = p.H_kv / l.m.H, all = l.m.B * p.H_kv;
+    const int share = p.H_kv / l.m.H, all = l.m.B * p.H_kv, lane = threadIdx.x % 64;
+    const int first = __builtin_amdgcn_readfirstlane(blockIdx.x * MOVE_THREADS + threadIdx.x / 64 * 64);
     uint8_t *data = static_cast<uint8_t *>(p.data);
     for (int y = blockIdx.y; y < all; y += gridDim.y) {
         const int b = y / p.H_kv, kv = y - b * p.H_kv, r = b * l.m.H + kv / share;
-        const int items = min(max(l.m.move_counts[r], 0), l.m.move_capacity) * units;
-        const int first = blockIdx.x * MOVE_THREADS * MOVE_ITEMS + threadIdx.x;
-        if (first >= items) continue;
-        V value[MOVE_ITEMS];
-        int64_t from, to[MOVE_ITEMS];
-        bool there[MOVE_ITEMS];
-#pragma unroll
-        for (int k = 0; k < MOVE_ITEMS; ++k) {
-            const int item = first + k * MOVE_THREADS;
-            there[k] = false;
-            if (item >= items) continue;
-            const int i = per_row.divide(item), u = item - i * units;
-            const int64_t list = r * l.m.move_stride_row + i;
-            there[k] = move_offset(l, p, b, kv, l.m.move_src[list], from) && move_offset(l, p, b, kv, l.m.move_dst[list], to[k]);
-            to[k] += u * (int)sizeof(V);
-            if (there[k]) value[k] = __builtin_nontemporal_load(reinterpret_cast<const V *>(data + from + u * (int)sizeof(V)));
+        const int moves = min(min(max(l.m.move_counts[r], 0), l.m.move_capacity) - first, 64);
+        if (moves <= 0) continue;
+        int64_t from = -1, to = -1;
+        if (lane < moves) {
+            const int64_t list = r * l.m.move_stride_row + first + lane;
+            const int src = l.m.move_src[list], dst = l.m.move_dst[list];
+            if (!move_offset(l, p, b, kv, src, from) || !move_offset(l, p, b, kv, dst, to)) from = -1;
         }
+        const int items = moves * units;
+        for (int i0 = 0; i0 < items; i0 += 64 * MOVE_FLIGHT) {
+            V value[MOVE_FLIGHT];
+            int64_t at[MOVE_FLIGHT];
 #pragma unroll
-        for (int k = 0; k < MOVE_ITEMS; ++k) if (there[k]) *reinterpret_cast<V *>(data + to[k]) = value[k];
+            for (int k = 0; k < MOVE_FLIGHT; ++k) {
+                const int item = min(i0 + 64 * k + lane, items - 1), m = per_row.divide(item), u = (item - m * units) * (int)sizeof(V);
+                const int64_t f = __shfl(from, m, 64), t = __shfl(to, m, 64);
+                at[k] = i0 + 64 * k + lane < items && f >= 0 ? t + u : -1;
+                if (f >= 0) value[k] = __builtin_nontemporal_load(reinterpret_cast<const V *>(data + f + u));
+            }
+#pragma unroll
+            for (int k = 0; k < MOVE_FLIGHT; ++k) if (at[k] >= 0) *reinterpret_cast<V *>(data + at[k]) = value[k];
+        }
     }
 }
 
@@ -261,23 +486,55 @@ __global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(MoveLaunch l)
 
 }  // namespace
 
+static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Rows that one workgroup cannot hold are cut up, and so are longer ones that leave most of the GPU idle.
+static int evict_slices(const specattn_evict_args *e)
+{
+    const int rows = e->B * e->H;
+    return e->n_max <= 8 * PICK_THREADS || (e->n_max <= 32 * PICK_THREADS && rows > 64) ? 0 : (e->n_max + SLICE - 1) / SLICE;
+}
+
+static int evict_stride(const specattn_evict_args *e) { return (e->n_max + 31) & ~31; }
+
 size_t evict_workspace_bytes(const specattn_evict_args *e)
 {
-    return ((size_t)e->B * e->H * e->n_max * sizeof(uint32_t) + 255) & ~(size_t)255;
+    const size_t rows = (size_t)e->B * e->H, keys = align256(rows * evict_stride(e) * sizeof(uint32_t)), slices = evict_slices(e);
+    return slices ? 2 * keys + align256(rows * TOP_BINS * sizeof(uint32_t)) + align256(rows * slices * 4 * sizeof(int32_t)) : keys;
 }
 
 specattn_status launch_evict_select(const specattn_evict_args *e, void *workspace, hipStream_t stream)
 {
     EvictLaunch l;
     l.e = *e;
-    l.keys = static_cast<uint32_t *>(workspace);
     l.members = e->probs ? e->H_draft / e->H * e->S : 0;
+    l.slices = evict_slices(e);
     const int rows = e->B * e->H;
+    char *ws = static_cast<char *>(workspace);
+    l.stride = evict_stride(e);
+    const size_t keys = align256((size_t)rows * l.stride * sizeof(uint32_t));
+    l.keys = reinterpret_cast<uint32_t *>(ws);
+    l.candidates = reinterpret_cast<uint32_t *>(ws + keys);
+    l.hist = reinterpret_cast<uint32_t *>(ws + 2 * keys);
+    l.info = reinterpret_cast<int32_t *>(ws + 2 * keys + align256((size_t)rows * TOP_BINS * sizeof(uint32_t)));
     evict_add_kernel<<<dim3((e->n_max + ADD_THREADS * ADD_SLOTS - 1) / (ADD_THREADS * ADD_SLOTS), std::min(rows, 65535)), ADD_THREADS, 0, stream>>>(l);
-    const specattn_status st = check_launch("evict_add_kernel");
+    specattn_status st = check_launch("evict_add_kernel");
     if (st != SPECATTN_OK) return st;
-    evict_pick_kernel<<<rows, PICK_THREADS, 0, stream>>>(l);
-    return check_launch("evict_pick_kernel");
+    if (l.slices == 0) {
+        if (e->n_max <= 8 * PICK_THREADS) evict_pick_kernel<8><<<rows, PICK_THREADS, 0, stream>>>(l);
+        else if (e->n_max <= 16 * PICK_THREADS) evict_pick_kernel<16><<<rows, PICK_THREADS, 0, stream>>>(l);
+        else evict_pick_kernel<32><<<rows, PICK_THREADS, 0, stream>>>(l);
+        return check_launch("evict_pick_kernel");
+    }
+    const dim3 grid(rows, l.slices);
+    evict_count_kernel<<<grid, SLICE_THREADS, 0, stream>>>(l);
+    if ((st = check_launch("evict_count_kernel")) != SPECATTN_OK) return st;
+    evict_collect_kernel<<<grid, SLICE_THREADS, 0, stream>>>(l);
+    if ((st = check_launch("evict_collect_kernel")) != SPECATTN_OK) return st;
+    evict_emit_kernel<<<grid, SLICE_THREADS, 0, stream>>>(l);
+    if ((st = check_launch("evict_emit_kernel")) != SPECATTN_OK) return st;
+    evict_state_kernel<<<dim3(rows, std::min((e->move_capacity + 1023) / 1024, 64)), 256, 0, stream>>>(l);
+    return check_launch("evict_state_kernel");
 }
 
 specattn_status launch_evict_move(const specattn_move_args *m, hipStream_t stream)
@@ -286,17 +543,14 @@ specattn_status launch_evict_move(const specattn_move_args *m, hipStream_t strea
     l.m = *m;
     l.page_shift = 0;
     while (m->page_table && (1 << l.page_shift) < m->page_size) ++l.page_shift;
-    int64_t most = 0;
     int rows = 0;
     for (int z = 0; z < m->num_planes; ++z) {
         const int bytes = m->planes[z].row_bytes;
         l.unit_shift[z] = bytes % 16 == 0 ? 4 : bytes % 8 == 0 ? 3 : 2;
         l.per_row[z] = FastDivisor(bytes >> l.unit_shift[z]);
-        most = std::max(most, (int64_t)m->move_capacity * (bytes >> l.unit_shift[z]));
         rows = std::max(rows, m->B * m->planes[z].H_kv);
     }
-    const int per = MOVE_THREADS * MOVE_ITEMS;
-    evict_move_kernel<<<dim3((int)((most + per - 1) / per), std::min(rows, 65535), m->num_planes), MOVE_THREADS, 0, stream>>>(l);
+    evict_move_kernel<<<dim3((m->move_capacity + MOVE_THREADS - 1) / MOVE_THREADS, std::min(rows, 65535), m->num_planes), MOVE_THREADS, 0, stream>>>(l);
     return check_launch("evict_move_kernel");
 }
 

@@ -169,3 +169,23 @@ def test_moves_that_lead_outside_are_left_out():
     plane.copy_(before.view(4, 1, 16, 4))
     sa.specattn_evict_move(sa.move_args(src, dst, count, [plane], B=1, page_table=table, n_max=n))
     assert torch.equal(plane.view(n, 4), before)
+
+
+@pytest.mark.parametrize("B,H,n,budget", [(3, 1, 33000, 20000), (2, 1, 70001, 69990), (1, 2, 100000, 3), (65, 1, 9000, 8000), (2, 40, 20000, 1000)])
+def test_long_rows(B, H, n, budget):
+    """Rows that one workgroup holds and rows that are cut up, on both sides of the lines between them; ties across the cuts."""
+    rng = np.random.default_rng(n)
+    scores = np.round(rng.random((B, H, n), dtype=np.float32) * 3000) / 64
+    positions = np.broadcast_to(np.arange(n, dtype=np.int32), (B, H, n)).copy()
+    lens = np.maximum(0, n - np.arange(B) * (n // 3 + 11))
+    probs = (np.round(rng.random((B, H, 1, n), dtype=np.float32) * 4) / 64).astype(np.float32)
+    _check(scores, positions, lens, np.full(B, n), budget, probs=probs, sinks=min(2, budget), recent=min(40, budget - min(2, budget)))
+
+
+@pytest.mark.parametrize("value", [0.0, 1.5])
+def test_one_value_throughout_a_long_row(value):
+    n = 50000
+    scores, positions = np.full((1, 1, n), value, dtype=np.float32), np.arange(n, dtype=np.int32).reshape(1, 1, n)
+    scores[0, 0, 40000] = np.nan
+    _check(scores, positions, np.array([n]), np.array([n]), 20000, sinks=4, recent=64)
+    _check(scores, positions, np.array([n]), np.array([n]), 20000, in_place=False)
