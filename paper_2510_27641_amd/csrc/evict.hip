@@ -20,6 +20,9 @@ constexpr int MAX_SLICES = SPECATTN_MAX_N / SLICE;
 // added one after the other, took most of it.
 constexpr int TOP_BITS = 12, MID_BITS = 10, LOW_BITS = 10;
 constexpr int TOP_BINS = 1 << TOP_BITS, MID_BINS = 1 << MID_BITS, LOW_BINS = 1 << LOW_BITS, TOP_SHIFT = 32 - TOP_BITS;
+// Bytes of a row that its selecting workgroup adds up itself: a launch less, but one CU takes 16 KiB per us (64 rows of 8197 slots,
+// five entries each: 20 us in two launches, 32 in one).
+constexpr int64_t ADD_ITSELF = 32 << 10;
 constexpr uint32_t KEY_STAYS = 0xffffffffu, KEY_NAN = 0;
 
 struct EvictLaunch {
@@ -46,41 +49,64 @@ __device__ __forceinline__ uint32_t key_of(float score)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(ADD_THREADS) void evict_add_kernel(EvictLaunch l)
+// New scores and keys of slots first, first + GAP, ... of row r; WIDTH neighbouring slots at each place.
+template <int PLACES, int WIDTH, int GAP> __device__ __forceinline__ void add_slots(const EvictLaunch &l, int r, int b, int h, int len, int first)
 {
+    typedef float Wide __attribute__((ext_vector_type(WIDTH)));
     const specattn_evict_args &e = l.e;
-    for (int r = blockIdx.y; r < e.B * e.H; r += gridDim.y) {
-        const int b = r / e.H, h = r - b * e.H, len = row_length(e, b);
-        const int first = blockIdx.x * ADD_THREADS * ADD_SLOTS + threadIdx.x;
-        const int64_t row = b * e.row_stride_b + h * e.row_stride_h;
-        if (l.slices && blockIdx.x == 0) {                    // (the launches behind this one add to these)
-            for (int i = threadIdx.x; i < TOP_BINS; i += ADD_THREADS) l.hist[(int64_t)r * TOP_BINS + i] = 0;
-            if (e.row_flags && threadIdx.x == 0) e.row_flags[r] = 0;
-        }
-        const int next = e.next_positions[b];
-        double sum[ADD_SLOTS];
-        int at[ADD_SLOTS];
+    if (first >= len) return;
+    const int64_t row = b * e.row_stride_b + h * e.row_stride_h;
+    const int next = e.next_positions[b];
+    double sum[PLACES][WIDTH];
+    int at[PLACES];
+    // (behind the row: its last place again, not written; with WIDTH > 1 rows are padded to whole places)
 #pragma unroll
-        for (int k = 0; k < ADD_SLOTS; ++k) {
-            at[k] = min(first + k * ADD_THREADS, len - 1);    // (behind the row: its last slot again, not written)
-            sum[k] = len > 0 ? e.decay * (double)e.scores[row + at[k]] : 0.0;
-        }
-        if (first >= len) continue;
-        const float *probs = e.probs + b * e.probs_stride_b + (int64_t)h * l.members * e.probs_stride_row;
-#pragma unroll 4
-        for (int m = 0; m < l.members; ++m)
+    for (int k = 0; k < PLACES; ++k) {
+        at[k] = min(first + k * GAP, (len - 1) / WIDTH * WIDTH);
+        const Wide x = *reinterpret_cast<const Wide *>(e.scores + row + at[k]);
 #pragma unroll
-            for (int k = 0; k < ADD_SLOTS; ++k) sum[k] += (double)__builtin_nontemporal_load(probs + m * e.probs_stride_row + at[k]);
+        for (int i = 0; i < WIDTH; ++i) sum[k][i] = e.decay * (double)x[i];
+    }
+    const float *probs = e.probs + b * e.probs_stride_b + (int64_t)h * l.members * e.probs_stride_row;
+    constexpr int TRIP = 4;                                   // rows requested together
+    for (int m0 = 0; m0 < l.members; m0 += TRIP) {
+        Wide x[TRIP][PLACES];
 #pragma unroll
-        for (int k = 0; k < ADD_SLOTS; ++k) {
-            const int j = first + k * ADD_THREADS;
+        for (int t = 0; t < TRIP; ++t)                        // (behind the last row: that one again, not added)
+#pragma unroll
+            for (int k = 0; k < PLACES; ++k) x[t][k] = __builtin_nontemporal_load(reinterpret_cast<const Wide *>(probs + min(m0 + t, l.members - 1) * e.probs_stride_row + at[k]));
+#pragma unroll
+        for (int t = 0; t < TRIP; ++t)
+#pragma unroll
+            for (int k = 0; k < PLACES; ++k)
+#pragma unroll
+                for (int i = 0; i < WIDTH; ++i) sum[k][i] += m0 + t < l.members ? (double)x[t][k][i] : 0.0;
+    }
+#pragma unroll
+    for (int k = 0; k < PLACES; ++k)
+#pragma unroll
+        for (int i = 0; i < WIDTH; ++i) {
+            const int j = first + k * GAP + i;
             if (j >= len) continue;
-            const float score = (float)sum[k];
+            const float score = (float)sum[k][i];
             const int64_t place = e.positions[row + j];
             const bool stays = place < e.sinks || place >= (int64_t)next - e.recent;
             e.scores_out[row + j] = score;
             l.keys[(int64_t)r * l.stride + j] = stays ? KEY_STAYS : key_of(score);
         }
+}
+
+// WIDTH 4 where rows start and lie at whole 16 bytes.
+template <int WIDTH> __global__ __launch_bounds__(ADD_THREADS) void evict_add_kernel(EvictLaunch l)
+{
+    const specattn_evict_args &e = l.e;
+    for (int r = blockIdx.y; r < e.B * e.H; r += gridDim.y) {
+        const int b = r / e.H, h = r - b * e.H, len = row_length(e, b);
+        if (l.slices && blockIdx.x == 0) {                    // (the launches behind this one add to these)
+            for (int i = threadIdx.x; i < TOP_BINS; i += ADD_THREADS) l.hist[(int64_t)r * TOP_BINS + i] = 0;
+            if (e.row_flags && threadIdx.x == 0) e.row_flags[r] = 0;
+        }
+        add_slots<ADD_SLOTS / WIDTH, WIDTH, ADD_THREADS * WIDTH>(l, r, b, h, len, blockIdx.x * ADD_THREADS * ADD_SLOTS + threadIdx.x * WIDTH);
     }
 }
 
@@ -226,6 +252,18 @@ template <int KEYS, int THREADS> __device__ __forceinline__ void emit(const Evic
     s.kept[threadIdx.x] = bits;
 }
 
+// to[j] = from[j] for begin <= j < end, eight requests of a thread at a time
+template <int THREADS> __device__ __forceinline__ void copy_range(int32_t *to, const int32_t *from, int begin, int end)
+{
+    for (int j0 = begin + threadIdx.x; j0 < end; j0 += 8 * THREADS) {
+        int32_t v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = from[min(j0 + k * THREADS, end - 1)];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (j0 + k * THREADS < end) to[j0 + k * THREADS] = v[k];
+    }
+}
+
 __device__ __forceinline__ bool nan_among(const float *scores, int from, int to, int threads)
 {
     int bad = 0;
@@ -233,13 +271,18 @@ __device__ __forceinline__ bool nan_among(const float *scores, int from, int to,
     return __syncthreads_or(bad);
 }
 
-// One workgroup per row of up to 1024 KEYS slots, which are read once.
-template <int KEYS> __global__ __launch_bounds__(PICK_THREADS) void evict_pick_kernel(EvictLaunch l)
+// One workgroup per row of up to 1024 KEYS slots, which are read once; with ADD it adds them up itself.
+template <int KEYS, bool ADD> __global__ __launch_bounds__(PICK_THREADS) void evict_pick_kernel(EvictLaunch l)
 {
     __shared__ Pick<PICK_THREADS> s;
     const specattn_evict_args &e = l.e;
     const int tid = threadIdx.x;
     const EvictRow w(e, blockIdx.x);
+    if constexpr (ADD) {
+        constexpr int PART = KEYS < 8 ? KEYS : 8;             // (as many sums at a time as the registers hold)
+        for (int k = 0; k < KEYS; k += PART) add_slots<PART, 1, PICK_THREADS>(l, w.r, w.b, w.h, w.len, k * PICK_THREADS + tid);
+        __syncthreads();                                      // (the keys are read back by other threads)
+    }
     Held<KEYS> x;
     if (w.len > w.K) x.load(l.keys + (int64_t)w.r * l.stride, 0, w.len);
     if (tid == 0 && w.h == 0) e.new_lens[w.b] = w.K;
@@ -247,7 +290,7 @@ template <int KEYS> __global__ __launch_bounds__(PICK_THREADS) void evict_pick_k
         const bool bad = nan_among(w.scores, 0, w.len, PICK_THREADS);
         if (tid == 0) e.row_flags[w.r] = bad ? SPECATTN_ROW_INVALID : 0u;
     }
-    if (w.from != w.to) for (int j = tid; j < w.K; j += PICK_THREADS) w.to[j] = w.from[j];
+    if (w.from != w.to) copy_range<PICK_THREADS>(w.to, w.from, 0, w.K);
     if (w.len == w.K) {                                       // nothing leaves
         if (tid == 0) e.move_counts[w.r] = 0;
         return;
@@ -331,76 +374,96 @@ __global__ __launch_bounds__(SLICE_THREADS) void evict_collect_kernel(EvictLaunc
 
 __global__ __launch_bounds__(SLICE_THREADS) void evict_emit_kernel(EvictLaunch l)
 {
-    constexpr int WAVES = SLICE_THREADS / 64;
+    constexpr int STAGED = 8192;                              // candidates of a row that are looked at in shared memory
     __shared__ Pick<SLICE_THREADS> s;
-    __shared__ int info[MAX_SLICES][4];                       // above the bin of the K-th largest and in it; later above and equal to the K-th largest
+    __shared__ int first[MAX_SLICES + 1];                     // of each slice's candidates among the row's
+    __shared__ int ahead[5];                                  // of this slice: above the cut and equal to it below K and beyond; candidates below K
+    __shared__ uint32_t staged[STAGED];
     const specattn_evict_args &e = l.e;
     const EvictRow w(e, blockIdx.x);
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, slice = blockIdx.y, start = slice * SLICE, end = min(start + SLICE, w.len);
+    const int tid = threadIdx.x, slice = blockIdx.y, start = slice * SLICE, end = min(start + SLICE, w.len);
     if (tid == 0 && w.h == 0 && slice == 0) e.new_lens[w.b] = w.K;
-    if (w.from != w.to) for (int j = start + tid; j < min(end, w.K); j += SLICE_THREADS) w.to[j] = w.from[j];
     if (w.len == w.K) {
+        if (w.from != w.to) copy_range<SLICE_THREADS>(w.to, w.from, start, end);
         if (tid == 0 && slice == 0) e.move_counts[w.r] = 0;
         return;
     }
     if (start >= w.len) return;
     const int slices = (w.len + SLICE - 1) / SLICE;
+    const uint32_t *candidates = l.candidates + (int64_t)w.r * l.stride;
     Held<SLICE_KEYS> x;
     x.load(l.keys + (int64_t)w.r * l.stride, start, w.len);
-    for (int i = tid; i < slices * 4; i += SLICE_THREADS) info[i / 4][i % 4] = l.info[(int64_t)w.r * l.slices * 4 + i];
     for (int i = tid; i < TOP_BINS; i += SLICE_THREADS) s.bins[i] = l.hist[(int64_t)w.r * TOP_BINS + i];
+    if (tid < 5) ahead[tid] = 0;
+    __syncthreads();
+    if (tid < 64) {
+        int base = 0;
+        for (int v0 = 0; v0 < slices; v0 += 64) {
+            const int v = v0 + tid;
+            int4 n = {0, 0, 0, 0};
+            if (v < slices) n = *reinterpret_cast<const int4 *>(l.info + ((int64_t)w.r * l.slices + v) * 4);
+            const int upto = base + wave_inclusive_sum(n.y + n.w);
+            if (v < slices) first[v + 1] = upto;
+            if (v < slice) { atomicAdd(&ahead[0], n.x); atomicAdd(&ahead[2], n.z); }
+            if (n.y) atomicAdd(&ahead[4], n.y);
+            base = wave_last(upto);
+        }
+        if (tid == 0) first[0] = 0;
+    }
     int bin, above, need = w.K;
     locate<TOP_BINS>(s, need, bin, above);
     uint32_t cut = bin;
     need -= above;
-    const uint32_t *candidates = l.candidates + (int64_t)w.r * l.stride;
-    // the waves are dealt to the slices
-    const int share = max(WAVES / slices, 1), step = 64 * share;
-    auto each = [&](auto &&f) {
-        if (wave >= share * slices) return;
-        for (int v = wave / share; v < slices; v += WAVES / share) {
-            const int all = info[v][1] + info[v][3];
-#pragma unroll 4
-            for (int i = wave % share * 64; i < all; i += step) f(v, i + lane, i + lane < all, candidates[v * SLICE + min(i + lane, all - 1)]);
+    const int all = first[slices], below = ahead[4], mine = first[slice];
+    auto from_memory = [&](int i) {                           // candidate i of the row
+        int lo = 0, hi = slices;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (first[mid] <= i) lo = mid; else hi = mid;
         }
+        return candidates[lo * SLICE + i - first[lo]];
+    };
+    const bool few = all <= STAGED;
+    if (few)
+#pragma unroll 4
+        for (int i = tid; i < all; i += SLICE_THREADS) staged[i] = from_memory(i);
+    auto each = [&](int n, auto &&f) {
+        if (few) for (int i = tid; i < n; i += SLICE_THREADS) f(i, staged[i]);
+        else
+#pragma unroll 4
+            for (int i = tid; i < n; i += SLICE_THREADS) f(i, from_memory(i));
     };
     clear<MID_BINS>(s);
-    each([&](int, int, bool in, uint32_t key) { if (in) atomicAdd(&s.bins[key >> LOW_BITS & (MID_BINS - 1)], 1u); });
+    each(all, [&](int, uint32_t key) { atomicAdd(&s.bins[key >> LOW_BITS & (MID_BINS - 1)], 1u); });
     locate<MID_BINS>(s, need, bin, above);
     cut = cut << MID_BITS | bin;
     need -= above;
     clear<LOW_BINS>(s);
-    each([&](int, int, bool in, uint32_t key) { if (in && key >> LOW_BITS == cut) atomicAdd(&s.bins[key & (LOW_BINS - 1)], 1u); });
+    each(all, [&](int, uint32_t key) { if (key >> LOW_BITS == cut) atomicAdd(&s.bins[key & (LOW_BINS - 1)], 1u); });
     locate<LOW_BINS>(s, need, bin, above);
     cut = cut << LOW_BITS | bin;
     need -= above;
-    // what lies ahead of this slice: of the earlier ones what is above the bin, and their candidates above the cut and equal to it
-    int *ahead = reinterpret_cast<int *>(s.bins);
-    if (tid < 4) ahead[tid] = 0;
-    __syncthreads();
-    each([&](int v, int i, bool in, uint32_t key) {
-        if (v >= slice) return;
-        const uint64_t low = __ballot(i < info[v][1]), over = __ballot(in && key > cut), equal = __ballot(in && key == cut);
-        if (lane == 0) {
-            if (over & low) atomicAdd(&ahead[0], __popcll(over & low));
-            if (equal & low) atomicAdd(&ahead[1], __popcll(equal & low));
-            if (over & ~low) atomicAdd(&ahead[2], __popcll(over & ~low));
-            if (equal & ~low) atomicAdd(&ahead[3], __popcll(equal & ~low));
-        }
+    // (candidates below K come first, as slots do)
+    int n[4] = {0, 0, 0, 0};
+    each(mine, [&](int i, uint32_t key) {
+        n[0] += i < below && key > cut; n[1] += i < below && key == cut;
+        n[2] += i >= below && key > cut; n[3] += i >= below && key == cut;
     });
-    for (int v = tid; v < slice; v += SLICE_THREADS) {
-        atomicAdd(&ahead[0], info[v][0]);
-        atomicAdd(&ahead[2], info[v][2]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int sum = wave_last(wave_inclusive_sum(n[k]));
+        if (tid % 64 == 0 && sum) atomicAdd(&ahead[k], sum);
     }
     __syncthreads();
-    Ahead mine;
-    mine.above_l = ahead[0]; mine.equal_l = ahead[1]; mine.above_r = ahead[2]; mine.equal_r = ahead[3];
-    Ahead upto = mine;
-    Sides all;
-    mine.add(scan_sides(s, count_sides(x, cut, 0, w.K, w.len), all));
-    upto.add(all);
-    emit(w, x, cut, need, mine, s);
+    Ahead at;
+    at.above_l = ahead[0]; at.equal_l = ahead[1]; at.above_r = ahead[2]; at.equal_r = ahead[3];
+    Ahead upto = at;
+    Sides sides;
+    at.add(scan_sides(s, count_sides(x, cut, 0, w.K, w.len), sides));
+    upto.add(sides);
+    emit(w, x, cut, need, at, s);
     if (slice == slices - 1 && tid == 0) e.move_counts[w.r] = upto.movers(need);
+    if (w.from != w.to) copy_range<SLICE_THREADS>(w.to, w.from, start, min(end, w.K));
     __syncthreads();
     for (int j = max(start, w.K) + tid; j < end; j += SLICE_THREADS)
         if (!(s.kept[(j - start) / SLICE_KEYS] >> (j - start) % SLICE_KEYS & 1)) { w.scores[j] = 0.0f; w.to[j] = -1; }
@@ -492,7 +555,7 @@ static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 static int evict_slices(const specattn_evict_args *e)
 {
     const int rows = e->B * e->H;
-    return e->n_max <= 8 * PICK_THREADS || (e->n_max <= 32 * PICK_THREADS && rows > 64) ? 0 : (e->n_max + SLICE - 1) / SLICE;
+    return e->n_max <= 16 * PICK_THREADS || (e->n_max <= 32 * PICK_THREADS && rows > 64) ? 0 : (e->n_max + SLICE - 1) / SLICE;
 }
 
 static int evict_stride(const specattn_evict_args *e) { return (e->n_max + 31) & ~31; }
@@ -517,13 +580,21 @@ specattn_status launch_evict_select(const specattn_evict_args *e, void *workspac
     l.candidates = reinterpret_cast<uint32_t *>(ws + keys);
     l.hist = reinterpret_cast<uint32_t *>(ws + 2 * keys);
     l.info = reinterpret_cast<int32_t *>(ws + 2 * keys + align256((size_t)rows * TOP_BINS * sizeof(uint32_t)));
-    evict_add_kernel<<<dim3((e->n_max + ADD_THREADS * ADD_SLOTS - 1) / (ADD_THREADS * ADD_SLOTS), std::min(rows, 65535)), ADD_THREADS, 0, stream>>>(l);
-    specattn_status st = check_launch("evict_add_kernel");
-    if (st != SPECATTN_OK) return st;
+    specattn_status st;
+    // A workgroup that holds its row also adds it up where that is little to read: a launch less.
+    const bool small = l.slices == 0 && (int64_t)e->n_max * (l.members + 2) * (int64_t)sizeof(float) <= ADD_ITSELF;
+    if (!small) {
+        const int64_t elements = (l.members ? e->probs_stride_b | e->probs_stride_row : 0) | e->row_stride_b | e->row_stride_h | e->n_max;
+        const bool wide = elements % 4 == 0 && (reinterpret_cast<uintptr_t>(e->probs) | reinterpret_cast<uintptr_t>(e->scores)) % 16 == 0;
+        const dim3 grid((e->n_max + ADD_THREADS * ADD_SLOTS - 1) / (ADD_THREADS * ADD_SLOTS), std::min(rows, 65535));
+        if (wide) evict_add_kernel<4><<<grid, ADD_THREADS, 0, stream>>>(l);
+        else evict_add_kernel<1><<<grid, ADD_THREADS, 0, stream>>>(l);
+        if ((st = check_launch("evict_add_kernel")) != SPECATTN_OK) return st;
+    }
     if (l.slices == 0) {
-        if (e->n_max <= 8 * PICK_THREADS) evict_pick_kernel<8><<<rows, PICK_THREADS, 0, stream>>>(l);
-        else if (e->n_max <= 16 * PICK_THREADS) evict_pick_kernel<16><<<rows, PICK_THREADS, 0, stream>>>(l);
-        else evict_pick_kernel<32><<<rows, PICK_THREADS, 0, stream>>>(l);
+        if (e->n_max <= 8 * PICK_THREADS) small ? evict_pick_kernel<8, true><<<rows, PICK_THREADS, 0, stream>>>(l) : evict_pick_kernel<8, false><<<rows, PICK_THREADS, 0, stream>>>(l);
+        else if (e->n_max <= 16 * PICK_THREADS) small ? evict_pick_kernel<16, true><<<rows, PICK_THREADS, 0, stream>>>(l) : evict_pick_kernel<16, false><<<rows, PICK_THREADS, 0, stream>>>(l);
+        else small ? evict_pick_kernel<32, true><<<rows, PICK_THREADS, 0, stream>>>(l) : evict_pick_kernel<32, false><<<rows, PICK_THREADS, 0, stream>>>(l);
         return check_launch("evict_pick_kernel");
     }
     const dim3 grid(rows, l.slices);
@@ -533,7 +604,7 @@ specattn_status launch_evict_select(const specattn_evict_args *e, void *workspac
     if ((st = check_launch("evict_collect_kernel")) != SPECATTN_OK) return st;
     evict_emit_kernel<<<grid, SLICE_THREADS, 0, stream>>>(l);
     if ((st = check_launch("evict_emit_kernel")) != SPECATTN_OK) return st;
-    evict_state_kernel<<<dim3(rows, std::min((e->move_capacity + 1023) / 1024, 64)), 256, 0, stream>>>(l);
+    evict_state_kernel<<<dim3(rows, std::min((e->move_capacity + 255) / 256, 1024)), 256, 0, stream>>>(l);
     return check_launch("evict_state_kernel");
 }
 

@@ -135,11 +135,13 @@ template <int D, int DTYPE, int U, bool LOAD> __global__ __launch_bounds__(THREA
         for (int u = 0; u < U; ++u) {
             const int t = first + u * ROWS;
             there[u] = t < count && slot_offsets(a.c, b, h, start + t, codes[u], scales[u]);
+            if (!there[u]) codes[u] = scales[u] = 0;
         }
         if constexpr (!LOAD) {
+            // (rows that are left out: others instead, so that all requests go out together; behind a condition each: 154 us for 125)
             Eight<DTYPE> e[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) if (there[u]) e[u] = load_eight<DTYPE>(side, base + (first + u * ROWS) * a.stride_t);
+            for (int u = 0; u < U; ++u) e[u] = load_eight<DTYPE>(side, base + min(first + u * ROWS, a.T - 1) * a.stride_t);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (!there[u]) continue;                          // (the four lanes of a block together)
@@ -148,12 +150,16 @@ template <int D, int DTYPE, int U, bool LOAD> __global__ __launch_bounds__(THREA
                 uint32_t word;
                 const uint32_t scale = quantise(x, word);
                 *reinterpret_cast<uint32_t *>(a.c.codes + codes[u] + 4 * lane) = word;
-                if (lane % 4 == 0) a.c.scales[scales[u] + lane / 4] = (uint8_t)scale;
+                // the four blocks of 16 lanes make a word
+                uint32_t four = scale << lane / 4 % 4 * 8;
+                four |= (uint32_t)__builtin_amdgcn_update_dpp(0, four, 0x124, 0xf, 0xf, true);      // four lanes on in the row of 16
+                four |= (uint32_t)__builtin_amdgcn_update_dpp(0, four, 0x128, 0xf, 0xf, true);      // and eight
+                if (lane % 16 == 0) *reinterpret_cast<uint32_t *>(a.c.scales + scales[u] + lane / 4) = four;
             }
         } else {
             uint32_t word[U], scale[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) if (there[u]) {
+            for (int u = 0; u < U; ++u) {
                 word[u] = *reinterpret_cast<const uint32_t *>(a.c.codes + codes[u] + 4 * lane);
                 scale[u] = a.c.scales[scales[u] + lane / 4];
             }
