@@ -16,7 +16,9 @@
 //            the lanes hold them; the queries are laid out to match.
 //   values   lane (c, g) takes d/16 consecutive elements of the eight positions 4g .. 4g+3 and 16+4g .. 16+4g+3: what a
 //            column tile of the second product needs of those positions, for d/16 column tiles
-//   S^T = K Q^T on mfma 16x16x32 in bf16: codes times scales are exact, and so are bf16 queries; fp16 queries go in two exact parts.
+//   S^T = K Q^T on mfma 16x16x32.  In bf16 codes times scales are exact, and so are bf16 queries.  fp16 queries are not: their keys go in
+//   fp16, in units of the largest scale of a position, and scores are multiplied by it.  (Queries in two exact bf16 parts took twice the
+//   matrix instructions: 64 sequences of 8 kv heads, 4 heads by 5 queries, up to 65536 positions, a third kept: 294 us / 250.)
 //   O^T += V^T P^T in fp16: a weight goes in two parts, 22 significant bits (bf16 took three: a third more matrix and twice the vector
 //   instructions), and the scales in units that follow the largest one of a block, since fp16 has not their range.  The first product
 //   leaves the weights of a query in the lanes that hold the values' positions, so weights never leave their lane.
@@ -60,12 +62,12 @@ template <int D> struct Geo {
     static constexpr int PITCH = D + 4;   // floats of a row in the merge buffer
     static constexpr int LPR = D / 16;    // lanes that fetch the codes of one position
     static constexpr int RPI = 64 / LPR;  // positions per instruction
-    static constexpr int CI = TILE / RPI; // instructions per tile: position CI * j + k is the j-th of instruction k
+    static constexpr int CI = TILE / RPI; // instructions per tile: instruction k fetches positions RPI k, RPI k + 1, ...
     static constexpr int CODES = TILE * D;
     // 16-byte piece c of the codes of position `pos` lies in place c ^ swz(pos), so that both reads spread over all banks: keys, one piece
     // of each of 16 positions, and values, 64 (32) bytes of the positions 4g + i of four g.
-    static __device__ __forceinline__ int swz(int pos) { return D == 128 ? (pos & 3) | ((pos >> 3 & 1) << 2) : (pos & 1) | (pos >> 3 & 1) << 1; }
-    static __device__ __forceinline__ int piece(int pos, int c) { return (pos % CI) * 1024 + (pos / CI) * D + ((c ^ swz(pos)) * 16); }
+    static __device__ __forceinline__ int swz(int pos) { return D == 128 ? (pos >> 1 & 3) | (pos >> 2 & 1) << 2 : pos >> 2 & 3; }
+    static __device__ __forceinline__ int piece(int pos, int c) { return pos * D + ((c ^ swz(pos)) * 16); }
 };
 
 // A wave's part of the LDS.
@@ -74,7 +76,9 @@ template <int D, int DEPTH> struct WaveLds {
     uint32_t scales[DEPTH][64];           // d = 128: of the keys of the 32 positions, then of the values; d = 64: of both
     uint32_t words[DEPTH][64];            // list words
     int32_t pages[DEPTH][64];             // page numbers
-    uint32_t codes_at[TILE];              // row offsets of the tile that is requested next
+    uint32_t codes_at[TILE];              // row offsets of the tile that is requested next; position p in place p % RPI * CI + p / RPI
+    float unit[TILE];                     // fp16 queries: largest scale of a position's keys, times what scores are scaled by
+    uint32_t unit_byte[TILE];             // the same scale as a byte
 };
 
 template <int D, int NW> struct MergeLds {
@@ -82,10 +86,10 @@ template <int D, int NW> struct MergeLds {
     float ml[NW][16][2];
 };
 
-template <int D, int NQ, int QP, bool FEW> struct Lds {
+template <int D, int NQ, bool FEW> struct Lds {
     static constexpr int NW = Waves<NQ, FEW>::N;
-    static constexpr bool Q = NQ * QP > 2;                                              // queries wait in LDS, else in registers
-    static constexpr int Q_BYTES = Q ? NQ * QP * Geo<D>::KW * 1024 : 16;
+    static constexpr bool Q = NQ > 2;                                                   // queries wait in LDS, else in registers
+    static constexpr int Q_BYTES = Q ? NQ * Geo<D>::KW * 1024 : 16;
     union {
         WaveLds<D, Waves<NQ, FEW>::DEPTH> wave[NW];
         MergeLds<D, NW> merge;
@@ -95,7 +99,7 @@ template <int D, int NQ, int QP, bool FEW> struct Lds {
     int count[MAX_ROWS];
     int red[2][NW];
 };
-static_assert(sizeof(Lds<128, 4, 2, false>) <= 160 * 1024, "a workgroup must fit a CU's LDS");
+static_assert(sizeof(Lds<128, 4, false>) <= 160 * 1024, "a workgroup must fit a CU's LDS");
 
 // Requests 16 or 4 bytes per lane from `src` to `to` + 16 or 4 * lane in LDS.  Counts as one request of the wave in order; nobody but
 // wait_requests waits for it.
@@ -138,6 +142,14 @@ __device__ __forceinline__ uint32_t half_pair_of(uint32_t codes, float scale, in
     const f16x2 x = B == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0) : B == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1)
                   : B == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3);
     return __builtin_bit_cast(uint32_t, x);
+}
+template <typename T> __device__ __forceinline__ T lds_at(uint32_t offset) { return *(const __attribute__((address_space(3))) T *)offset; }
+// The largest of three, NaNs aside.  (Written as fmaxf every operand is made quiet first: an instruction more for each.)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
 }
 __device__ __forceinline__ float shuffle_xor(float x, int mask) { return __shfl_xor(x, mask, 64); }
 
@@ -204,12 +216,12 @@ __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readla
 // row's tiles are dealt to them evenly.  Otherwise the tiles of all rows form one line with SEG_COST ahead of every row, and every
 // workgroup takes an equal stretch of it.  Picking up a second row costs a workgroup about 8 us, the time of 20 tiles: 64 rows of 7500
 // positions 42 us in equal stretches / 36 in whole workgroups.
-template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<NQ, FEW>::THREADS)) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
+template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves<NQ, FEW>::THREADS)) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
 {
     typedef Geo<D> G;
     constexpr int NW = Waves<NQ, FEW>::N, DEPTH = Waves<NQ, FEW>::DEPTH, AHEAD = DEPTH - 1, THREADS = Waves<NQ, FEW>::THREADS;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds_bytes[];
-    Lds<D, NQ, QP, FEW> &lds = *reinterpret_cast<Lds<D, NQ, QP, FEW> *>(lds_bytes);
+    Lds<D, NQ, FEW> &lds = *reinterpret_cast<Lds<D, NQ, FEW> *>(lds_bytes);
     const Lengths lengths = {counts, seq_lens, per_h_mul, per_h_shift, rows, row0, n_max, capacity, dense, chunk_shift};
     const int tid = threadIdx.x, lane = tid % 64, low = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -305,30 +317,14 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
         const int head0 = h * (a.H_q / a.H_kv) + a.first_head;
 
         // queries: element j of k-step s in lane (q, g) is element (d/4) g + 8 s + j of query 16 qt + q
-        uint32_t qf[Lds<D, NQ, QP, FEW>::Q ? 1 : NQ * QP][G::KW][4];
+        uint32_t qf[Lds<D, NQ, FEW>::Q ? 1 : NQ][G::KW][4];
         {
             auto query = [&](int qt) {
                 const int i = min(qt * 16 + low, a.queries - 1), gh = a.per_t.divide(i), t = i - gh * a.T;      // (behind the last query: that one again)
                 return a.q + b * a.q_b + (head0 + gh) * a.q_h + t * a.q_t + (D / 4) * g;
             };
-            auto split = [&](u32x4 w, uint32_t (&part)[QP][4]) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if constexpr (QP == 1) part[0][k] = w[k];
-                    else {
-                        const float x = (float)__builtin_bit_cast(_Float16, (uint16_t)w[k]), y = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[k] >> 16));
-                        part[0][k] = to_bf16(x, y);
-                        part[1][k] = to_bf16(x - low_half(part[0][k]), y - high_half(part[0][k]));
-                    }
-                }
-            };
-            if constexpr (Lds<D, NQ, QP, FEW>::Q) {
-                for (int k = wave; k < NQ * G::KW; k += NW) {
-                    uint32_t part[QP][4];
-                    split(*reinterpret_cast<const u32x4 *>(query(k / G::KW) + 8 * (k % G::KW)), part);
-#pragma unroll
-                    for (int q = 0; q < QP; ++q) *reinterpret_cast<u32x4 *>(lds.q + ((q * NQ * G::KW + k) * 64 + lane) * 16) = u32x4{part[q][0], part[q][1], part[q][2], part[q][3]};
-                }
+            if constexpr (Lds<D, NQ, FEW>::Q) {
+                for (int k = wave; k < NQ * G::KW; k += NW) *reinterpret_cast<u32x4 *>(lds.q + (k * 64 + lane) * 16) = *reinterpret_cast<const u32x4 *>(query(k / G::KW) + 8 * (k % G::KW));
                 __syncthreads();
             } else {
 #pragma unroll
@@ -336,12 +332,9 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
                     const uint16_t *from = query(qt);
 #pragma unroll
                     for (int s = 0; s < G::KW; ++s) {
-                        uint32_t part[QP][4];
-                        split(*reinterpret_cast<const u32x4 *>(from + 8 * s), part);
+                        const u32x4 w = *reinterpret_cast<const u32x4 *>(from + 8 * s);
 #pragma unroll
-                        for (int q = 0; q < QP; ++q)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) qf[q * NQ + qt][s][k] = part[q][k];
+                        for (int k = 0; k < 4; ++k) qf[qt][s][k] = w[k];
                     }
                 }
             }
@@ -363,11 +356,16 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
         WaveLds<D, DEPTH> &mine = lds.wave[wave];
         const uint32_t codes_lds = lds_offset(mine.codes), scales_lds = lds_offset(mine.scales), words_lds = lds_offset(mine.words), pages_lds = lds_offset(mine.pages);
         const int32_t *list = a.indices + row * a.idx_stride, *pages = a.page_table + (int64_t)b * a.max_pages;
-        const uint8_t *codes = a.codes + (a.paged ? 0 : b * a.codes_b) + h * a.codes_h;
+        const uint8_t *codes = a.codes + (a.paged ? 0 : b * a.codes_b) + h * a.codes_h + ((lane % G::LPR) ^ G::swz(lane / G::LPR)) * 16;
         const uint8_t *scales = a.scales + (a.paged ? 0 : b * a.scales_b) + h * a.scales_h + (D == 128 ? lane / 32 * 4 : 0);
         const bool listed = !dense, looked_up = a.paged == 1;
         const int base_tile = t0 + wave, in_tile = lane % TILE;
-        const int lane_piece = (lane % G::LPR) ^ G::swz(lane / G::LPR * G::CI);      // (of instruction 0; of instruction k: ^ k)
+        const int at_place = in_tile % G::RPI * G::CI + in_tile / G::RPI;
+        // where the lane reads its keys (positions low, 16 + low), its values (4g + i, 16 + 4g + i) and their scales, in buffer 0
+        const uint32_t keys_lds = codes_lds + G::piece(low, D == 128 ? g : g / 2) + (D == 128 ? 0 : g % 2 * 8);
+        const uint32_t values_lds = codes_lds + G::piece(4 * g, D == 128 ? 4 + low / 4 : 2 + low / 8) + (D == 128 ? low % 4 * 4 : low % 8 * 2);
+        const uint32_t values2_lds = codes_lds + G::piece(4 * g + 2, D == 128 ? 4 + low / 4 : 2 + low / 8) + (D == 128 ? low % 4 * 4 : low % 8 * 2) - 2 * D;     // (places of i = 2, 3)
+        const uint32_t key_scale_lds = scales_lds + 4 * low + (F16 ? 0 : D == 128 ? g : g / 2), value_scale_lds = scales_lds + (D == 128 ? 128 : 0) + 16 * g;
         auto list_rank = [&](int i) { return min((base_tile + i * NW) * TILE + in_tile, n - 1); };
         auto list_at = [&](int i) { return list + (list_rank(i) >> a.chunk_shift); };
         auto slot_of = [&](int i, int word) -> int {
@@ -389,7 +387,7 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
                 code_at = (uint32_t)slot * a.codes_n;
                 scale_at = (uint32_t)slot * a.scales_n;
             }
-            mine.codes_at[in_tile] = code_at;
+            mine.codes_at[at_place] = code_at;
             uint32_t off[G::CI];
 #pragma unroll
             for (int k = 0; k < G::CI; ++k) off[k] = mine.codes_at[lane / G::LPR * G::CI + k];
@@ -397,7 +395,7 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
             request4(scales + ((uint64_t)scale_at << 2), scales_lds + at * 256);
 #pragma unroll
             for (int k = 0; k < G::CI; ++k)
-                request16(codes + ((uint64_t)(off[k] + (lane_piece ^ k)) << 4), codes_lds + at * G::CODES + k * 1024);
+                request16(codes + ((uint64_t)off[k] << 4), codes_lds + at * G::CODES + k * 1024);
         };
 
         uint32_t w[NQ][PARTS][4], v[8];
@@ -451,18 +449,26 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
                 else wait_requests<(AHEAD - 1) * R>();
                 const int prev = at == 0 ? DEPTH - 1 : at - 1, after = at == DEPTH - 1 ? 0 : at + 1;
                 const int word_at = DEPTH == 2 ? at : after;      // of tile i + 2 AHEAD, like its pages
-                const uint8_t *codes_in = mine.codes[at], *scales_in = reinterpret_cast<const uint8_t *>(mine.scales[at]);
+                const uint32_t codes_in = at * G::CODES, scales_in = at * 256;
                 const int word = listed ? (int)mine.words[word_at][lane] : 0, in_page = looked_up ? mine.pages[prev][lane] : 0;
                 uint32_t key[2][G::KW], key_scale[2];
+                if constexpr (F16) {                              // keys in units of the largest scale of their position
+                    const uint32_t four = lds_at<uint32_t>(scales_lds + scales_in + 4 * in_tile);
+                    uint32_t top = max(four & 255, four >> 8 & 255);
+                    if constexpr (D == 128) top = max(max(top, four >> 16 & 255), four >> 24);
+                    mine.unit[in_tile] = top == 255 ? NAN : __uint_as_float(top << 23) * a.to_log2;
+                    mine.unit_byte[in_tile] = top;
+                }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    key_scale[k] = scales_in[4 * (16 * k + low) + (D == 128 ? g : g / 2)];
+                    if constexpr (F16) key_scale[k] = lds_at<uint32_t>(key_scale_lds + scales_in + 64 * k) >> (D == 128 ? g : g / 2) * 8 & 255;
+                    else key_scale[k] = lds_at<uint8_t>(key_scale_lds + scales_in + 64 * k);
                     if constexpr (D == 128) {
-                        const u32x4 x = *reinterpret_cast<const u32x4 *>(codes_in + G::piece(16 * k + low, g));
+                        const u32x4 x = lds_at<u32x4>(keys_lds + codes_in + 16 * D * k);
 #pragma unroll
                         for (int s = 0; s < 4; ++s) key[k][s] = x[s];
                     } else {
-                        const u32x2 x = *reinterpret_cast<const u32x2 *>(codes_in + G::piece(16 * k + low, g / 2) + g % 2 * 8);
+                        const u32x2 x = lds_at<u32x2>(keys_lds + codes_in + 16 * D * k);
                         key[k][0] = x[0];
                         key[k][1] = x[1];
                     }
@@ -474,38 +480,47 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
                 request_pages(slot[AHEAD - 1], word_at);
                 request_words(i + 3 * AHEAD, DEPTH == 2 ? after : at);
 
-                f32x4 s[NQ][2];
+                f32x4 s[NQ][2], unit_of[2];
 #pragma unroll
                 for (int qt = 0; qt < NQ; ++qt) s[qt][0] = s[qt][1] = f32x4{0, 0, 0, 0};
+                float scale_of[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const float scale = __uint_as_float(key_scale[k] << 23);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int step = 0; step < G::KW; ++step) {
-                        uint32_t f[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) f[j] = pair_of(key[k][step], scale, j);
-#pragma unroll
-                        for (int q = 0; q < QP * NQ; ++q) {
-                            if constexpr (Lds<D, NQ, QP, FEW>::Q) {
-                                const u32x4 x = *reinterpret_cast<const u32x4 *>(lds.q + ((q * G::KW + step) * 64 + lane) * 16);
-                                const uint32_t y[4] = {x[0], x[1], x[2], x[3]};
-                                s[q % NQ][k] = mfma(f, y, s[q % NQ][k]);
-                            } else s[q % NQ][k] = mfma(f, qf[q][step], s[q % NQ][k]);
-                        }
-                    }
+                    if constexpr (F16) {
+                        scale_of[k] = __int_as_float(max((int)(key_scale[k] - mine.unit_byte[16 * k + low]) + 127, 0) << 23);
+                        unit_of[k] = *reinterpret_cast<const f32x4 *>(&mine.unit[16 * k + 4 * g]);
+                    } else scale_of[k] = __uint_as_float(key_scale[k] << 23);
                 }
 #pragma unroll
+                for (int step = 0; step < G::KW; ++step)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t f[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f[j] = F16 ? half_pair_of(key[k][step], scale_of[k], j) : pair_of(key[k][step], scale_of[k], j);
+#pragma unroll
+                        for (int qt = 0; qt < NQ; ++qt) {
+                            uint32_t y[4];
+                            if constexpr (Lds<D, NQ, FEW>::Q) {
+                                const u32x4 x = *reinterpret_cast<const u32x4 *>(lds.q + ((qt * G::KW + step) * 64 + lane) * 16);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) y[j] = x[j];
+                            } else
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) y[j] = qf[qt][step][j];
+                            s[qt][k] = F16 ? mfma_f16(f, y, s[qt][k]) : mfma(f, y, s[qt][k]);
+                        }
+                    }
+#pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const u32x4 four = *reinterpret_cast<const u32x4 *>(scales_in + (D == 128 ? 128 : 0) + 4 * (16 * k + 4 * g));
+                    const u32x4 four = lds_at<u32x4>(value_scale_lds + scales_in + 64 * k);
                     const int block = D == 128 ? low / 4 : 2 + low / 8;        // byte of a position's word
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         v_scale[4 * k + j] = (int)__builtin_amdgcn_ubfe(four[j], 8 * block, 8);
-                        const uint8_t *src = codes_in + G::piece(16 * k + 4 * g + j, D == 128 ? 4 + low / 4 : 2 + low / 8);
-                        if constexpr (D == 128) v[4 * k + j] = *reinterpret_cast<const uint32_t *>(src + low % 4 * 4);
-                        else v[4 * k + j] = *reinterpret_cast<const uint16_t *>(src + low % 8 * 2);
+                        const uint32_t from = (j < 2 ? values_lds : values2_lds) + codes_in + (16 * k + j) * D;
+                        if constexpr (D == 128) v[4 * k + j] = lds_at<uint32_t>(from);
+                        else v[4 * k + j] = lds_at<uint16_t>(from);
                     }
                 }
                 // The scores are read by the vector unit next, in another block of the program.  The compiler has been seen to leave the wait
@@ -516,6 +531,11 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
                     if (qt == 0) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(s[qt][0]), "+v"(s[qt][1]));
                     else asm volatile("" : "+v"(s[qt][0]), "+v"(s[qt][1]));
                 }
+                if constexpr (F16)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll
+                        for (int qt = 0; qt < NQ; ++qt) s[qt][k / 4][k % 4] *= unit_of[k / 4][k % 4];
                 const int left = n - t * TILE;
                 if (__builtin_expect(left < TILE, 0)) {                                // a row's last tile: what lies behind it repeats its last position
 #pragma unroll
@@ -526,10 +546,8 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
 #pragma unroll
                 for (int qt = 0; qt < NQ; ++qt) {
                     __builtin_amdgcn_sched_barrier(0);
-                    float most = fmaxf(s[qt][0][0], s[qt][1][0]);
-#pragma unroll
-                    for (int k = 1; k < 4; ++k) most = fmaxf(most, fmaxf(s[qt][0][k], s[qt][1][k]));
-                    most *= a.to_log2;
+                    float most = max3(max3(s[qt][0][0], s[qt][0][1], s[qt][0][2]), max3(s[qt][0][3], s[qt][1][0], s[qt][1][1]), max3(s[qt][1][2], s[qt][1][3], s[qt][1][3]));
+                    if constexpr (!F16) most *= a.to_log2;
                     if (__builtin_expect(__any(most > ref[qt] + RANGE), 0)) {
                         most = fmaxf(most, shuffle_xor(most, 16));
                         most = fmaxf(most, shuffle_xor(most, 32));
@@ -541,12 +559,12 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
                     }
                     float e[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][k / 4][k % 4], a.to_log2, -ref[qt]));
+                    for (int k = 0; k < 8; ++k) e[k] = __builtin_amdgcn_exp2f(F16 ? s[qt][k / 4][k % 4] - ref[qt] : __builtin_fmaf(s[qt][k / 4][k % 4], a.to_log2, -ref[qt]));
                     sum[qt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         w[qt][0][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[2 * k], e[2 * k + 1]));
-                        w[qt][1][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[2 * k] - f16_low(w[qt][0][k]), e[2 * k + 1] - f16_high(w[qt][0][k])));
+                        w[qt][1][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf(-1.0f, f16_low(w[qt][0][k]), e[2 * k]), __builtin_fmaf(-1.0f, f16_high(w[qt][0][k]), e[2 * k + 1])));
                     }
                 }
                 // scales in units of 2^(unit - 127)
@@ -572,8 +590,9 @@ template <int D, int NQ, int QP, bool FEW> __global__ __launch_bounds__((Waves<N
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v_scale[j] = v_scale[j] == 255 ? unit + 128 : max(v_scale[j], unit - 100);    // (NaN; zero)
                 }
+                const int unit_bits = (127 - unit) * (1 << 23);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v_scale[j] = (v_scale[j] - unit + 127) << 23;
+                for (int j = 0; j < 8; ++j) v_scale[j] = (int)((uint32_t)v_scale[j] << 23) + unit_bits;
                 add_values();
                 at = after;
             }
@@ -721,23 +740,17 @@ template <int D> __global__ __launch_bounds__(256) void mx_merge_kernel(const ui
 
 template <int D, int NQ> const void *variant(bool f16, bool few)
 {
-    return f16 ? few ? reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 2, true>) : reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 2, false>)
-               : few ? reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 1, true>) : reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, 1, false>);
+    return f16 ? few ? reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, true, true>) : reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, true, false>)
+               : few ? reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, false, true>) : reinterpret_cast<const void *>(mx_attn_kernel<D, NQ, false, false>);
 }
 template <int D> const void *variant(int nq, bool f16, bool few)
 {
     return nq == 1 ? variant<D, 1>(f16, few) : nq == 2 ? variant<D, 2>(f16, few) : nq == 3 ? variant<D, 3>(f16, few) : variant<D, 4>(f16, few);
 }
 const void *variant(int d, int nq, bool f16, bool few) { return d == 128 ? variant<128>(nq, f16, few) : variant<64>(nq, f16, few); }
-template <int D, int NQ> size_t lds_size(bool f16, bool few)
-{
-    return f16 ? few ? sizeof(Lds<D, NQ, 2, true>) : sizeof(Lds<D, NQ, 2, false>) : few ? sizeof(Lds<D, NQ, 1, true>) : sizeof(Lds<D, NQ, 1, false>);
-}
-template <int D> size_t lds_size(int nq, bool f16, bool few)
-{
-    return nq == 1 ? lds_size<D, 1>(f16, few) : nq == 2 ? lds_size<D, 2>(f16, few) : nq == 3 ? lds_size<D, 3>(f16, few) : lds_size<D, 4>(f16, few);
-}
-size_t lds_size(int d, int nq, bool f16, bool few) { return d == 128 ? lds_size<128>(nq, f16, few) : lds_size<64>(nq, f16, few); }
+template <int D, int NQ> size_t lds_size(bool few) { return few ? sizeof(Lds<D, NQ, true>) : sizeof(Lds<D, NQ, false>); }
+template <int D> size_t lds_size(int nq, bool few) { return nq == 1 ? lds_size<D, 1>(few) : nq == 2 ? lds_size<D, 2>(few) : nq == 3 ? lds_size<D, 3>(few) : lds_size<D, 4>(few); }
+size_t lds_size(int d, int nq, bool few) { return d == 128 ? lds_size<128>(nq, few) : lds_size<64>(nq, few); }
 int threads_of(int nq, bool few) { return few && nq == 1 ? Waves<1, true>::THREADS : Waves<1, false>::THREADS; }
 
 // Query heads of a kv head per launch: groups of more than 64 query rows go out in equal parts.
@@ -771,9 +784,9 @@ specattn_status mx_attn_configure()
     for (int k = 0; k < 32; ++k) {
         const int d = k & 1 ? 128 : 64, nq = (k >> 1 & 3) + 1;
         const bool f16 = k & 8, few = k & 16;
-        if (hipFuncSetAttribute(variant(d, nq, f16, few), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_size(d, nq, f16, few)) != hipSuccess) {
+        if (hipFuncSetAttribute(variant(d, nq, f16, few), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_size(d, nq, few)) != hipSuccess) {
             (void)hipGetLastError();
-            set_error("cannot reserve %zu bytes of LDS", lds_size(d, nq, f16, few));
+            set_error("cannot reserve %zu bytes of LDS", lds_size(d, nq, few));
             return SPECATTN_EHIP;
         }
     }
@@ -818,7 +831,7 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
             void *args[] = {&n.counts, &n.seq_lens, &n.per_h_mul, &n.per_h_shift, &n.rows, &n.row0, &n.n_max, &n.capacity, &n.dense, &n.chunk_shift, &a};
             const bool f16 = c.dtype == SPECATTN_F16;
             const bool few = here <= std::min(64, cu_count());
-            if (hipLaunchKernel(variant(c.d, nq, f16, few), dim3(cu_count()), dim3(threads_of(nq, few)), args, lds_size(c.d, nq, f16, few), stream) != hipSuccess) return check_launch("mx_attn_kernel");
+            if (hipLaunchKernel(variant(c.d, nq, f16, few), dim3(cu_count()), dim3(threads_of(nq, few)), args, lds_size(c.d, nq, few), stream) != hipSuccess) return check_launch("mx_attn_kernel");
             st = check_launch("mx_attn_kernel");
             if (st != SPECATTN_OK) return st;
             const dim3 grid((a.queries + 3) / 4, here);

@@ -196,6 +196,29 @@ def test_far_scales_and_large_scores():
     c.check([[np.arange(300)]], scale=0.05)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_key_blocks_of_any_scale_and_rows_of_zeros(dtype, d):
+    """Blocks of a key 2^120 apart, the smallest scale there is, and positions without any key, the last one among them, behind which a
+    tile is masked."""
+    c = Case(1, 4, 1, 3, d, 45, dtype, seed=15)
+    c.scales[..., :d // 32] = np.random.default_rng(15).choice([0, 1, 60, 100, 112, 120, 124], size=(1, 1, 45, d // 32))
+    for at in (3, 20, 44):
+        c.codes[0, 0, at, :d // 2], c.scales[0, 0, at, :d // 32] = 0, 0
+    c.check([[np.arange(45)]])
+    c.scales[..., :d // 32] = 0
+    c.check([[np.arange(45)]])
+
+
+def test_nan_keys_with_fp16_queries():
+    c = Case(1, 4, 2, 2, 128, 70, "f16", seed=19)
+    c.scales[0, 1, 69, 3] = 255
+    got, lse = c.run()
+    k, v = c.rows()
+    want, _, tol = ref.attention(c.q.double().numpy(), np.nan_to_num(k), v, [[np.arange(70)] * 2], 128 ** -0.5)
+    assert (np.abs(got - want) <= tol[..., None])[:, :2].all() and np.isnan(got[0, 2:]).all() and np.isnan(lse[0, 2:]).all()
+
+
 def test_a_sink_of_almost_all_weight():
     """One position 25 binary orders above the others: their small weights have to come through."""
     c = Case(1, 2, 1, 1, 128, 5000, "f16", seed=17)
