@@ -43,11 +43,11 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // Waves per workgroup, and tiles of a wave in use and on their way.
 template <int NQ, bool FEW> struct Waves {
-    static constexpr int N = FEW && NQ == 1 ? 12 : 8, DEPTH = N == 12 ? 2 : 3, THREADS = N * 64;
+    static constexpr int N = !FEW ? 4 : NQ == 1 ? 12 : 8, DEPTH = N == 12 ? 2 : 3, THREADS = N * 64;
 };
 constexpr int TILE = 32;                  // positions per tile
-constexpr int MAX_ROWS = 1024;            // rows per launch
-constexpr int SEG_COST = 20;              // cost of picking a row up, in tiles
+constexpr int MAX_ROWS = 512;             // rows per launch: two for each thread
+constexpr int SEG_COST = 10;              // cost of picking a row up, in tiles
 constexpr int PARTS = 2;                  // fp16 parts of a weight
 // Weights are taken in units of 2^ref.  ref puts the largest weight so far at 2^HEAD and moves when one exceeds 2^RANGE: fp16 ends at 2^16
 // and, downwards, at 2^-24, so that a weight 2^-36 below the largest still counts.
@@ -99,7 +99,7 @@ template <int D, int NQ, bool FEW> struct Lds {
     int count[MAX_ROWS];
     int red[2][NW];
 };
-static_assert(sizeof(Lds<128, 4, false>) <= 160 * 1024, "a workgroup must fit a CU's LDS");
+static_assert(sizeof(Lds<128, 4, true>) <= 160 * 1024 && sizeof(Lds<128, 4, false>) <= 80 * 1024, "workgroups must fit a CU's LDS");
 
 // Requests 16 or 4 bytes per lane from `src` to `to` + 16 or 4 * lane in LDS.  Counts as one request of the wave in order; nobody but
 // wait_requests waits for it.
@@ -129,8 +129,19 @@ __device__ __forceinline__ f32x4 mfma_f16(const uint32_t (&a)[4], const uint32_t
     const u32x4 x = {a[0], a[1], a[2], a[3]}, y = {b[0], b[1], b[2], b[3]};
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
 }
-__device__ __forceinline__ float f16_low(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[0]; }
-__device__ __forceinline__ float f16_high(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[1]; }
+// x less the low, the high half of w: exact where the half is x cut to fp16.
+__device__ __forceinline__ float less_low(float x, uint32_t w)
+{
+    float y;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[0,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(w), "v"(x));
+    return y;
+}
+__device__ __forceinline__ float less_high(float x, uint32_t w)
+{
+    float y;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(w), "v"(x));
+    return y;
+}
 // Elements 2B and 2B + 1 of eight codes.  (The conversion takes a scale's exponent alone.)
 __device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int B)
 {
@@ -216,7 +227,7 @@ __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readla
 // row's tiles are dealt to them evenly.  Otherwise the tiles of all rows form one line with SEG_COST ahead of every row, and every
 // workgroup takes an equal stretch of it.  Picking up a second row costs a workgroup about 8 us, the time of 20 tiles: 64 rows of 7500
 // positions 42 us in equal stretches / 36 in whole workgroups.
-template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves<NQ, FEW>::THREADS)) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
+template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves<NQ, FEW>::THREADS), 2) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
 {
     typedef Geo<D> G;
     constexpr int NW = Waves<NQ, FEW>::N, DEPTH = Waves<NQ, FEW>::DEPTH, AHEAD = DEPTH - 1, THREADS = Waves<NQ, FEW>::THREADS;
@@ -564,7 +575,7 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         w[qt][0][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(e[2 * k], e[2 * k + 1]));
-                        w[qt][1][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf(-1.0f, f16_low(w[qt][0][k]), e[2 * k]), __builtin_fmaf(-1.0f, f16_high(w[qt][0][k]), e[2 * k + 1])));
+                        w[qt][1][k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(less_low(e[2 * k], w[qt][0][k]), less_high(e[2 * k + 1], w[qt][0][k])));
                     }
                 }
                 // scales in units of 2^(unit - 127)
@@ -622,17 +633,17 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
                 for (int d = 0; d < G::DT; d += 4)
                     *reinterpret_cast<f32x4 *>(&lds.merge.o[wave][low][G::DT * (4 * g + i) + d]) = f32x4{acc[qt][d][i], acc[qt][d + 1][i], acc[qt][d + 2][i], acc[qt][d + 3][i]};
             __syncthreads();
-            const int q = tid / (D / 4), col = tid % (D / 4) * 4;
-            if (q < 16) {
+            for (int x = tid; x < 16 * D / 4; x += THREADS) {
+                const int q = x / (D / 4), col = x % (D / 4) * 4;
                 float top = -INFINITY, all = 0.0f, m[NW];
 #pragma unroll
-                for (int x = 0; x < NW; ++x) { m[x] = lds.merge.ml[x][q][0]; top = fmaxf(top, m[x]); }
+                for (int k = 0; k < NW; ++k) { m[k] = lds.merge.ml[k][q][0]; top = fmaxf(top, m[k]); }
                 f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-                for (int x = 0; x < NW; ++x) {
-                    const float f = m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[x] - top);
-                    all += f * lds.merge.ml[x][q][1];
-                    o += f * *reinterpret_cast<const f32x4 *>(&lds.merge.o[x][q][col]);
+                for (int k = 0; k < NW; ++k) {
+                    const float f = m[k] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[k] - top);
+                    all += f * lds.merge.ml[k][q][1];
+                    o += f * *reinterpret_cast<const f32x4 *>(&lds.merge.o[k][q][col]);
                 }
                 const int i = qt * 16 + q;
                 if (!alone) {
@@ -751,7 +762,7 @@ const void *variant(int d, int nq, bool f16, bool few) { return d == 128 ? varia
 template <int D, int NQ> size_t lds_size(bool few) { return few ? sizeof(Lds<D, NQ, true>) : sizeof(Lds<D, NQ, false>); }
 template <int D> size_t lds_size(int nq, bool few) { return nq == 1 ? lds_size<D, 1>(few) : nq == 2 ? lds_size<D, 2>(few) : nq == 3 ? lds_size<D, 3>(few) : lds_size<D, 4>(few); }
 size_t lds_size(int d, int nq, bool few) { return d == 128 ? lds_size<128>(nq, few) : lds_size<64>(nq, few); }
-int threads_of(int nq, bool few) { return few && nq == 1 ? Waves<1, true>::THREADS : Waves<1, false>::THREADS; }
+int threads_of(int nq, bool few) { return !few ? Waves<1, false>::THREADS : nq == 1 ? Waves<1, true>::THREADS : Waves<2, true>::THREADS; }
 
 // Query heads of a kv head per launch: groups of more than 64 query rows go out in equal parts.
 int heads_per_launch(int G, int T)
@@ -765,7 +776,7 @@ int heads_per_launch(int G, int T)
 size_t mx_attn_workspace_bytes(int rows, int G, int T, int d)
 {
     const int per = std::min(rows, MAX_ROWS), padded = (heads_per_launch(G, T) * T + 15) / 16 * 16;
-    return (((size_t)per * 4 + 255) & ~(size_t)255) + (((size_t)(cu_count() + per) * padded * (d + 2) * sizeof(float) + 255) & ~(size_t)255);
+    return (((size_t)per * 4 + 255) & ~(size_t)255) + (((size_t)(2 * cu_count() + per) * padded * (d + 2) * sizeof(float) + 255) & ~(size_t)255);
 }
 
 specattn_status mx_attn_configure()
@@ -831,7 +842,7 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
             void *args[] = {&n.counts, &n.seq_lens, &n.per_h_mul, &n.per_h_shift, &n.rows, &n.row0, &n.n_max, &n.capacity, &n.dense, &n.chunk_shift, &a};
             const bool f16 = c.dtype == SPECATTN_F16;
             const bool few = here <= std::min(64, cu_count());
-            if (hipLaunchKernel(variant(c.d, nq, f16, few), dim3(cu_count()), dim3(threads_of(nq, few)), args, lds_size(c.d, nq, few), stream) != hipSuccess) return check_launch("mx_attn_kernel");
+            if (hipLaunchKernel(variant(c.d, nq, f16, few), dim3(few ? cu_count() : 2 * cu_count()), dim3(threads_of(nq, few)), args, lds_size(c.d, nq, few), stream) != hipSuccess) return check_launch("mx_attn_kernel");
             st = check_launch("mx_attn_kernel");
             if (st != SPECATTN_OK) return st;
             const dim3 grid((a.queries + 3) / 4, here);
