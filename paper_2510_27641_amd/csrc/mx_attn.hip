@@ -1,16 +1,15 @@
 // Sparse decode attention (Section 3.1.2, Eq. 2-3; Section 3.5) over a cache in 4 bits, d = 128 or 64, up to 64 query rows
 // per kv head and launch.
 //
-// Work split: the attended positions of all rows, in tiles of 32, form one line; the line is cut into equal shares, one per
-// workgroup of eight waves (one per CU).  A share that crosses row boundaries yields one partial (m, l, o) per (row, share)
-// in slot share + row; mx_merge_kernel combines a row's partials in share order.  Inside a share tile k goes to wave k mod 8,
-// so every sum is taken in a fixed order.
+// Work split: the attended positions of a row go in tiles of 32, and consecutive tiles to one share, a workgroup's work.  Inside a share
+// tile k goes to wave k mod (waves), so every sum is taken in a fixed order.  A row in one share is finished there; otherwise each
+// leaves a partial (m, l, o) in slot share + row, and mx_merge_kernel combines a row's partials in share order.
 //
 // Per wave and tile, codes and scales go from memory straight into LDS (global_load_lds): d/16 lanes fetch the d bytes of a
-// position as one piece, 1 KiB per instruction, and the list words and page numbers that tell where they lie come the same way, two and
-// four tiles earlier.  A wave holds three tiles: one in use, two on their way, 68 KiB per CU at d = 128, and waits by the
-// number of requests behind the ones it needs.  (Requests straight into registers, one tile ahead: a tile took as long as a trip
-// to memory; 8 dense sequences of up to 32768 positions 45 us.)  From LDS,
+// position as one piece, 1 KiB per instruction, and the list words and page numbers that tell where they lie come the same way, one trip
+// each ahead.  A wave holds three tiles, one in use and two on their way (12 waves: two), 70 to 100 KiB under way per CU at d = 128, and
+// waits by the number of requests behind the ones it needs.  (Requests straight into registers, one tile ahead: a tile took as long as a trip
+// to memory; 8 dense sequences of up to 32768 positions 45 us / 39.)  From LDS,
 //   keys     lane (p, g) = (lane % 16, lane / 16) takes a quarter of the codes of positions p and 16 + p, d/4 elements that lie
 //            in one block, so one scale serves all of a lane's conversions.  The contraction runs over the elements in the order
 //            the lanes hold them; the queries are laid out to match.
@@ -41,7 +40,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// Waves per workgroup, and tiles of a wave in use and on their way.
+// Waves per workgroup, and tiles of a wave in use and on their way.  Up to 64 rows a workgroup has a CU to itself: 12 waves where registers
+// allow it (one query tile; 8 dense sequences of up to 32768 positions 39 us / 44 with 8), else 8.  Beyond, two workgroups of 4 share it,
+// so that one works while the other changes rows (64 sequences of 8 kv heads, two query tiles: 240 us / 250 with one of 8).
 template <int NQ, bool FEW> struct Waves {
     static constexpr int N = !FEW ? 4 : NQ == 1 ? 12 : 8, DEPTH = N == 12 ? 2 : 3, THREADS = N * 64;
 };
@@ -225,8 +226,8 @@ __device__ __forceinline__ int wave_last(int v) { return __builtin_amdgcn_readla
 // How the work is cut.  FEW, up to 64 rows, which every wave holds one to a lane: each row goes to whole workgroups, as many as its
 // tiles take at `size` tiles each, the smallest size at which the workgroups suffice (small ones in whole rounds of the waves); the
 // row's tiles are dealt to them evenly.  Otherwise the tiles of all rows form one line with SEG_COST ahead of every row, and every
-// workgroup takes an equal stretch of it.  Picking up a second row costs a workgroup about 8 us, the time of 20 tiles: 64 rows of 7500
-// positions 42 us in equal stretches / 36 in whole workgroups.
+// workgroup takes an equal stretch of it (10 or 20 tiles: 240 us both, 64 sequences as above).  Whole workgroups need no tables and pick up
+// one row: 64 rows of 7500 positions 23 us / 28 in equal stretches (one query tile), 31 / 38 (two); 8 rows of 1900 13.9 / 16.1.
 template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves<NQ, FEW>::THREADS), 2) void mx_attn_kernel(LENGTHS_PARAMS, MxArgs a)
 {
     typedef Geo<D> G;
@@ -618,7 +619,7 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
         }
         __syncthreads();
 
-        // The eight waves' states, one query tile at a time.
+        // The waves' states, one query tile at a time.
         const bool alone = t0 == 0 && t1 == row_tiles && !a.tail;
         float *slot_o = a.slots + (size_t)(me + r) * NQ * 16 * (D + 2), *slot_ml = slot_o + NQ * 16 * D;
 #pragma unroll
