@@ -117,6 +117,21 @@ def test_lists_of_very_different_lengths(d, page, new):
     c.check(kept, lists=lists, counts=counts)
 
 
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 0), ("f16", 128, 16), ("bf16", 64, 16), ("f16", 64, 0)])
+@pytest.mark.parametrize("G,T", [(1, 1), (4, 5), (5, 8), (8, 8)])
+def test_more_than_64_rows(dtype, d, page, G, T):
+    """One to four query tiles where workgroups take stretches of the rows' tiles: rows of nothing, of one position, of many."""
+    B, H, n = 10, 7, 700
+    c = Case(B, G * H, H, T, d, n, dtype, page=page, new=(T == 5), seed=G + T)
+    rng = np.random.default_rng(G * T)
+    kept = [[np.sort(rng.permutation(n)[:rng.choice([0, 1, 31, 33, 200, 700])]) for _ in range(H)] for _ in range(B)]
+    lists, counts = np.full((B * H, n), -1, dtype=np.int32), np.zeros(B * H, dtype=np.int32)
+    for r in range(B * H):
+        x = kept[r // H][r % H]
+        lists[r, :len(x)], counts[r] = x, len(x)
+    c.check(kept, lists=lists, counts=counts)
+
+
 @pytest.mark.parametrize("chunk", [2, 16, 128])
 @pytest.mark.parametrize("page", [0, 16])
 def test_chunk_lists(chunk, page):
