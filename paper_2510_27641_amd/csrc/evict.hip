@@ -5,6 +5,10 @@
 // lowest of all, tokens that have to stay highest of all); the K slots that stay are those above the K-th largest key, which radix
 // passes over the keys find, and the lowest slots among those that equal it.  What stays beyond the new length moves into the
 // holes below it: as many bytes as slots dropped there, instead of a new copy of everything behind the first hole.
+//
+// Bound by memory where rows are long, by the chain of launches and of radix passes where they are short.  64 rows of 32768 slots, 20
+// entries each, a quarter stays, 4-bit cache: sums 38 us (0.2 GB, 5.3 TB/s), selection in slices 4.7 + 4.9 + 13.6 + 7.9, moves 29 us; 4
+// sequences of up to 131072, half stays, 8 bf16 heads: moves 93 us (4.4 TB/s; a plain copy 4.8).  64 rows of 8197: 8.3 + 12.8 + 4.0 us.
 #include "mx.h"
 
 #include <algorithm>

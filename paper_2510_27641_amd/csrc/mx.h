@@ -8,8 +8,6 @@ namespace specattn {
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
-constexpr int MX_BLOCK = 32;              // elements under one scale
-
 // Where the rows of a cache lie; offsets in bytes.
 struct MxCache {
     uint8_t *codes, *scales;

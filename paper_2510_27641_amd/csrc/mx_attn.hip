@@ -117,9 +117,6 @@ template <int N> __device__ __forceinline__ void wait_requests() { asm volatile(
 __device__ __forceinline__ uint32_t lds_offset(const void *p) { return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p); }
 
 __device__ __forceinline__ uint32_t bits(bf16x2 x) { return __builtin_bit_cast(uint32_t, x); }
-__device__ __forceinline__ uint32_t to_bf16(float a, float b) { return bits(__builtin_convertvector(f32x2{a, b}, bf16x2)); }
-__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ f32x4 mfma(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c)
 {
     const u32x4 x = {a[0], a[1], a[2], a[3]}, y = {b[0], b[1], b[2], b[3]};
@@ -179,7 +176,7 @@ struct MxArgs {
     uint32_t codes_n, codes_page, scales_n, scales_page;
     FastDivisor per_h, per_t;
     int max_pages, page_shift, last_page, last_slot;
-    int H_q, H_kv, T, first_head, heads, queries, chunk_shift;
+    int H_q, H_kv, T, first_head, queries, chunk_shift;
     int paged, tail, dtype;               // paged: 1 by a page table, 2 by the list itself
     float to_log2;
     const uint16_t *k_new, *v_new;        // (the merge alone)
@@ -847,8 +844,7 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
     a.k_new = static_cast<const uint16_t *>(c.k_new); a.v_new = static_cast<const uint16_t *>(c.v_new);
     for (int first = 0; first < G; first += per) {
         a.first_head = first;
-        a.heads = std::min(per, G - first);
-        a.queries = a.heads * c.T;
+        a.queries = std::min(per, G - first) * c.T;
         const int nq = (a.queries + 15) / 16;
         for (int row0 = 0; row0 < rows; row0 += MAX_ROWS) {
             int here = std::min(MAX_ROWS, rows - row0), at = row0;
