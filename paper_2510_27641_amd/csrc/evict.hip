@@ -8,7 +8,7 @@
 //
 // Bound by memory where rows are long, by the chain of launches and of radix passes where they are short.  64 rows of 32768 slots, 20
 // entries each, a quarter stays, 4-bit cache: sums 38 us (0.2 GB, 5.3 TB/s), selection in slices 4.7 + 4.9 + 13.6 + 7.9, moves 29 us; 4
-// sequences of up to 131072, half stays, 8 bf16 heads: moves 93 us (4.4 TB/s; a plain copy 4.8).  64 rows of 8197: 8.3 + 12.8 + 4.0 us.
+// sequences of up to 131072, half stays, 8 bf16 heads: moves 93 us (4.4 TB/s; a plain copy 4.8).  64 rows of 8197: 7.3 + 12.8 + 4.1 us.
 #include "mx.h"
 
 #include <algorithm>
@@ -62,14 +62,18 @@ template <int PLACES, int WIDTH, int GAP> __device__ __forceinline__ void add_sl
     const int64_t row = b * e.row_stride_b + h * e.row_stride_h;
     const int next = e.next_positions[b];
     double sum[PLACES][WIDTH];
-    int at[PLACES];
-    // (behind the row: its last place again, not written; with WIDTH > 1 rows are padded to whole places)
+    int at[PLACES], place[PLACES][WIDTH];
+    // (behind the row: its last place again, not written; with WIDTH > 1 rows are padded to whole places.  Places in the text are asked for
+    // here, not where they are used: a trip to memory less, 1 us of 8.2 for 64 rows of 8197.)
 #pragma unroll
     for (int k = 0; k < PLACES; ++k) {
         at[k] = min(first + k * GAP, (len - 1) / WIDTH * WIDTH);
         const Wide x = *reinterpret_cast<const Wide *>(e.scores + row + at[k]);
 #pragma unroll
-        for (int i = 0; i < WIDTH; ++i) sum[k][i] = e.decay * (double)x[i];
+        for (int i = 0; i < WIDTH; ++i) {
+            sum[k][i] = e.decay * (double)x[i];
+            place[k][i] = e.positions[row + min(first + k * GAP + i, len - 1)];
+        }
     }
     const float *probs = e.probs + b * e.probs_stride_b + (int64_t)h * l.members * e.probs_stride_row;
     constexpr int TRIP = 4;                                   // rows requested together
@@ -93,8 +97,7 @@ template <int PLACES, int WIDTH, int GAP> __device__ __forceinline__ void add_sl
             const int j = first + k * GAP + i;
             if (j >= len) continue;
             const float score = (float)sum[k][i];
-            const int64_t place = e.positions[row + j];
-            const bool stays = place < e.sinks || place >= (int64_t)next - e.recent;
+            const bool stays = place[k][i] < e.sinks || place[k][i] >= (int64_t)next - e.recent;
             e.scores_out[row + j] = score;
             l.keys[(int64_t)r * l.stride + j] = stays ? KEY_STAYS : key_of(score);
         }
