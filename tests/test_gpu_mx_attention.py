@@ -225,6 +225,17 @@ def test_key_blocks_of_any_scale_and_rows_of_zeros(dtype, d):
     c.check([[np.arange(45)]])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp16_queries_below_the_normal_numbers(d):
+    """Queries of a few units of 2^-24 against keys large enough for them to matter, single blocks of which lie 2^-12 lower."""
+    c = Case(2, 8, 2, 4, d, 90, "f16", seed=37, spread=1)
+    c.q = (c.q.float() * 2.0 ** -18).half()
+    assert (c.q.abs() < 2.0 ** -14).all() and (c.q != 0).any()
+    c.scales[..., :d // 32] += 17
+    c.scales[..., 1] -= 12
+    c.check([[np.arange(90)] * 2] * 2)
+
+
 def test_nan_keys_with_fp16_queries():
     c = Case(1, 4, 2, 2, 128, 70, "f16", seed=19)
     c.scales[0, 1, 69, 3] = 255
