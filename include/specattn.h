@@ -364,8 +364,9 @@ typedef struct specattn_mx_cache {
     uint8_t *codes, *scales;
     int64_t codes_stride_b, codes_stride_h, codes_stride_n, codes_stride_page;       /* _b contiguous, _page paged */
     int64_t scales_stride_b, scales_stride_h, scales_stride_n, scales_stride_page;
-    const int32_t *page_table;   /* [B][max_pages_per_seq] page ids, or NULL = contiguous */
-    int32_t page_size, max_pages_per_seq, num_pages;     /* page_size: a power of two */
+    const int32_t *page_table;   /* [B][max_pages_per_seq] page ids, or NULL = contiguous (for indices_are_physical: a pool) */
+    int32_t page_size, max_pages_per_seq, num_pages;     /* page_size: a power of two; num_pages: 0 for a contiguous cache.
+                                    A pool (num_pages > 0) without a page table takes indices_are_physical alone (SPECATTN_EINVAL) */
     int32_t B, H_kv, n_max, d;   /* n_max: slots per sequence; d: 64 or 128 */
 } specattn_mx_cache;
 

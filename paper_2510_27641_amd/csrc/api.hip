@@ -234,6 +234,8 @@ specattn_status check_mx_cache(const specattn_mx_cache *c, bool pool)
     if (c->B <= 0 || c->H_kv <= 0 || c->n_max <= 0 || c->d <= 0) { set_error("the cache's sizes must be positive"); return SPECATTN_EINVAL; }
     if (c->d != 64 && c->d != 128) { set_error("d must be 64 or 128"); return SPECATTN_ESHAPE; }
     if ((int64_t)c->B * c->H_kv > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
+    // (its rows do not lie at _stride_b and slot * _stride_n: they would be taken from, and put, where others are)
+    if (!pool && c->num_pages > 0) { set_error("a pool without a page table takes lists of pool slots alone (num_pages is 0 for a contiguous cache)"); return SPECATTN_EINVAL; }
     if (pool) {
         const specattn_status st = check_pages(c->page_table, c->page_size, c->max_pages_per_seq, c->n_max);
         if (st != SPECATTN_OK) return st;
