@@ -386,11 +386,12 @@ typedef struct specattn_mx_rows_args {
  * once).  The scale of a block is 2^X with X = floor(log2(largest magnitude)) - 2, between -127 and 125, and each element goes to
  * the nearest of its block's values (ties to the even code, magnitudes beyond 6 to 6, signs kept, of zeros too); a block of
  * zeros gets scale byte 0, one with an infinity or NaN scale byte 255.  Slots that no row goes to are left as they were.
- * Rows that lie beyond n_max or in a page outside the pool are left out.  Two rows must not go to the same slot.
+ * Rows that lie beyond n_max or in a page outside the pool are left out.  Two rows must not go to the same slot: a cache whose
+ * strides let rows share bytes is refused (SPECATTN_ESHAPE), and slots that rows go to lie in pages of one sequence alone.
  *
  * specattn_mx_load: the values of slots in the type of k and v (rounded to nearest even where it cannot hold them; a
  * magnitude that fp16 cannot hold becomes infinite).  Rows at and beyond counts[b] are left as they were, and so are rows of
- * slots beyond n_max or in a page outside the pool.
+ * slots beyond n_max or in a page outside the pool.  Rows of k and v must not share bytes (SPECATTN_ESHAPE).
  */
 specattn_status specattn_mx_store(const specattn_mx_rows_args *args, void *stream);
 specattn_status specattn_mx_load(const specattn_mx_rows_args *args, void *stream);

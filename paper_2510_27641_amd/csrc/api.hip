@@ -228,6 +228,23 @@ specattn_status check_pages(const int32_t *page_table, int page_size, int max_pa
     return SPECATTN_OK;
 }
 
+// Whether rows of `bytes` bytes at these strides share any: dimension by dimension from the smallest stride up, each has to lie beyond all that
+// the ones before it reach.
+struct Dim { int64_t size; __int128 stride; };
+bool rows_overlap(Dim a, Dim b, Dim c, int64_t bytes)
+{
+    Dim dims[] = {a, b, c};
+    for (Dim &d : dims) d.stride = d.stride < 0 ? -d.stride : d.stride;
+    std::sort(dims, dims + 3, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
+    __int128 reach = bytes;
+    for (const Dim &d : dims) {
+        if (d.size <= 1) continue;
+        if (d.stride < reach) return true;
+        reach += (d.size - 1) * d.stride;
+    }
+    return false;
+}
+
 specattn_status check_mx_cache(const specattn_mx_cache *c, bool pool)
 {
     if (!c->codes || !c->scales) { set_error("codes and scales must not be NULL"); return SPECATTN_EINVAL; }
@@ -266,17 +283,27 @@ MxCache make_mx_cache(const specattn_mx_cache *c, bool pool)
     return m;
 }
 
-specattn_status check_mx_rows(const specattn_mx_rows_args *r)
+specattn_status check_mx_rows(const specattn_mx_rows_args *r, bool store)
 {
     if (!r) { set_error("rows args are NULL"); return SPECATTN_EINVAL; }
-    const specattn_status st = check_mx_cache(&r->cache, r->cache.page_table != nullptr);
+    const specattn_mx_cache *c = &r->cache;
+    const bool pool = c->page_table != nullptr;
+    const specattn_status st = check_mx_cache(c, pool);
     if (st != SPECATTN_OK) return st;
+    // what is written must not share bytes: the rows of the cache here, those of k and v below
+    const int64_t outer = pool ? c->num_pages : c->B, inner = pool ? c->page_size : c->n_max;
+    if (store && (rows_overlap({outer, pool ? c->codes_stride_page : c->codes_stride_b}, {c->H_kv, c->codes_stride_h}, {inner, c->codes_stride_n}, c->d) ||
+                  rows_overlap({outer, pool ? c->scales_stride_page : c->scales_stride_b}, {c->H_kv, c->scales_stride_h}, {inner, c->scales_stride_n}, c->d / 16))) {
+        set_error("rows of the cache share bytes");
+        return SPECATTN_ESHAPE;
+    }
     if (!r->k || !r->v) { set_error("k and v must not be NULL"); return SPECATTN_EINVAL; }
     if (r->T <= 0) { set_error("T must be positive"); return SPECATTN_EINVAL; }
     if (r->dtype != SPECATTN_F32 && r->dtype != SPECATTN_BF16 && r->dtype != SPECATTN_F16) { set_error("unknown dtype %d", (int)r->dtype); return SPECATTN_EUNSUPPORTED; }
-    if (!aligned(r->k, 16) || !aligned(r->v, 16)) { set_error("k and v must be 16-byte aligned"); return SPECATTN_EALIGN; }
     const int64_t es = r->dtype == SPECATTN_F32 ? 4 : 2;
     if ((r->stride_b * es) % 16 || (r->stride_h * es) % 16 || (r->stride_t * es) % 16) { set_error("strides must be multiples of 16 bytes"); return SPECATTN_EALIGN; }
+    if (!store && rows_overlap({c->B, r->stride_b}, {c->H_kv, r->stride_h}, {r->T, r->stride_t}, c->d)) { set_error("rows of k and v share bytes"); return SPECATTN_ESHAPE; }
+    if (!aligned(r->k, 16) || !aligned(r->v, 16)) { set_error("k and v must be 16-byte aligned"); return SPECATTN_EALIGN; }
     return SPECATTN_OK;
 }
 
@@ -678,7 +705,7 @@ size_t specattn_workspace_size(const specattn_select_args *sel, const specattn_a
 specattn_status specattn_mx_store(const specattn_mx_rows_args *args, void *stream)
 {
     clear_error();
-    const specattn_status st = check_mx_rows(args);
+    const specattn_status st = check_mx_rows(args, true);
     if (st != SPECATTN_OK) return st;
     return launch_mx_store(make_mx_rows(args), static_cast<hipStream_t>(stream));
 }
@@ -686,7 +713,7 @@ specattn_status specattn_mx_store(const specattn_mx_rows_args *args, void *strea
 specattn_status specattn_mx_load(const specattn_mx_rows_args *args, void *stream)
 {
     clear_error();
-    const specattn_status st = check_mx_rows(args);
+    const specattn_status st = check_mx_rows(args, false);
     if (st != SPECATTN_OK) return st;
     return launch_mx_load(make_mx_rows(args), static_cast<hipStream_t>(stream));
 }

@@ -1,4 +1,4 @@
-"""Layouts that the calls around the 4-bit cache and the eviction refuse: a pool taken for a contiguous cache.  Found on the host, before
+"""Layouts that the calls around the 4-bit cache and the eviction refuse: a pool taken for a contiguous cache, rows that share bytes.  Found on the host, before
 anything is launched (no GPU needed)."""
 import ctypes as C
 
@@ -23,3 +23,37 @@ def test_a_pool_without_a_page_table_takes_lists_of_pool_slots_alone(kw):
             _refused(fn, args, sa.EINVAL)
     # and lists of pool slots are taken (refused for their workspace, behind every other check)
     _refused(lib.specattn_mx_decode_attn, _attn(sa.mx_cache(codes, scales, B=2), indices_are_physical=1), sa.EWORKSPACE)
+
+
+OVERLAPPING_CACHES = [
+    (False, dict(codes_stride_b=0)), (False, dict(scales_stride_b=0)), (False, dict(codes_stride_h=0)), (False, dict(scales_stride_h=0)),
+    (False, dict(codes_stride_b=4 * 512 * 128 - 16)), (False, dict(scales_stride_h=512 * 8 - 4)), (False, dict(codes_stride_h=64)),
+    (True, dict(codes_stride_h=16 * 128 - 16)), (True, dict(scales_stride_h=0)), (True, dict(codes_stride_page=16 * 128)), (True, dict(scales_stride_page=8)),
+]
+
+
+@pytest.mark.parametrize("paged,kw", OVERLAPPING_CACHES)
+def test_rows_do_not_go_into_a_cache_whose_rows_share_bytes(paged, kw):
+    """Stores race there; reading such a cache (a prompt that all sequences share) is no fault."""
+    lib = sa.load()
+    cache = _cache(paged, **kw)
+    _refused(lib.specattn_mx_store, _rows(cache))
+    _refused(lib.specattn_mx_decode_attn, _attn(cache), sa.EWORKSPACE)
+
+
+@pytest.mark.parametrize("kw", [dict(stride_b=0), dict(stride_h=0), dict(stride_t=0), dict(stride_t=64), dict(stride_h=6 * 128), dict(stride_b=-8 * 128), dict(stride_h=-120)])
+def test_rows_do_not_come_out_into_rows_that_share_bytes(kw):
+    _refused(sa.load().specattn_mx_load, _rows(_cache(), **kw))
+
+
+def test_layouts_without_shared_bytes_are_taken():
+    """Heads inside positions, pitched rows, dimensions of size 1 with any stride: refused for what is looked at behind the layout alone."""
+    lib = sa.load()
+    one = _cache(B=1, codes_stride_b=0, scales_stride_b=0, H_kv=1, codes_stride_h=0, scales_stride_h=0)
+    inside = _cache(codes_stride_n=4 * 128, codes_stride_h=128, scales_stride_n=4 * 8, scales_stride_h=8)
+    pitched = _cache(codes_stride_n=144, codes_stride_h=512 * 144, codes_stride_b=4 * 512 * 144)
+    for cache in (one, inside, pitched, _cache(True)):
+        for fn in (lib.specattn_mx_store, lib.specattn_mx_load):
+            _refused(fn, _rows(cache, stride_b=7 * 8 * 128, stride_t=8 * 128, stride_h=128, k=0x40008), sa.EALIGN)
+    # rows that are read may be the same for all
+    _refused(lib.specattn_mx_store, _rows(_cache(), stride_b=0, stride_h=0, stride_t=0, v=0x40008), sa.EALIGN)
