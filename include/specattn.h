@@ -375,7 +375,7 @@ typedef struct specattn_mx_rows_args {
     specattn_mx_cache cache;
     void *k, *v;                 /* [B][H_kv][T][d]; read by specattn_mx_store, written by specattn_mx_load */
     specattn_dtype dtype;        /* of k and v */
-    int32_t T;                   /* rows per sequence */
+    int32_t T;                   /* rows per sequence, at most 2^30 */
     int64_t stride_b, stride_h, stride_t;                /* elements, of k and v alike; last dim contiguous; 16-byte multiples */
     const int32_t *starts;       /* [B] first slot of each sequence, or NULL for 0 */
     const int32_t *counts;       /* [B] rows of each sequence (at most T are taken), or NULL for T */

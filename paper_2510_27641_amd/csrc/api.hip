@@ -299,6 +299,7 @@ specattn_status check_mx_rows(const specattn_mx_rows_args *r, bool store)
     }
     if (!r->k || !r->v) { set_error("k and v must not be NULL"); return SPECATTN_EINVAL; }
     if (r->T <= 0) { set_error("T must be positive"); return SPECATTN_EINVAL; }
+    if (r->T > (1 << 30)) { set_error("more than 2^30 rows per sequence"); return SPECATTN_ESHAPE; }       // (counted in 31 bits, whole workgroups of them)
     if (r->dtype != SPECATTN_F32 && r->dtype != SPECATTN_BF16 && r->dtype != SPECATTN_F16) { set_error("unknown dtype %d", (int)r->dtype); return SPECATTN_EUNSUPPORTED; }
     const int64_t es = r->dtype == SPECATTN_F32 ? 4 : 2;
     if ((r->stride_b * es) % 16 || (r->stride_h * es) % 16 || (r->stride_t * es) % 16) { set_error("strides must be multiples of 16 bytes"); return SPECATTN_EALIGN; }

@@ -57,3 +57,11 @@ def test_layouts_without_shared_bytes_are_taken():
             _refused(fn, _rows(cache, stride_b=7 * 8 * 128, stride_t=8 * 128, stride_h=128, k=0x40008), sa.EALIGN)
     # rows that are read may be the same for all
     _refused(lib.specattn_mx_store, _rows(_cache(), stride_b=0, stride_h=0, stride_t=0, v=0x40008), sa.EALIGN)
+
+
+@pytest.mark.parametrize("T", [2 ** 30 + 1, 2 ** 31 - 40, 2 ** 31 - 1])
+def test_more_rows_than_are_counted_in_31_bits_are_refused(T):
+    """The kernels count rows of whole workgroups past the last one."""
+    lib = sa.load()
+    for fn in (lib.specattn_mx_store, lib.specattn_mx_load):
+        _refused(fn, _rows(_cache(), T=T, stride_h=2 ** 31 * 128, stride_b=2 ** 33 * 128))
