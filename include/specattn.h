@@ -486,7 +486,7 @@ size_t specattn_evict_workspace_size(const specattn_evict_args *args);     /* 0 
 #define SPECATTN_MAX_PLANES 8
 typedef struct specattn_move_plane {
     void *data;                  /* contiguous [B][H_kv][n_max][row_bytes] or pool [num_pages][H_kv][page_size][row_bytes] */
-    int64_t stride_b, stride_h, stride_n, stride_page;   /* bytes; _b contiguous, _page paged */
+    int64_t stride_b, stride_h, stride_n, stride_page;   /* bytes; _b contiguous, _page paged; not negative, no two rows may share bytes */
     int32_t row_bytes;           /* a multiple of 4 up to 8192; data and strides are multiples of the largest of 16, 8, 4 dividing it */
     int32_t H_kv;                /* a multiple of H */
     int32_t num_pages;           /* paged: pages of this pool */

@@ -430,7 +430,13 @@ specattn_status check_move(const specattn_move_args *m)
         if (m->page_table && (p->num_pages <= 0 || p->stride_page <= 0)) { set_error("plane %d needs num_pages and a page stride", i); return SPECATTN_ESHAPE; }
         const int unit = p->row_bytes % 16 == 0 ? 16 : p->row_bytes % 8 == 0 ? 8 : 4;
         const int64_t outer = m->page_table ? p->stride_page : p->stride_b;
+        if (p->stride_h < 0 || outer < 0) { set_error("strides of plane %d must not be negative", i); return SPECATTN_ESHAPE; }      // (offsets below 0 mean no such slot)
         if (!aligned(p->data, unit) || p->stride_h % unit || p->stride_n % unit || outer % unit) { set_error("data and strides of plane %d must be multiples of %d bytes", i, unit); return SPECATTN_EALIGN; }
+    }
+    for (int i = 0; i < m->num_planes; ++i) {
+        const specattn_move_plane *p = &m->planes[i];
+        const Dim outer = m->page_table ? Dim{p->num_pages, p->stride_page} : Dim{m->B, p->stride_b}, inner = {m->page_table ? m->page_size : m->n_max, p->stride_n};
+        if (rows_overlap(outer, {p->H_kv, p->stride_h}, inner, p->row_bytes)) { set_error("rows of plane %d share bytes", i); return SPECATTN_ESHAPE; }
     }
     return SPECATTN_OK;
 }

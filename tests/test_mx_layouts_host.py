@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2510_27641_amd import binding as sa
-from test_mx_host import _attn, _cache, _rows
+from test_mx_host import _attn, _cache, _evict, _move, _rows
 
 
 def _refused(fn, args, status=sa.ESHAPE):
@@ -65,3 +65,11 @@ def test_more_rows_than_are_counted_in_31_bits_are_refused(T):
     lib = sa.load()
     for fn in (lib.specattn_mx_store, lib.specattn_mx_load):
         _refused(fn, _rows(_cache(), T=T, stride_h=2 ** 31 * 128, stride_b=2 ** 33 * 128))
+
+
+@pytest.mark.parametrize("paged,plane", [
+    (False, (("stride_b", -8 * 512 * 256),)), (False, (("stride_h", -512 * 256),)), (True, (("stride_h", -16 * 256),)),
+    (False, (("stride_b", 0),)), (False, (("stride_h", 0),)), (False, (("stride_h", 512 * 256 - 16),)), (True, (("stride_h", 16),)), (True, (("stride_page", 16 * 256),)),
+])
+def test_moves_are_refused_in_planes_that_run_backwards_or_whose_rows_share_bytes(paged, plane):
+    _refused(sa.load().specattn_evict_move, _move(paged, plane))
