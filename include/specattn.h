@@ -464,7 +464,7 @@ typedef struct specattn_evict_args {
     const int32_t *positions;    /* [B][H][n_max] place in the text of the token in each slot; same strides */
     float *scores_out;           /* may be `scores` */
     int32_t *positions_out;      /* may be `positions` */
-    int64_t row_stride_b, row_stride_h;                  /* elements, of the four arrays above */
+    int64_t row_stride_b, row_stride_h;                  /* elements, of the four arrays above; rows share no entries */
     const int32_t *seq_lens;     /* [B] occupied slots, or NULL for n_max */
     const int32_t *next_positions;   /* [B] place in the text of the sequence's next token */
     double decay;                /* in [0, 1] */

@@ -228,7 +228,7 @@ specattn_status check_pages(const int32_t *page_table, int page_size, int max_pa
     return SPECATTN_OK;
 }
 
-// Whether rows of `bytes` bytes at these strides share any: dimension by dimension from the smallest stride up, each has to lie beyond all that
+// Whether rows of `bytes` bytes (or elements) at these strides share any: dimension by dimension from the smallest stride up, each has to lie beyond all that
 // the ones before it reach.
 struct Dim { int64_t size; __int128 stride; };
 bool rows_overlap(Dim a, Dim b, Dim c, int64_t bytes)
@@ -401,6 +401,7 @@ specattn_status check_evict(const specattn_evict_args *e)
     }
     if ((int64_t)e->B * e->H > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
     if (e->row_stride_h < e->n_max || e->row_stride_b < e->n_max) { set_error("row strides are smaller than n_max"); return SPECATTN_ESHAPE; }
+    if (rows_overlap({e->B, e->row_stride_b}, {e->H, e->row_stride_h}, {1, 0}, e->n_max)) { set_error("rows of the scores share entries"); return SPECATTN_ESHAPE; }
     if (e->sinks < 0 || e->recent < 0 || (int64_t)e->sinks + e->recent > e->budget) { set_error("sinks and recent must not be negative, nor exceed the budget together"); return SPECATTN_ESHAPE; }
     if (e->move_capacity < 1 || e->move_capacity < std::min(e->budget, e->n_max - e->budget)) { set_error("move_capacity must be at least 1 and hold min(budget, n_max - budget) moves"); return SPECATTN_ESHAPE; }
     if (e->move_stride_row < e->move_capacity) { set_error("move_stride_row is smaller than move_capacity"); return SPECATTN_ESHAPE; }

@@ -73,3 +73,15 @@ def test_more_rows_than_are_counted_in_31_bits_are_refused(T):
 ])
 def test_moves_are_refused_in_planes_that_run_backwards_or_whose_rows_share_bytes(paged, plane):
     _refused(sa.load().specattn_evict_move, _move(paged, plane))
+
+
+@pytest.mark.parametrize("kw", [dict(row_stride_b=512), dict(row_stride_b=4 * 512 - 1), dict(row_stride_b=1000, row_stride_h=600)])
+def test_score_rows_that_share_entries_are_refused(kw):
+    lib = sa.load()
+    _refused(lambda args, stream: lib.specattn_evict_select(args, None, 0, stream), _evict(**kw))
+
+
+def test_score_rows_of_any_order_are_taken():
+    lib = sa.load()
+    for kw in (dict(row_stride_b=512, row_stride_h=2 * 512), dict(row_stride_b=600, row_stride_h=5000), dict(B=1, row_stride_b=512), dict(H=1, row_stride_h=512, row_stride_b=512)):
+        _refused(lambda args, stream: lib.specattn_evict_select(args, None, 0, stream), _evict(**kw), sa.EWORKSPACE)
