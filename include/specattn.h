@@ -452,7 +452,9 @@ size_t specattn_mx_workspace_size(const specattn_mx_attn_args *args);      /* 0 
  *
  * specattn_evict_move applies the moves to the rows of any caches of the sequences, in place: keys and values in any type,
  * codes and scales, the draft model's cache.  The kv heads h*H_kv/H .. (h+1)*H_kv/H - 1 of a plane follow row h.  Moves that
- * lead outside [0, n_max) or into a page outside the pool are left out.
+ * lead outside [0, n_max) or into a page outside the pool are left out.  Rows move where they lie, so that no page may stand twice in the
+ * tables, in one sequence's or in two sequences' (a prompt they share), unless none of its slots is moved to: give the sequences
+ * pages of their own before slots are moved there.  Two planes, too, must not share rows.
  */
 typedef struct specattn_evict_args {
     const float *probs;          /* [B][H_draft][S][n_max] fp32: row (b, x, s) starts at b*probs_stride_b +

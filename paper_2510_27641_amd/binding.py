@@ -482,7 +482,8 @@ def evict_args(probs: Optional[torch.Tensor], scores: torch.Tensor, positions: t
 
 def move_args(move_src: torch.Tensor, move_dst: torch.Tensor, move_counts: torch.Tensor, planes, *, B: int,
               page_table: Optional[torch.Tensor] = None, n_max: Optional[int] = None) -> MoveArgs:
-    """planes: up to MAX_PLANES tensors [B,H_kv,n,.] or, with page_table [B,max_pages] int32, pools [pages,H_kv,page_size,.], any type."""
+    """planes: up to MAX_PLANES tensors [B,H_kv,n,.] or, with page_table [B,max_pages] int32, pools [pages,H_kv,page_size,.], any type.
+    Pages that slots are moved to must belong to one sequence alone."""
     assert move_src.dtype == move_dst.dtype == torch.int32 and move_src.shape == move_dst.shape and move_src.stride() == move_dst.stride()
     assert move_src.dim() == 2 and move_src.stride(1) == 1 and move_src.shape[0] % B == 0
     a = MoveArgs()
