@@ -379,7 +379,8 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
         auto list_at = [&](int i) { return list + (list_rank(i) >> a.chunk_shift); };
         auto slot_of = [&](int i, int word) -> int {
             if (!listed) return list_rank(i);                     // (below the length: inside the cache)
-            if (a.chunk_shift) word = (word << a.chunk_shift) | (list_rank(i) & ((1 << a.chunk_shift) - 1));
+            // (a number beyond the last chunk has no position in 32 bits where it is large)
+            if (a.chunk_shift) word = word > a.last_slot >> a.chunk_shift ? INT32_MAX : word < 0 ? word : (word << a.chunk_shift) | (list_rank(i) & ((1 << a.chunk_shift) - 1));
             return min(max(word, 0), a.last_slot);
         };
         auto request_words = [&](int i, int at) { if (listed) request4(list_at(i), words_lds + at * 256); };
