@@ -837,7 +837,7 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
     a.scales_n = (uint32_t)(l.c.scales_n >> 2); a.scales_page = (uint32_t)(l.c.scales_page >> 2);
     a.per_h = FastDivisor(c.H_kv); a.per_t = FastDivisor(c.T);
     a.max_pages = l.c.max_pages; a.page_shift = l.c.page_shift; a.last_page = l.c.num_pages - 1;
-    a.last_slot = c.indices_are_physical ? INT32_MAX : c.n_max - 1;
+    a.last_slot = c.indices_are_physical ? (int)std::min<int64_t>(((int64_t)l.c.num_pages << l.c.page_shift) - 1, INT32_MAX) : c.n_max - 1;
     a.H_q = c.H_q; a.H_kv = c.H_kv; a.T = c.T;
     a.chunk_shift = c.chunk_shift;
     a.paged = l.c.page_table ? 1 : c.indices_are_physical ? 2 : 0; a.tail = c.k_new != nullptr; a.dtype = c.dtype;

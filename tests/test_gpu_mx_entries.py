@@ -21,3 +21,21 @@ def test_chunk_numbers_far_outside(page, d):
     # (a negative number's positions lie below 0)
     kept = np.concatenate([np.zeros(16, dtype=np.int64) if u < 0 else at(int(u)) for u in lists[0].astype(np.int64)])
     c.check([[kept]], lists=lists, counts=np.array([10], dtype=np.int32), chunk=chunk)
+
+
+@pytest.mark.parametrize("page", [1, 16])
+def test_pool_slots_outside_the_pool(page):
+    B, H, d, n = 1, 2, 128, 64
+    c = Case(B, 4, H, 2, d, n, page=page, seed=43)
+    slots = c.codes.shape[0] * page
+    entries = np.array([[0, slots - 1, slots, slots + 3, 10 ** 6 + 5, 2 ** 31 - 1, -1, -7, 5, 9]] * H, dtype=np.int32)
+    k, v = (x.transpose(1, 0, 2, 3).reshape(1, H, slots, d) for x in ref.cache_values(c.codes, c.scales))
+    kept = np.clip(entries[0].astype(np.int64), 0, slots - 1)
+    want, _, tol = ref.attention(c.q.double().numpy(), k, v, [[kept] * H], d ** -0.5)
+    codes, scales, q = torch.from_numpy(c.codes).cuda(), torch.from_numpy(c.scales).cuda(), c.q.cuda()
+    out, idx, cnt = torch.empty((B, 4, 2, d), device="cuda"), torch.from_numpy(entries).cuda(), torch.full((H,), 10, dtype=torch.int32, device="cuda")
+    args = sa.mx_attn_args(q, sa.mx_cache(codes, scales, B=B), out=out, indices=idx, counts=cnt, indices_are_physical=True)
+    ws = sa.alloc_workspace(sa.specattn_mx_workspace_size(args))
+    args.workspace, args.workspace_bytes = ws.data_ptr(), ws.numel()
+    sa.specattn_mx_decode_attn(args)
+    assert (np.abs(out.cpu().double().numpy() - want) <= tol[..., None]).all()
