@@ -176,6 +176,7 @@ struct MxArgs {
     uint32_t codes_n, codes_page, scales_n, scales_page;
     FastDivisor per_h, per_t;
     int max_pages, page_shift, last_page, last_slot;
+    int end_chunk;                        // the first chunk number behind the cache; larger ones have no position in 32 bits
     int H_q, H_kv, T, first_head, queries, chunk_shift;
     int paged, tail, dtype;               // paged: 1 by a page table, 2 by the list itself
     float to_log2;
@@ -379,8 +380,7 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
         auto list_at = [&](int i) { return list + (list_rank(i) >> a.chunk_shift); };
         auto slot_of = [&](int i, int word) -> int {
             if (!listed) return list_rank(i);                     // (below the length: inside the cache)
-            // (a number beyond the last chunk has no position in 32 bits where it is large)
-            if (a.chunk_shift) word = word > a.last_slot >> a.chunk_shift ? INT32_MAX : word < 0 ? word : (word << a.chunk_shift) | (list_rank(i) & ((1 << a.chunk_shift) - 1));
+            if (a.chunk_shift) word = (int)((uint32_t)min(max(word, -1), a.end_chunk) << a.chunk_shift) | (list_rank(i) & ((1 << a.chunk_shift) - 1));
             return min(max(word, 0), a.last_slot);
         };
         auto request_words = [&](int i, int at) { if (listed) request4(list_at(i), words_lds + at * 256); };
@@ -840,6 +840,7 @@ specattn_status launch_mx_attn(const MxAttnLaunch &l, hipStream_t stream)
     a.last_slot = c.indices_are_physical ? (int)std::min<int64_t>(((int64_t)l.c.num_pages << l.c.page_shift) - 1, INT32_MAX) : c.n_max - 1;
     a.H_q = c.H_q; a.H_kv = c.H_kv; a.T = c.T;
     a.chunk_shift = c.chunk_shift;
+    a.end_chunk = std::min((a.last_slot >> a.chunk_shift) + 1, INT32_MAX >> a.chunk_shift);
     a.paged = l.c.page_table ? 1 : c.indices_are_physical ? 2 : 0; a.tail = c.k_new != nullptr; a.dtype = c.dtype;
     a.to_log2 = c.sm_scale * 1.44269504088896340736f;
     a.k_new = static_cast<const uint16_t *>(c.k_new); a.v_new = static_cast<const uint16_t *>(c.v_new);
