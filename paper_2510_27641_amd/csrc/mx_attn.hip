@@ -3,7 +3,7 @@
 //
 // Work split: the attended positions of a row go in tiles of 32, and consecutive tiles to one share, a workgroup's work.  Inside a share
 // tile k goes to wave k mod (waves), so every sum is taken in a fixed order.  A row in one share is finished there; otherwise each
-// leaves a partial (m, l, o) in slot share + row, and mx_merge_kernel combines a row's partials in share order.
+// leaves a partial (m, l, o), o the average of its values, in slot share + row, and mx_merge_kernel combines a row's partials in share order.
 //
 // Per wave and tile, codes and scales go from memory straight into LDS (global_load_lds): d/16 lanes fetch the d bytes of a
 // position as one piece, 1 KiB per instruction, and the list words and page numbers that tell where they lie come the same way, one trip
@@ -84,7 +84,7 @@ template <int D, int DEPTH> struct WaveLds {
 
 template <int D, int NW> struct MergeLds {
     float o[NW][16][Geo<D>::PITCH];
-    float ml[NW][16][2];
+    f32x4 ml[NW][16];                     // the largest score's power, the sum of weights over 2^e, 2^e
 };
 
 template <int D, int NQ, bool FEW> struct Lds {
@@ -607,13 +607,19 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
                 at = after;
             }
             wait_requests<0>();                                   // (the buffers are used for other things next)
+            // The sums leave the units of weights and values for those of the values over 2^e, e the exponent of the sum of weights: what
+            // comes out lies below the largest value, however many there are (in the weights' units sums of values beyond 2^103 are infinite).
             const int up = __shfl(unit, D == 128 ? 4 * g : 8 * (g / 2), 64) - 127;
 #pragma unroll
-            for (int qt = 0; qt < NQ; ++qt)
+            for (int qt = 0; qt < NQ; ++qt) {
+                sum[qt] += shuffle_xor(sum[qt], 16);
+                sum[qt] += shuffle_xor(sum[qt], 32);
+                const int scale = up - __builtin_amdgcn_frexp_expf(sum[qt]);
 #pragma unroll
                 for (int d = 0; d < G::DT; ++d)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[qt][d][k] = __builtin_ldexpf(acc[qt][d][k], up);
+                    for (int k = 0; k < 4; ++k) acc[qt][d][k] = __builtin_ldexpf(acc[qt][d][k], scale);
+            }
         }
         __syncthreads();
 
@@ -622,10 +628,10 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
         float *slot_o = a.slots + (size_t)(me + r) * NQ * 16 * (D + 2), *slot_ml = slot_o + NQ * 16 * D;
 #pragma unroll
         for (int qt = 0; qt < NQ; ++qt) {
-            float l = sum[qt];
-            l += shuffle_xor(l, 16);
-            l += shuffle_xor(l, 32);
-            if (g == 0) { lds.merge.ml[wave][low][0] = ref[qt]; lds.merge.ml[wave][low][1] = l; }
+            if (g == 0) {
+                const int e = __builtin_amdgcn_frexp_expf(sum[qt]);
+                lds.merge.ml[wave][low] = f32x4{ref[qt], __builtin_ldexpf(sum[qt], -e), __builtin_ldexpf(1.0f, e), 0.0f};
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -634,16 +640,19 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
             __syncthreads();
             for (int x = tid; x < 16 * D / 4; x += THREADS) {
                 const int q = x / (D / 4), col = x % (D / 4) * 4;
-                float top = -INFINITY, all = 0.0f, m[NW];
+                float top = -INFINITY, all = 0.0f, f[NW];
+                f32x4 ml[NW];
 #pragma unroll
-                for (int k = 0; k < NW; ++k) { m[k] = lds.merge.ml[k][q][0]; top = fmaxf(top, m[k]); }
-                f32x4 o = {0, 0, 0, 0};
+                for (int k = 0; k < NW; ++k) { ml[k] = lds.merge.ml[k][q]; top = fmaxf(top, ml[k][0]); }
 #pragma unroll
                 for (int k = 0; k < NW; ++k) {
-                    const float f = m[k] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[k] - top);
-                    all += f * lds.merge.ml[k][q][1];
-                    o += f * *reinterpret_cast<const f32x4 *>(&lds.merge.o[k][q][col]);
+                    f[k] = ml[k][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k][0] - top) * ml[k][2];
+                    all += f[k] * ml[k][1];
                 }
+                const float inverse = 1.0f / all;
+                f32x4 o = {0, 0, 0, 0};                           // the weighted average of the waves': never beyond the largest value
+#pragma unroll
+                for (int k = 0; k < NW; ++k) o += f[k] * inverse * *reinterpret_cast<const f32x4 *>(&lds.merge.o[k][q][col]);
                 const int i = qt * 16 + q;
                 if (!alone) {
                     *reinterpret_cast<f32x4 *>(slot_o + i * D + col) = o;
@@ -651,7 +660,6 @@ template <int D, int NQ, bool F16, bool FEW> __global__ __launch_bounds__((Waves
                 } else if (i < a.queries) {
                     const int gh = a.per_t.divide(i), tq = i - gh * a.T;
                     const int64_t orow = ((int64_t)b * a.H_q + head0 + gh) * a.T + tq;
-                    o = o / all;
                     if (a.out) *reinterpret_cast<f32x4 *>(a.out + orow * D + col) = o;
                     if (a.out_lowp)
                         for (int k = 0; k < 4; ++k) st_lowp(a.out_lowp, orow * D + col + k, o[k], a.dtype);
@@ -694,7 +702,7 @@ template <int D, bool TAIL> __global__ __launch_bounds__(256) void mx_merge_kern
             v_new[j] = *reinterpret_cast<const W *>(a.v_new + at);
         }
     }
-    float m = -INFINITY, l = 0.0f, o[E];
+    float m = -INFINITY, l = 0.0f, o[E];                          // o: the average so far, as in the partials; sums of large values have no fp32
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.0f;
     if (parts != EMPTY) {
@@ -715,17 +723,21 @@ template <int D, bool TAIL> __global__ __launch_bounds__(256) void mx_merge_kern
             float now = m;
 #pragma unroll
             for (int k = 0; k < TRIP; ++k) now = fmaxf(now, w + k <= last ? mw[k] : -INFINITY);
-            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now);
-            l *= f;
+            const float before = m == -INFINITY ? 0.0f : l * __builtin_amdgcn_exp2f(m - now);
+            l = before;
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] *= f;
+            for (int k = 0; k < TRIP; ++k) {
+                lw[k] = w + k <= last ? lw[k] * __builtin_amdgcn_exp2f(mw[k] - now) : 0.0f;
+                l += lw[k];
+            }
+            const float inverse = 1.0f / l;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= before * inverse;
 #pragma unroll
             for (int k = 0; k < TRIP; ++k) {
                 if (w + k > last) break;
-                const float fw = __builtin_amdgcn_exp2f(mw[k] - now);
-                l += lw[k] * fw;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] += ow[k][e] * fw;
+                for (int e = 0; e < E; ++e) o[e] += ow[k][e] * (lw[k] * inverse);
             }
             m = now;
         }
@@ -742,21 +754,34 @@ template <int D, bool TAIL> __global__ __launch_bounds__(256) void mx_merge_kern
         for (int k = 1; k < 64; k *= 2)
 #pragma unroll
             for (int j = 0; j < NEW; ++j) s[j] += shuffle_xor(s[j], k);
+        float now = m;
+#pragma unroll
+        for (int j = 0; j < NEW; ++j) {
+            s[j] = j <= t ? s[j] * a.to_log2 : -INFINITY;
+            now = fmaxf(now, s[j]);
+        }
+        const float before = m == -INFINITY ? 0.0f : l * __builtin_amdgcn_exp2f(m - now);
+        l = before;
+#pragma unroll
+        for (int j = 0; j < NEW; ++j) {
+            s[j] = j <= t ? __builtin_amdgcn_exp2f(s[j] - now) : 0.0f;
+            l += s[j];
+        }
+        const float inverse = 1.0f / l;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= before * inverse;
 #pragma unroll
         for (int j = 0; j < NEW; ++j) {
             if (j > t) break;
-            const float x = s[j] * a.to_log2, now = fmaxf(m, x);
-            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now), fw = __builtin_amdgcn_exp2f(x - now);
-            l = l * f + fw;
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = o[e] * f + value(v_new[j], e) * fw;
-            m = now;
+            for (int e = 0; e < E; ++e) o[e] += value(v_new[j], e) * (s[j] * inverse);
         }
+        m = now;
     }
     const bool any = l != 0.0f;                                   // (also where l is NaN)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float x = any ? o[e] / l : 0.0f;
+        const float x = any ? o[e] : 0.0f;
         if (a.out) a.out[orow * D + E * lane + e] = x;
         if (a.out_lowp) st_lowp(a.out_lowp, orow * D + E * lane + e, x, a.dtype);
     }
