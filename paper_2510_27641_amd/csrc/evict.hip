@@ -286,8 +286,7 @@ template <int KEYS, bool ADD> __global__ __launch_bounds__(PICK_THREADS) void ev
     const int tid = threadIdx.x;
     const EvictRow w(e, blockIdx.x);
     if constexpr (ADD) {
-        constexpr int PART = KEYS < 8 ? KEYS : 8;             // (as many sums at a time as the registers hold)
-        for (int k = 0; k < KEYS; k += PART) add_slots<PART, 1, PICK_THREADS>(l, w.r, w.b, w.h, w.len, k * PICK_THREADS + tid);
+        add_slots<KEYS, 1, PICK_THREADS>(l, w.r, w.b, w.h, w.len, tid);
         __syncthreads();                                      // (the keys are read back by other threads)
     }
     Held<KEYS> x;
@@ -601,9 +600,11 @@ specattn_status launch_evict_select(const specattn_evict_args *e, void *workspac
         if ((st = check_launch("evict_add_kernel")) != SPECATTN_OK) return st;
     }
     if (l.slices == 0) {
-        if (e->n_max <= 8 * PICK_THREADS) small ? evict_pick_kernel<8, true><<<rows, PICK_THREADS, 0, stream>>>(l) : evict_pick_kernel<8, false><<<rows, PICK_THREADS, 0, stream>>>(l);
-        else if (e->n_max <= 16 * PICK_THREADS) small ? evict_pick_kernel<16, true><<<rows, PICK_THREADS, 0, stream>>>(l) : evict_pick_kernel<16, false><<<rows, PICK_THREADS, 0, stream>>>(l);
-        else small ? evict_pick_kernel<32, true><<<rows, PICK_THREADS, 0, stream>>>(l) : evict_pick_kernel<32, false><<<rows, PICK_THREADS, 0, stream>>>(l);
+        static_assert(ADD_ITSELF / (2 * sizeof(float)) <= 8 * PICK_THREADS, "a row that its workgroup adds up itself must fit 8 keys to a thread");
+        if (small) evict_pick_kernel<8, true><<<rows, PICK_THREADS, 0, stream>>>(l);
+        else if (e->n_max <= 8 * PICK_THREADS) evict_pick_kernel<8, false><<<rows, PICK_THREADS, 0, stream>>>(l);
+        else if (e->n_max <= 16 * PICK_THREADS) evict_pick_kernel<16, false><<<rows, PICK_THREADS, 0, stream>>>(l);
+        else evict_pick_kernel<32, false><<<rows, PICK_THREADS, 0, stream>>>(l);
         return check_launch("evict_pick_kernel");
     }
     const dim3 grid(rows, l.slices);
