@@ -449,6 +449,9 @@ size_t specattn_mx_workspace_size(const specattn_mx_attn_args *args);      /* 0 
  * nothing.  scores_out and positions_out get the new state: slots below the new length hold the kept slots' scores and positions,
  * those from there up to len hold 0 and -1, the others are left as they were.  Both may be the input arrays themselves.
  * Slots are thus in no order; positions tells which token a slot holds.
+ * Tokens that come into the cache afterwards, behind new_lens[b], are the caller's to enter before the next call: their places in the
+ * text into positions (a slot that still holds -1 counts as the place -1, below `sinks`: a sink for good, or with sinks = 0 an old token of
+ * little weight), and, if 0 is not wanted, the scores that they start from.
  *
  * specattn_evict_move applies the moves to the rows of any caches of the sequences, in place: keys and values in any type,
  * codes and scales, the draft model's cache.  The kv heads h*H_kv/H .. (h+1)*H_kv/H - 1 of a plane follow row h.  Moves that

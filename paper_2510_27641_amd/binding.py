@@ -456,7 +456,8 @@ def evict_args(probs: Optional[torch.Tensor], scores: torch.Tensor, positions: t
                seq_lens: Optional[torch.Tensor] = None, sinks: int = 0, recent: int = 0, decay: float = 1.0,
                row_flags: Optional[torch.Tensor] = None) -> EvictArgs:
     """probs [B,H_draft,S,n] fp32 as for union_args, or None; scores [B,H,n] fp32 and positions [B,H,n] int32, updated in place
-    unless scores_out and positions_out are given; move_src and move_dst [B*H, cap] int32, cap >= min(budget, n - budget)."""
+    unless scores_out and positions_out are given; move_src and move_dst [B*H, cap] int32, cap >= min(budget, n - budget).
+    Whoever appends tokens behind new_lens writes their places in the text into positions before the next call."""
     B, H, n = scores.shape
     scores_out, positions_out = scores if scores_out is None else scores_out, positions if positions_out is None else positions_out
     for t, dtype in ((scores, torch.float32), (scores_out, torch.float32), (positions, torch.int32), (positions_out, torch.int32)):
