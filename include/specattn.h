@@ -399,7 +399,8 @@ specattn_status specattn_mx_load(const specattn_mx_rows_args *args, void *stream
 /*
  * Sparse decode attention (Section 3.1.2, Eq. 2-3; Section 3.5) over a cache in 4 bits: the same computation, lists and
  * results as specattn_sparse_decode_attn on the values the cache stands for.  Accumulation and the softmax are fp32, weights
- * enter the second product with 22 significant bits, and repeated calls give bit-identical results.  (Values of a block that lie
+ * enter the second product with 22 significant bits, none of them below 2^-36 of the largest weight, and repeated calls give
+ * bit-identical results.  (Values of a block that lie
  * under a scale 2^-23 of the largest one attended to in the same block or smaller are rounded to 2^-24 of that; with fp16 queries
  * keys under such a scale of the same position's largest one likewise.)  q, k_new and v_new are bf16 or fp16.  Lists of
  * positions, lists of chunks (chunk_size), pool slots (indices_are_physical) or, with indices == counts == NULL, every

@@ -24,8 +24,10 @@ constexpr int MAX_SLICES = SPECATTN_MAX_N / SLICE;
 // added one after the other, took most of it.
 constexpr int TOP_BITS = 12, MID_BITS = 10, LOW_BITS = 10;
 constexpr int TOP_BINS = 1 << TOP_BITS, MID_BINS = 1 << MID_BITS, LOW_BINS = 1 << LOW_BITS, TOP_SHIFT = 32 - TOP_BITS;
-// Bytes of a row that its selecting workgroup adds up itself: a launch less (8 or 64 rows of up to 24 KiB 1 to 2 us of 11.5), but one CU
-// takes few bytes per us (64 rows of 8197 slots, five entries each, 230 KiB: 20 us in two launches, 32 in one).
+// Bytes of a row that its selecting workgroup adds up itself, a launch less.  In one launch / two, us: 64 rows of 1024 slots with one entry each,
+// 12 KiB, 10.5 / 11.6; 512 rows of 2048 with one, 24 KiB, 23.1 / 26.7; with five entries 1024 slots are even, 28 KiB (64 rows 12.1 / 11.9, 512 rows
+// 24.9 / 21.6), and with 16 no longer, 72 KiB (14.6 / 12.6, 33.7 / 23.8): one CU waits for one trip of entries after the other.  (Longer rows with up to
+// three entries would gain beyond the line: 64 rows of 4096 with three, 80 KiB, 12.4 / 14.0.)
 constexpr int64_t ADD_ITSELF = 32 << 10;
 constexpr uint32_t KEY_STAYS = 0xffffffffu, KEY_NAN = 0;
 
@@ -557,9 +559,9 @@ __global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(MoveLaunch l)
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Rows that one workgroup cannot hold are cut up, and so are longer ones that leave most of the GPU idle.  In one workgroup each / cut up,
-// one entry to add: 512, 128, 64, 8 rows of 16384 slots 99 / 137, 35 / 45, 28 / 32, 23 / 23 us; of 32768 slots 213 / 286, 66 / 81, 50 / 47,
-// 105 / 26; 96 rows of those 58 / 60.
+// Rows that one workgroup cannot hold are cut up, and so are longer ones that leave most of the GPU idle.  In one workgroup each / cut up, us,
+// one entry to add, 8, 64, 72, 128, 512 rows: of 16384 slots 21 / 24, 28 / 32, 29 / 37, 35 / 46, 97 / 134; of 16400 slots, where a thread
+// holds 32 keys in place of 16, 27 / 23, 35 / 34, 36 / 36, 42 / 45, 111 / 139; of 32768 slots 37 / 26, 50 / 48, 52 / 52, 65 / 80, 214 / 280.
 static int evict_slices(const specattn_evict_args *e)
 {
     const int rows = e->B * e->H;

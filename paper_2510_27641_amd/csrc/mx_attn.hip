@@ -7,7 +7,7 @@
 //
 // Per wave and tile, codes and scales go from memory straight into LDS (global_load_lds): d/16 lanes fetch the d bytes of a
 // position as one piece, 1 KiB per instruction, and the list words and page numbers that tell where they lie come the same way, one trip
-// each ahead.  A wave holds three tiles, one in use and two on their way (12 waves: two), 70 to 100 KiB under way per CU at d = 128, and
+// each ahead.  A wave holds three tiles, one in use and two on their way (12 waves: two, one on its way), 68 (51) KiB under way per CU at d = 128, and
 // waits by the number of requests behind the ones it needs.  (Requests straight into registers, one tile ahead: a tile took as long as a trip
 // to memory; 8 dense sequences of up to 32768 positions 45 us / 39.)  From LDS,
 //   keys     lane (p, g) = (lane % 16, lane / 16) takes a quarter of the codes of positions p and 16 + p, d/4 elements that lie
@@ -100,7 +100,8 @@ template <int D, int NQ, bool FEW> struct Lds {
     int count[MAX_ROWS];
     int red[2][NW];
 };
-static_assert(sizeof(Lds<128, 4, true>) <= 160 * 1024 && sizeof(Lds<128, 4, false>) <= 80 * 1024, "workgroups must fit a CU's LDS");
+template <int D, int NQ> constexpr bool fits() { return sizeof(Lds<D, NQ, true>) <= 160 * 1024 && sizeof(Lds<D, NQ, false>) <= 80 * 1024; }
+static_assert(fits<128, 1>() && fits<128, 2>() && fits<128, 3>() && fits<128, 4>() && fits<64, 1>() && fits<64, 2>() && fits<64, 3>() && fits<64, 4>(), "one workgroup, or two, must fit a CU's LDS");
 
 // Requests 16 or 4 bytes per lane from `src` to `to` + 16 or 4 * lane in LDS.  Counts as one request of the wave in order; nobody but
 // wait_requests waits for it.
