@@ -375,7 +375,7 @@ typedef struct specattn_mx_rows_args {
     specattn_mx_cache cache;
     void *k, *v;                 /* [B][H_kv][T][d]; read by specattn_mx_store, written by specattn_mx_load */
     specattn_dtype dtype;        /* of k and v */
-    int32_t T;                   /* rows per sequence, at most 2^30 */
+    int32_t T;                   /* rows per sequence, at most 2^28 */
     int64_t stride_b, stride_h, stride_t;                /* elements, of k and v alike; last dim contiguous; 16-byte multiples */
     const int32_t *starts;       /* [B] first slot of each sequence, or NULL for 0 */
     const int32_t *counts;       /* [B] rows of each sequence (at most T are taken), or NULL for T */
@@ -464,7 +464,7 @@ typedef struct specattn_evict_args {
     const float *probs;          /* [B][H_draft][S][n_max] fp32: row (b, x, s) starts at b*probs_stride_b +
                                     (x*S + s)*probs_stride_row; NULL (with H_draft = S = 0) = nothing to add */
     int64_t probs_stride_b, probs_stride_row;            /* elements */
-    int32_t B, H, n_max;         /* score rows: B * H; n_max <= SPECATTN_MAX_N slots each */
+    int32_t B, H, n_max;         /* score rows: B * H, fewer than 2^22; n_max <= SPECATTN_MAX_N slots each */
     int32_t H_draft, S;          /* H_draft % H == 0 */
     const float *scores;         /* [B][H][n_max] fp32, last dim contiguous */
     const int32_t *positions;    /* [B][H][n_max] place in the text of the token in each slot; same strides */

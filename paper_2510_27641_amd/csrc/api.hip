@@ -299,7 +299,8 @@ specattn_status check_mx_rows(const specattn_mx_rows_args *r, bool store)
     }
     if (!r->k || !r->v) { set_error("k and v must not be NULL"); return SPECATTN_EINVAL; }
     if (r->T <= 0) { set_error("T must be positive"); return SPECATTN_EINVAL; }
-    if (r->T > (1 << 30)) { set_error("more than 2^30 rows per sequence"); return SPECATTN_ESHAPE; }       // (counted in 31 bits, whole workgroups of them)
+    // (256 threads to 32 rows or more, and a launch has fewer than 2^32 along an axis; rows are counted in 31 bits, whole workgroups of them)
+    if (r->T > (1 << 28)) { set_error("more than 2^28 rows per sequence"); return SPECATTN_ESHAPE; }
     if (r->dtype != SPECATTN_F32 && r->dtype != SPECATTN_BF16 && r->dtype != SPECATTN_F16) { set_error("unknown dtype %d", (int)r->dtype); return SPECATTN_EUNSUPPORTED; }
     const int64_t es = r->dtype == SPECATTN_F32 ? 4 : 2;
     if ((r->stride_b * es) % 16 || (r->stride_h * es) % 16 || (r->stride_t * es) % 16) { set_error("strides must be multiples of 16 bytes"); return SPECATTN_EALIGN; }
@@ -385,6 +386,8 @@ MxAttnLaunch make_mx_attn(const specattn_mx_attn_args *a)
     return m;
 }
 
+constexpr int MAX_EVICT_ROWS = (1 << 22) - 1;                 // a launch has fewer than 2^32 threads along an axis, a row 1024
+
 specattn_status check_evict(const specattn_evict_args *e)
 {
     if (!e) { set_error("evict args are NULL"); return SPECATTN_EINVAL; }
@@ -399,7 +402,7 @@ specattn_status check_evict(const specattn_evict_args *e)
         if ((int64_t)e->B * e->H_draft * e->S > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
         if (e->probs_stride_row < e->n_max) { set_error("probs_stride_row is smaller than n_max"); return SPECATTN_ESHAPE; }
     }
-    if ((int64_t)e->B * e->H > (1 << 24)) { set_error("too many rows"); return SPECATTN_ESHAPE; }
+    if ((int64_t)e->B * e->H > MAX_EVICT_ROWS) { set_error("too many rows"); return SPECATTN_ESHAPE; }
     if (e->row_stride_h < e->n_max || e->row_stride_b < e->n_max) { set_error("row strides are smaller than n_max"); return SPECATTN_ESHAPE; }
     if (rows_overlap({e->B, e->row_stride_b}, {e->H, e->row_stride_h}, {1, 0}, e->n_max)) { set_error("rows of the scores share entries"); return SPECATTN_ESHAPE; }
     if (e->sinks < 0 || e->recent < 0 || (int64_t)e->sinks + e->recent > e->budget) { set_error("sinks and recent must not be negative, nor exceed the budget together"); return SPECATTN_ESHAPE; }
@@ -745,7 +748,7 @@ specattn_status specattn_mx_decode_attn(const specattn_mx_attn_args *args, void 
 
 size_t specattn_evict_workspace_size(const specattn_evict_args *e)
 {
-    if (!e || e->B <= 0 || e->H <= 0 || e->n_max <= 0 || e->n_max > SPECATTN_MAX_N || (int64_t)e->B * e->H > (1 << 24)) return 0;
+    if (!e || e->B <= 0 || e->H <= 0 || e->n_max <= 0 || e->n_max > SPECATTN_MAX_N || (int64_t)e->B * e->H > MAX_EVICT_ROWS) return 0;
     return evict_workspace_bytes(e);
 }
 

@@ -85,3 +85,15 @@ def test_score_rows_of_any_order_are_taken():
     lib = sa.load()
     for kw in (dict(row_stride_b=512, row_stride_h=2 * 512), dict(row_stride_b=600, row_stride_h=5000), dict(B=1, row_stride_b=512), dict(H=1, row_stride_h=512, row_stride_b=512)):
         _refused(lambda args, stream: lib.specattn_evict_select(args, None, 0, stream), _evict(**kw), sa.EWORKSPACE)
+
+
+def test_more_work_than_a_launch_takes_is_refused():
+    """A launch has fewer than 2^32 threads along each axis: what asks for more is refused before anything runs."""
+    lib = sa.load()
+    for fn in (lib.specattn_mx_store, lib.specattn_mx_load):
+        _refused(fn, _rows(_cache(), T=2 ** 28 + 1, stride_h=2 ** 31 * 128, stride_b=2 ** 33 * 128))
+        _refused(fn, _rows(_cache(), T=2 ** 28, stride_h=2 ** 31 * 128, stride_b=2 ** 33 * 128, k=0x40008), sa.EALIGN)
+    select = lambda args, stream: lib.specattn_evict_select(args, None, 0, stream)  # noqa: E731
+    _refused(select, _evict(B=2 ** 18, H=16, H_draft=16, S=1, row_stride_b=16 * 512))
+    _refused(select, _evict(B=2 ** 18 - 1, H=16, H_draft=16, S=1, row_stride_b=16 * 512), sa.EWORKSPACE)
+    assert sa.specattn_evict_workspace_size(_evict(B=2 ** 18, H=16)) == 0
