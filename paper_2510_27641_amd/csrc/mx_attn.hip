@@ -84,7 +84,7 @@ template <int D, int DEPTH> struct WaveLds {
 
 template <int D, int NW> struct MergeLds {
     float o[NW][16][Geo<D>::PITCH];
-    f32x4 ml[NW][16];                     // the largest score's power, the sum of weights over 2^e, 2^e
+    f32x4 ml[NW][16];                     // ref, the sum of weights over 2^e, 2^e (e: that sum's exponent; o is over 2^e as well)
 };
 
 template <int D, int NQ, bool FEW> struct Lds {
