@@ -49,6 +49,7 @@ typedef enum specattn_dtype { SPECATTN_F32 = 0, SPECATTN_BF16 = 1, SPECATTN_F16 
 #define SPECATTN_MAX_N (1 << 19)       /* longest row the selection handles */
 #define SPECATTN_SEL_BLOCK 1024        /* positions per entry of block_counts */
 #define SPECATTN_MAX_T 8               /* most verifier queries (gamma + 1) per head */
+#define SPECATTN_MAX_TREE 64           /* most drafted nodes of a tree */
 #define SPECATTN_STATIC_SCRATCH_BYTES (16u << 20)   /* built-in scratch of specattn_sparse_decode_attn_static */
 
 /*
@@ -510,6 +511,138 @@ typedef struct specattn_move_args {
 } specattn_move_args;
 
 specattn_status specattn_evict_move(const specattn_move_args *args, void *stream);
+
+/*
+ * A serving loop in pages: prompts come in, trees of drafted tokens are verified, the accepted tokens stay.
+ *
+ * specattn_pages_update: page tables, free pages and the slots of new tokens, from the lengths that the sequences have (seq_lens) and are to have
+ * (new_lens).  A sequence of len tokens owns the first ceil(len / page_size) entries of its row of the table, pages of its own.
+ *  - Sequences that shrink (0: all of it ends) return the pages behind their new end: they go onto the stack of free pages in the order of the
+ *    sequences and of their entries.
+ *  - Sequences that grow then take pages off its top, in the same order, into the entries behind those they have.
+ *  - A sequence is refused, and stays as it was (row_flags: SPECATTN_ROW_OVERFLOW), if it asks for pages and the sequences up to it ask for more
+ *    than there are on the stack, if the new tokens of the sequences up to it (those without pages apart) are more than token_capacity, or if its new
+ *    length does not fit in its row of the table.  A negative length, or one that the table cannot hold, is SPECATTN_ROW_INVALID: nothing is done.
+ *  - New token i of the call, sequence after sequence, gets slots[i] = page * page_size + offset, its place in its text positions[i] and its
+ *    sequence owners[i]; the entries behind the last one hold -1, so that a captured call of a fixed capacity can be followed by
+ *    calls over all of it (specattn_cache_store leaves -1 out).  Tokens of sequence b: token_starts[b] .. token_starts[b + 1] - 1.
+ * Entries of returned pages are left in the table.  A page that stands twice in what the sequences own would be returned twice: pages are not shared.
+ * In place: lens_out may be seq_lens or new_lens, free_count_out may be free_count.  Outputs must not overlap otherwise.
+ */
+typedef struct specattn_pages_args {
+    int32_t *page_table;         /* [B][max_pages_per_seq], updated */
+    int32_t B, page_size, max_pages_per_seq, num_pages;      /* page_size: a power of two; num_pages * page_size < 2^31 */
+    int32_t *free_pages;         /* [num_pages] the stack: the first *free_count are free, the last of them its top; updated */
+    const int32_t *free_count;   /* [1] */
+    int32_t *free_count_out;     /* out [1] */
+    const int32_t *seq_lens, *new_lens;                      /* [B] */
+    int32_t *lens_out;           /* out [B] */
+    int32_t *token_starts;       /* out [B + 1], optional */
+    int32_t *slots;              /* out [token_capacity], optional (NULL: no limit on new tokens) */
+    int32_t *positions, *owners; /* out [token_capacity], optional; with slots */
+    int32_t token_capacity;
+    uint32_t *row_flags;         /* out [B], optional */
+} specattn_pages_args;
+
+/* workspace: specattn_pages_workspace_size(args) bytes, 256-byte aligned */
+specattn_status specattn_pages_update(const specattn_pages_args *args, void *workspace, size_t workspace_bytes, void *stream);
+size_t specattn_pages_workspace_size(const specattn_pages_args *args);     /* 0 for invalid arguments */
+
+/*
+ * specattn_cache_store: rows of keys and values into the slots of a cache (Algorithm 1 updates the caches with every accepted token).
+ * Entry i takes source row rows[i] (i itself without rows): row b * T + t lies at b * stride_b + t * stride_t, head h stride_h further.  Packed
+ * prompts [tokens][H_kv][d] are B = 1, T = tokens; the nodes of drafted trees [B][H_kv][T][d] go in by the numbers of the accepted
+ * ones.  Slot s is offset s % page_size of page s / page_size; for a contiguous cache [B][H_kv][n][d] pages are sequences (page_size = n).
+ * Entries with a slot or row that does not exist (-1) are left out; no slot may be written twice.  Source rows may be read many times.
+ */
+typedef struct specattn_store_args {
+    const void *k, *v;
+    specattn_dtype dtype;        /* of k, v and the caches: any of the three */
+    int32_t B, T, H_kv, d;       /* d: any whole number of 16-byte pieces; H_kv * d <= 2^24 */
+    int64_t stride_b, stride_t, stride_h;                    /* elements, of k and v alike; last dim contiguous; 16-byte multiples */
+    void *k_cache, *v_cache;
+    int64_t cache_stride_page, cache_stride_h, cache_stride_n;   /* elements, of both; no two rows share bytes (SPECATTN_ESHAPE) */
+    int32_t num_pages, page_size;                            /* page_size: any */
+    const int32_t *slots;        /* [num_slots] */
+    const int32_t *rows;         /* [num_slots] or NULL */
+    int32_t num_slots;
+} specattn_store_args;
+
+specattn_status specattn_cache_store(const specattn_store_args *args, void *stream);
+
+/*
+ * specattn_prompt_attn: causal attention (Eq. 1) of the tokens of B sequences packed one behind the other, with grouped query heads.
+ * Sequence b has query rows q_starts[b] .. q_starts[b + 1] - 1 and L keys and values: those of the same rows of k and v, rows kv_starts[b] .. of them
+ * where kv_starts is given, or positions 0 .. seq_lens[b] - 1 of its pages.  Its last query sees all L, the one before one less: query i of m
+ * sees the first L - m + i + 1.  A query that sees nothing gives out = 0 and lse = -inf.  What a query does not see has no effect on it,
+ * infinities and NaN included; rows of out and lse that belong to no sequence are left as they were.
+ * Accumulation and the softmax are fp32.  Where `out` is asked for the weights enter the second product in two parts of the element type
+ * (16 significant bits with bf16, 22 with fp16), for out_lowp alone rounded to it.  Repeated calls give bit-identical results.
+ * Starts ascend.  Lengths are cut to what there is (total_q, total_kv, the page table); a page number outside the pool reads the nearest page.
+ */
+typedef struct specattn_prompt_args {
+    const void *q;               /* [total_q][H_q][d] */
+    const void *k, *v;           /* packed [total_kv][H_kv][d], or pools [num_pages][H_kv][page_size][d] */
+    specattn_dtype dtype;        /* SPECATTN_BF16 or SPECATTN_F16 */
+    int32_t B, H_q, H_kv, d;     /* H_q a multiple of H_kv; d: 64 or 128 */
+    int32_t total_q, total_kv;   /* rows of q, and of packed k and v; total_q * H_q <= 2^30 */
+    float sm_scale;              /* <= 0 selects 1/sqrt(d) */
+    int64_t q_stride_t, q_stride_h;                          /* elements; last dim contiguous; 16-byte multiples */
+    int64_t kv_stride_n, kv_stride_h, kv_stride_page;        /* likewise, of k and v alike */
+    const int32_t *q_starts;     /* [B + 1] */
+    const int32_t *kv_starts;    /* [B + 1], or NULL for q_starts; packed keys and values only */
+    const int32_t *page_table;   /* [B][max_pages_per_seq], or NULL: packed */
+    int32_t page_size, max_pages_per_seq, num_pages;
+    const int32_t *seq_lens;     /* [B], with page_table: positions in the cache, the new tokens' among them */
+    float *out;                  /* [total_q][H_q][d] fp32, contiguous; optional if out_lowp is given */
+    void *out_lowp;              /* [total_q][H_q][d] in dtype, contiguous; optional if out is given */
+    float *lse;                  /* [total_q][H_q]; optional */
+    void *workspace;             /* specattn_prompt_workspace_size(args) bytes (0: none), 256-byte aligned */
+    size_t workspace_bytes;
+} specattn_prompt_args;
+
+specattn_status specattn_prompt_attn(const specattn_prompt_args *args, void *stream);
+size_t specattn_prompt_workspace_size(const specattn_prompt_args *args);   /* 0 for invalid arguments too */
+
+/*
+ * specattn_tree_attn: sparse decode attention (Section 3.1.2, Eq. 2-3; Section 3.5) of a tree of T drafted tokens: the computation of
+ * specattn_sparse_decode_attn with k_new and v_new, where node t attends, behind the kept positions, to the nodes whose bits are set in
+ * tree_masks[b][t] - those it descends from and itself, in a tree; any set will do - in place of nodes 0 .. t.
+ * Lists of positions, lists of chunks (chunk_size), pool slots (indices_are_physical) or, with indices == counts == NULL, every position below
+ * seq_lens[b].  Nodes from node_counts[b] on are not there: their rows give out = 0 and lse = -inf, as does a row with nothing to attend to; their
+ * bits, queries, keys and values have no effect.  Keys and values that a row's mask hides have none either, infinities and NaN included.
+ * Weights and results as for specattn_prompt_attn.  A list entry outside the cache is read as the nearest slot inside it, a page number outside the
+ * pool as the nearest page.  Any number of query heads per kv head up to 65536 query rows G*T; a row attends to 2^24 positions at most.
+ */
+typedef struct specattn_tree_args {
+    const void *q;               /* [B][H_q][T][d] */
+    const void *k, *v;           /* [B][H_kv][n_max][d], or pools [num_pages][H_kv][page_size][d] */
+    const void *k_new, *v_new;   /* [B][H_kv][T][d], contiguous */
+    specattn_dtype dtype;        /* SPECATTN_BF16 or SPECATTN_F16 */
+    int32_t B, H_q, H_kv, T, d, n_max;                       /* T: 1 .. SPECATTN_MAX_TREE; d: 64 or 128 */
+    float sm_scale;              /* <= 0 selects 1/sqrt(d) */
+    int64_t q_stride_b, q_stride_h, q_stride_t;              /* elements; last dim contiguous; 16-byte multiples */
+    int64_t kv_stride_b, kv_stride_h, kv_stride_n, kv_stride_page;   /* likewise, of k and v alike; _b contiguous, _page paged */
+    const int32_t *page_table;   /* [B][max_pages_per_seq], or NULL = contiguous (for indices_are_physical: a pool) */
+    int32_t page_size, max_pages_per_seq, num_pages;         /* num_pages: 0 for a contiguous cache */
+    const uint64_t *tree_masks;  /* [B][T]: bit u of word t: node t attends to node u */
+    const int32_t *node_counts;  /* [B] nodes of each tree, or NULL for T */
+    const int32_t *seq_lens;     /* [B] or NULL for n_max; used by dense calls and chunk lists */
+    const int32_t *indices;      /* [B*H_kv][idx_stride_row] */
+    int64_t idx_stride_row;
+    const int32_t *counts;       /* [B*H_kv]; values above idx_capacity are clamped to it */
+    int32_t idx_capacity;
+    int32_t chunk_size;          /* 0 or 1: positions; a power of two up to 1024: chunk numbers */
+    int32_t indices_are_physical;/* 1: entries are pool slots page * page_size + offset */
+    float *out;                  /* [B][H_q][T][d] fp32, contiguous; optional if out_lowp is given */
+    void *out_lowp;              /* [B][H_q][T][d] in dtype, contiguous; optional if out is given */
+    float *lse;                  /* [B][H_q][T]; optional */
+    void *workspace;             /* specattn_tree_workspace_size(args) bytes, 256-byte aligned */
+    size_t workspace_bytes;
+} specattn_tree_args;
+
+specattn_status specattn_tree_attn(const specattn_tree_args *args, void *stream);
+size_t specattn_tree_workspace_size(const specattn_tree_args *args);       /* 0 for invalid arguments */
 
 /* Text of the calling thread's last error ("" if none).  Never NULL. */
 const char *specattn_last_error(void);

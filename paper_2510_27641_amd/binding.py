@@ -24,7 +24,8 @@ EXPORTS = ("specattn_topp_select", "specattn_topp_select_union", "specattn_union
            "specattn_workspace_size", "specattn_layer_similarity", "specattn_layer_similarity_workspace_size",
            "specattn_layer_map", "specattn_layer_map_workspace_size", "specattn_check_lists", "specattn_lists_to_csr", "specattn_stream_read",
            "specattn_mx_store", "specattn_mx_load", "specattn_mx_decode_attn", "specattn_mx_workspace_size", "specattn_evict_select", "specattn_evict_workspace_size",
-           "specattn_evict_move", "specattn_init", "specattn_last_error", "specattn_version")
+           "specattn_evict_move", "specattn_pages_update", "specattn_pages_workspace_size", "specattn_cache_store", "specattn_prompt_attn",
+           "specattn_prompt_workspace_size", "specattn_tree_attn", "specattn_tree_workspace_size", "specattn_init", "specattn_last_error", "specattn_version")
 
 
 class SelectArgs(C.Structure):
@@ -136,6 +137,54 @@ class MoveArgs(C.Structure):
     ]
 
 
+class PagesArgs(C.Structure):
+    _fields_ = [
+        ("page_table", C.c_void_p), ("B", C.c_int32), ("page_size", C.c_int32), ("max_pages_per_seq", C.c_int32), ("num_pages", C.c_int32),
+        ("free_pages", C.c_void_p), ("free_count", C.c_void_p), ("free_count_out", C.c_void_p),
+        ("seq_lens", C.c_void_p), ("new_lens", C.c_void_p), ("lens_out", C.c_void_p), ("token_starts", C.c_void_p),
+        ("slots", C.c_void_p), ("positions", C.c_void_p), ("owners", C.c_void_p), ("token_capacity", C.c_int32), ("row_flags", C.c_void_p),
+    ]
+
+
+class StoreArgs(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int), ("B", C.c_int32), ("T", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32),
+        ("stride_b", C.c_int64), ("stride_t", C.c_int64), ("stride_h", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
+        ("cache_stride_page", C.c_int64), ("cache_stride_h", C.c_int64), ("cache_stride_n", C.c_int64),
+        ("num_pages", C.c_int32), ("page_size", C.c_int32), ("slots", C.c_void_p), ("rows", C.c_void_p), ("num_slots", C.c_int32),
+    ]
+
+
+class PromptArgs(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int),
+        ("B", C.c_int32), ("H_q", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32), ("total_q", C.c_int32), ("total_kv", C.c_int32),
+        ("sm_scale", C.c_float), ("q_stride_t", C.c_int64), ("q_stride_h", C.c_int64),
+        ("kv_stride_n", C.c_int64), ("kv_stride_h", C.c_int64), ("kv_stride_page", C.c_int64),
+        ("q_starts", C.c_void_p), ("kv_starts", C.c_void_p),
+        ("page_table", C.c_void_p), ("page_size", C.c_int32), ("max_pages_per_seq", C.c_int32), ("num_pages", C.c_int32),
+        ("seq_lens", C.c_void_p), ("out", C.c_void_p), ("out_lowp", C.c_void_p), ("lse", C.c_void_p),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+MAX_TREE = 64
+
+
+class TreeArgs(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("dtype", C.c_int),
+        ("B", C.c_int32), ("H_q", C.c_int32), ("H_kv", C.c_int32), ("T", C.c_int32), ("d", C.c_int32), ("n_max", C.c_int32),
+        ("sm_scale", C.c_float), ("q_stride_b", C.c_int64), ("q_stride_h", C.c_int64), ("q_stride_t", C.c_int64),
+        ("kv_stride_b", C.c_int64), ("kv_stride_h", C.c_int64), ("kv_stride_n", C.c_int64), ("kv_stride_page", C.c_int64),
+        ("page_table", C.c_void_p), ("page_size", C.c_int32), ("max_pages_per_seq", C.c_int32), ("num_pages", C.c_int32),
+        ("tree_masks", C.c_void_p), ("node_counts", C.c_void_p), ("seq_lens", C.c_void_p),
+        ("indices", C.c_void_p), ("idx_stride_row", C.c_int64), ("counts", C.c_void_p), ("idx_capacity", C.c_int32),
+        ("chunk_size", C.c_int32), ("indices_are_physical", C.c_int32),
+        ("out", C.c_void_p), ("out_lowp", C.c_void_p), ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
 class SpecAttnError(RuntimeError):
     def __init__(self, status: int, text: str):
         super().__init__(f"specattn status {status}: {text}")
@@ -184,11 +233,18 @@ def load() -> C.CDLL:
         lib.specattn_lists_to_csr.restype = C.c_int
         lib.specattn_lists_to_csr.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
         for name, args in (("specattn_mx_store", MxRowsArgs), ("specattn_mx_load", MxRowsArgs), ("specattn_mx_decode_attn", MxAttnArgs),
-                           ("specattn_evict_move", MoveArgs)):
+                           ("specattn_evict_move", MoveArgs), ("specattn_cache_store", StoreArgs), ("specattn_prompt_attn", PromptArgs),
+                           ("specattn_tree_attn", TreeArgs)):
             getattr(lib, name).restype = C.c_int
             getattr(lib, name).argtypes = [C.POINTER(args), C.c_void_p]
         lib.specattn_mx_workspace_size.restype = C.c_size_t
         lib.specattn_mx_workspace_size.argtypes = [C.POINTER(MxAttnArgs)]
+        for name, args in (("specattn_pages_workspace_size", PagesArgs), ("specattn_prompt_workspace_size", PromptArgs),
+                           ("specattn_tree_workspace_size", TreeArgs)):
+            getattr(lib, name).restype = C.c_size_t
+            getattr(lib, name).argtypes = [C.POINTER(args)]
+        lib.specattn_pages_update.restype = C.c_int
+        lib.specattn_pages_update.argtypes = [C.POINTER(PagesArgs), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.specattn_evict_select.restype = C.c_int
         lib.specattn_evict_select.argtypes = [C.POINTER(EvictArgs), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.specattn_evict_workspace_size.restype = C.c_size_t
@@ -512,6 +568,141 @@ def move_args(move_src: torch.Tensor, move_dst: torch.Tensor, move_counts: torch
     return a
 
 
+def pages_args(page_table: torch.Tensor, page_size: int, free_pages: torch.Tensor, free_count: torch.Tensor, seq_lens: torch.Tensor,
+               new_lens: torch.Tensor, *, lens_out: Optional[torch.Tensor] = None, free_count_out: Optional[torch.Tensor] = None,
+               token_starts: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+               owners: Optional[torch.Tensor] = None, row_flags: Optional[torch.Tensor] = None) -> PagesArgs:
+    """page_table [B,max_pages], free_pages [pages], free_count [1], seq_lens and new_lens [B], all int32; seq_lens and free_count are
+    updated in place unless lens_out and free_count_out are given.  slots (and positions, owners): [capacity] int32."""
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.dim() == 2
+    B = page_table.shape[0]
+    a = PagesArgs()
+    a.page_table, a.B, a.max_pages_per_seq = page_table.data_ptr(), B, page_table.shape[1]
+    a.page_size, a.num_pages = page_size, free_pages.numel()
+    a.free_pages, a.free_count = _int32(free_pages, free_pages.numel()), _int32(free_count, 1)
+    a.free_count_out = _int32(free_count if free_count_out is None else free_count_out, 1)
+    a.seq_lens, a.new_lens = _int32(seq_lens, B), _int32(new_lens, B)
+    a.lens_out = _int32(seq_lens if lens_out is None else lens_out, B)
+    a.token_starts, a.row_flags = _int32(token_starts, B + 1), _int32(row_flags, B)
+    if slots is not None:
+        a.token_capacity = slots.numel()
+        a.slots = _int32(slots, slots.numel())
+    a.positions, a.owners = _int32(positions, a.token_capacity), _int32(owners, a.token_capacity)
+    return a
+
+
+def store_args(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor, *,
+               rows: Optional[torch.Tensor] = None) -> StoreArgs:
+    """k, v: packed rows [N,H_kv,d], or [B,H_kv,T,d], whose row b * T + t is node t of sequence b; caches: pools [pages,H_kv,page_size,d] (or
+    contiguous [B,H_kv,n,d], slots b * n + position); slots [M] int32, -1 for none; rows [M] int32: the source row of each slot."""
+    assert k.shape == v.shape and k.stride() == v.stride() and k.stride(-1) == 1 and k_cache.shape == v_cache.shape and k_cache.stride() == v_cache.stride()
+    assert k.dtype == v.dtype == k_cache.dtype == v_cache.dtype and k.dtype in _DTYPES and k.dim() in (3, 4) and k_cache.dim() == 4 and k_cache.stride(3) == 1
+    a = StoreArgs()
+    a.k, a.v, a.dtype = k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype]
+    if k.dim() == 3:
+        a.B, a.T, a.stride_t, a.stride_h = 1, k.shape[0], k.stride(0), k.stride(1)
+    else:
+        a.B, a.T, a.stride_b, a.stride_t, a.stride_h = k.shape[0], k.shape[2], k.stride(0), k.stride(2), k.stride(1)
+    a.H_kv, a.d = k.shape[1], k.shape[-1]
+    assert k_cache.shape[1] == a.H_kv and k_cache.shape[3] == a.d
+    a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
+    a.num_pages, a.page_size = k_cache.shape[0], k_cache.shape[2]
+    a.cache_stride_page, a.cache_stride_h, a.cache_stride_n = k_cache.stride(0), k_cache.stride(1), k_cache.stride(2)
+    a.num_slots = slots.numel()
+    a.slots, a.rows = _int32(slots, a.num_slots), _int32(rows, a.num_slots)
+    return a
+
+
+def _outputs(a, shape, dtype, out, out_lowp, lse):
+    if out is not None:
+        assert out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == shape
+        a.out = out.data_ptr()
+    if out_lowp is not None:
+        assert out_lowp.dtype == dtype and out_lowp.is_contiguous() and tuple(out_lowp.shape) == shape
+        a.out_lowp = out_lowp.data_ptr()
+    if lse is not None:
+        assert lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == shape[:-1]
+        a.lse = lse.data_ptr()
+
+
+def prompt_args(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, *, kv_starts: Optional[torch.Tensor] = None,
+                page_table: Optional[torch.Tensor] = None, seq_lens: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                out_lowp: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, sm_scale: float = 0.0,
+                workspace: Optional[torch.Tensor] = None) -> PromptArgs:
+    """q [rows,H_q,d] bf16 or fp16; k, v [kv_rows,H_kv,d] or, with page_table [B,max_pages] and seq_lens [B], pools [pages,H_kv,page_size,d];
+    q_starts, kv_starts [B+1] int32; out, out_lowp [rows,H_q,d]; lse [rows,H_q]."""
+    assert q.dim() == 3 and k.shape == v.shape and k.stride() == v.stride() and q.dtype == k.dtype == v.dtype and q.dtype in _DTYPES
+    assert q.stride(2) == 1 and k.stride(-1) == 1 and k.shape[-1] == q.shape[2] and k.dim() == (3 if page_table is None else 4)
+    a = PromptArgs()
+    B = q_starts.numel() - 1
+    a.q, a.k, a.v, a.dtype = q.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPES[q.dtype]
+    a.B, a.H_q, a.H_kv, a.d, a.total_q, a.sm_scale = B, q.shape[1], k.shape[1], q.shape[2], q.shape[0], sm_scale
+    a.q_stride_t, a.q_stride_h, a.kv_stride_h = q.stride(0), q.stride(1), k.stride(1)
+    a.q_starts, a.kv_starts = _int32(q_starts, B + 1), _int32(kv_starts, B + 1)
+    if page_table is None:
+        a.total_kv, a.kv_stride_n = k.shape[0], k.stride(0)
+        assert seq_lens is None and (kv_starts is not None or k.shape[0] >= q.shape[0])
+    else:
+        assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] == B
+        a.page_table, a.max_pages_per_seq, a.num_pages, a.page_size = page_table.data_ptr(), page_table.shape[1], k.shape[0], k.shape[2]
+        a.kv_stride_page, a.kv_stride_n = k.stride(0), k.stride(2)
+        a.seq_lens = _int32(seq_lens, B)
+    _outputs(a, tuple(q.shape), q.dtype, out, out_lowp, lse)
+    if workspace is not None:
+        set_workspace(a, workspace)
+    return a
+
+
+def tree_args(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, tree_masks: torch.Tensor, *,
+              out: Optional[torch.Tensor] = None, out_lowp: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+              indices: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None, node_counts: Optional[torch.Tensor] = None,
+              seq_lens: Optional[torch.Tensor] = None, n_max: Optional[int] = None, sm_scale: float = 0.0, chunk_size: int = 0,
+              page_table: Optional[torch.Tensor] = None, page_size: int = 0, indices_are_physical: bool = False,
+              workspace: Optional[torch.Tensor] = None) -> TreeArgs:
+    """q [B,H_q,T,d] bf16 or fp16; k, v, lists and pages as for attn_args; k_new, v_new [B,H_kv,T,d] contiguous; tree_masks [B,T] int64,
+    bit u of word t set where node t attends to node u; node_counts [B] int32."""
+    assert q.dim() == 4 and k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and q.dtype == k.dtype == v.dtype and q.dtype in _DTYPES
+    assert q.stride(3) == 1 and k.stride(3) == 1 and k.shape[3] == q.shape[3]
+    B, H_q, T, d = q.shape
+    a = TreeArgs()
+    a.q, a.k, a.v, a.dtype = q.data_ptr(), k.data_ptr(), v.data_ptr(), _DTYPES[q.dtype]
+    a.B, a.H_q, a.H_kv, a.T, a.d, a.sm_scale = B, H_q, k.shape[1], T, d, sm_scale
+    a.q_stride_b, a.q_stride_h, a.q_stride_t = q.stride(0), q.stride(1), q.stride(2)
+    a.kv_stride_h, a.kv_stride_n = k.stride(1), k.stride(2)
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        assert t.dtype == q.dtype and t.is_contiguous() and tuple(t.shape) == (B, a.H_kv, T, d)
+        setattr(a, name, t.data_ptr())
+    assert tree_masks.dtype == torch.int64 and tree_masks.is_contiguous() and tuple(tree_masks.shape) == (B, T)
+    a.tree_masks = tree_masks.data_ptr()
+    if page_table is not None or indices_are_physical:
+        a.kv_stride_page, a.num_pages, a.page_size = k.stride(0), k.shape[0], k.shape[2]
+        assert page_size in (0, k.shape[2])
+        slots = k.shape[0] * k.shape[2]
+        if page_table is not None:
+            assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.shape[0] == B
+            a.page_table, a.max_pages_per_seq = page_table.data_ptr(), page_table.shape[1]
+            slots = page_table.shape[1] * k.shape[2]
+        a.n_max = slots if n_max is None else n_max
+    else:
+        assert k.shape[0] == B
+        a.kv_stride_b, a.n_max = k.stride(0), k.shape[2] if n_max is None else n_max
+        assert a.n_max <= k.shape[2]
+    a.node_counts, a.seq_lens, a.counts = _int32(node_counts, B), _int32(seq_lens, B), _int32(counts, B * a.H_kv)
+    if indices is not None:
+        assert indices.dtype == torch.int32 and indices.dim() == 2 and indices.stride(1) == 1 and indices.shape[0] == B * a.H_kv
+        a.indices, a.idx_stride_row, a.idx_capacity = indices.data_ptr(), indices.stride(0), indices.shape[1]
+    a.chunk_size, a.indices_are_physical = chunk_size, int(indices_are_physical)
+    _outputs(a, (B, H_q, T, d), q.dtype, out, out_lowp, lse)
+    if workspace is not None:
+        set_workspace(a, workspace)
+    return a
+
+
+def set_workspace(args, workspace: torch.Tensor) -> None:
+    """The workspace of argument structs that carry one."""
+    args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 # ------------------------------------------------------------------------------------------
 # the entry points (same names as the C ABI)
 # ------------------------------------------------------------------------------------------
@@ -609,6 +800,39 @@ def specattn_evict_select(args: EvictArgs, workspace: torch.Tensor, stream=None)
 
 def specattn_evict_move(args: MoveArgs, stream=None) -> None:
     _check(load().specattn_evict_move(C.byref(args), _stream(stream)))
+
+
+def specattn_pages_workspace_size(args: PagesArgs) -> int:
+    return int(load().specattn_pages_workspace_size(C.byref(args)))
+
+
+def specattn_pages_update(args: PagesArgs, workspace: torch.Tensor, stream=None) -> None:
+    """Page tables, free pages and the slots of new tokens, from the lengths that sequences have and are to have."""
+    nbytes = workspace.numel() * workspace.element_size()
+    _check(load().specattn_pages_update(C.byref(args), _ptr(workspace), nbytes, _stream(stream)))
+
+
+def specattn_cache_store(args: StoreArgs, stream=None) -> None:
+    """Rows of keys and values into the slots of a cache."""
+    _check(load().specattn_cache_store(C.byref(args), _stream(stream)))
+
+
+def specattn_prompt_workspace_size(args: PromptArgs) -> int:
+    return int(load().specattn_prompt_workspace_size(C.byref(args)))
+
+
+def specattn_prompt_attn(args: PromptArgs, stream=None) -> None:
+    """Causal attention over packed prompts, alone or behind a prefix in pages."""
+    _check(load().specattn_prompt_attn(C.byref(args), _stream(stream)))
+
+
+def specattn_tree_workspace_size(args: TreeArgs) -> int:
+    return int(load().specattn_tree_workspace_size(C.byref(args)))
+
+
+def specattn_tree_attn(args: TreeArgs, stream=None) -> None:
+    """Sparse decode attention of a tree of drafted tokens."""
+    _check(load().specattn_tree_attn(C.byref(args), _stream(stream)))
 
 
 def specattn_init() -> None:

@@ -1,7 +1,8 @@
 // C ABI of the library: host-side argument checks and dispatch.  Nothing here touches device
 // memory; every check runs before the first launch so that a failing call writes nothing.
-#include "common.h"
+#include "checks.h"
 #include "mx.h"
+#include "serve.h"
 
 #include <algorithm>
 #include <cmath>
@@ -51,10 +52,6 @@ specattn_status check_launch(const char *what)
 }
 
 namespace {
-
-bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
-int log2i(int x) { int s = 0; while ((1 << s) < x) ++s; return s; }
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 specattn_status check_select(const specattn_select_args *s, bool fused)
 {
@@ -121,15 +118,6 @@ specattn_status check_attn(const specattn_attn_args *a, bool fused)
                                a->kv_stride_n, paged ? a->kv_stride_page : 0};
     for (int64_t st : strides)
         if ((st * (int64_t)es) % 16) { set_error("strides must be multiples of 16 bytes"); return SPECATTN_EALIGN; }
-    return SPECATTN_OK;
-}
-
-specattn_status check_workspace(const void *ws, size_t have, size_t need)
-{
-    if (need == 0) return SPECATTN_OK;
-    if (!ws) { set_error("workspace is NULL, %zu bytes needed", need); return SPECATTN_EWORKSPACE; }
-    if (!aligned(ws, 256)) { set_error("workspace must be 256-byte aligned"); return SPECATTN_EWORKSPACE; }
-    if (have < need) { set_error("workspace has %zu bytes, %zu needed", have, need); return SPECATTN_EWORKSPACE; }
     return SPECATTN_OK;
 }
 
@@ -221,30 +209,6 @@ AttnLaunch make_attn(const specattn_attn_args *a)
 }
 
 // ---- the 4-bit cache and the eviction --------------------------------------------------------
-specattn_status check_pages(const int32_t *page_table, int page_size, int max_pages, int n_max)
-{
-    if (!is_pow2(page_size)) { set_error("page_size must be a power of two"); return SPECATTN_ESHAPE; }
-    if (page_table && (int64_t)max_pages * page_size < n_max) { set_error("page table is shorter than n_max"); return SPECATTN_ESHAPE; }
-    return SPECATTN_OK;
-}
-
-// Whether rows of `bytes` bytes (or elements) at these strides share any: dimension by dimension from the smallest stride up, each has to lie beyond all that
-// the ones before it reach.
-struct Dim { int64_t size; __int128 stride; };
-bool rows_overlap(Dim a, Dim b, Dim c, int64_t bytes)
-{
-    Dim dims[] = {a, b, c};
-    for (Dim &d : dims) d.stride = d.stride < 0 ? -d.stride : d.stride;
-    std::sort(dims, dims + 3, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
-    __int128 reach = bytes;
-    for (const Dim &d : dims) {
-        if (d.size <= 1) continue;
-        if (d.stride < reach) return true;
-        reach += (d.size - 1) * d.stride;
-    }
-    return false;
-}
-
 specattn_status check_mx_cache(const specattn_mx_cache *c, bool pool)
 {
     if (!c->codes || !c->scales) { set_error("codes and scales must not be NULL"); return SPECATTN_EINVAL; }
@@ -832,6 +796,10 @@ specattn_status specattn_init(void)
     if (sm != SPECATTN_OK) return sm;
     const specattn_status sx = mx_attn_configure();
     if (sx != SPECATTN_OK) return sx;
+    const specattn_status sp = prompt_configure();
+    if (sp != SPECATTN_OK) return sp;
+    const specattn_status str = tree_configure();
+    if (str != SPECATTN_OK) return str;
     return attn_mfma_configure();
 }
 

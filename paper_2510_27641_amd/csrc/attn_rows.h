@@ -1,0 +1,466 @@
+// Attention of many query rows per kv head (prompts, trees of drafted tokens; bf16 or fp16, d = 128 or 64): the tile loop that
+// both kernels share.
+//
+// A workgroup of four waves takes up to 32 * WQ query rows of one kv head - rows of all its query heads, which share keys and
+// values - over tiles of keys and values.  Tiles go from memory straight to LDS (16-byte chunks in a swizzled order), two
+// buffers in turn: behind one barrier per tile, the next tile is requested and this one computed.
+//   S^T = K Q^T    : mfma 32x32x16, A = K fragment (ds_read_b128), B = Q fragment (registers)
+//   softmax        : one pass, a running reference per query row that follows its maximum up
+//   O^T += V^T P^T : A = V^T fragment (ds_read_b64_tr_b16), B = P
+// A query row is a column of S^T and O^T and stays in one lane and the lane 32 beyond it: the 16 scores that a lane holds of 32
+// positions are, eight by eight, the B fragment of the second product when the positions of its k-steps are numbered the same
+// way (slot 8 h + j of 16 stands for position 8 (j / 4) + 4 h + j % 4), so weights never leave their lane.
+// With WQ < 4 the waves share query rows and take different positions of a tile; their results are joined in LDS at the end.
+#pragma once
+
+#include "serve.h"
+
+namespace specattn {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int WAVES = 4;
+constexpr int THREADS = WAVES * 64;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// The element types.  Weights are taken in units of 2^ref, the row's running reference: the largest lies between 2^HEAD and 2^(HEAD + SLACK)
+// of them, and a tile moves the reference only when it leaves that range (that scales all accumulators).  bf16 has the exponents of
+// fp32.  fp16 ends at 2^-24: with 2^12 for the largest, weights down to 2^-36 of it are still told apart.
+template <bool F16> struct Half;
+template <> struct Half<false> {
+    static constexpr float HEAD = 0.0f, SLACK = 8.0f;
+    typedef bf16x8 x8;
+    typedef bf16x2 x2;
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+};
+template <> struct Half<true> {
+    static constexpr float HEAD = 12.0f, SLACK = 3.0f;
+    typedef f16x8 x8;
+    typedef f16x2 x2;
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float widen(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
+};
+
+// Two values in the element type, the first in the low half (round to nearest even).
+template <bool F16> __device__ __forceinline__ uint32_t pack2(float x, float y)
+{
+    const f32x2 pair = {x, y};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, typename Half<F16>::x2));
+}
+
+template <int D, int WQ> struct Geo {
+    static constexpr int WK = WAVES / WQ;                     // waves that share query rows
+    static constexpr int SUBS = WK == 1 ? 2 : 1;              // pieces of 32 positions of a tile that a wave takes
+    static constexpr int SPAN = 32 * SUBS;                    // its positions of a tile
+    static constexpr int TILE = SPAN * WK;
+    static constexpr int QROWS = 32 * WQ;
+    static constexpr int ROW_BYTES = D * 2;
+    static constexpr int CHUNKS = ROW_BYTES / 16;             // lanes that fetch a row
+    static constexpr int RPI = 64 / CHUNKS;                   // rows that a wave fetches at a time
+    static constexpr int LOADS = TILE / RPI / WAVES;          // times it does so, of keys and of values
+    static constexpr int TILE_BYTES = TILE * ROW_BYTES;
+    static constexpr int STAGE_BYTES = 2 * TILE_BYTES;        // keys, values
+    static constexpr int OFF_ML = 2 * STAGE_BYTES;            // float[2][WAVES][32]: references and sums of the waves' rows
+    static constexpr int LDS_BYTES = OFF_ML + 2 * WAVES * 32 * 4;
+    static_assert(WAVES * 32 * D * 4 <= OFF_ML, "the waves' results are laid out over the tile buffers");
+    // 16-byte chunk c of row r lies in place c ^ swz(r): both the key reads (a chunk of 32 rows) and the transposing value reads (4 rows x
+    // 32 bytes to 16 lanes) then spread over all banks.
+    static __device__ __forceinline__ int swz(int row)
+    {
+        return D == 128 ? ((row & 7) << 1) | ((row >> 3) & 1) : (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
+    }
+};
+
+// 16 bytes per lane from memory to LDS, to `to` + 16 * lane.  Written out because the compiler, which cannot tell where such a load goes,
+// makes every read of LDS wait for it; the loop's own wait stands ahead of its barrier.
+__device__ __forceinline__ void load_to_lds(const void *src, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(to) : "memory", "m0");
+}
+// All loads of this wave have arrived, LDS is read and written, and the other waves are here.
+__device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
+
+// Over the two lanes that hold a query row.
+__device__ __forceinline__ float pair_max(float x)
+{
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+__device__ __forceinline__ float pair_sum(float x)
+{
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+
+// The low `n` bits (none below 1, all from 64 on).
+__device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+// What a tile is to a wave.
+enum Seen { NOTHING = 0, EVERYTHING = 1, SOME = 2 };
+
+// One wave's 32 query rows.
+// PARTS: parts of the element type that a weight enters the second product in.  Where the result is asked for in that type alone, one:
+// its rounding (half a step, averaged over the row) is below the result's own.  Where it is asked for in fp32, two.
+template <int D, bool F16, int WQ, int PARTS> struct RowsOfWave {
+    typedef Geo<D, WQ> G;
+    typedef typename Half<F16>::x8 x8;
+    x8 q[D / 16];
+    f32x16 o[D / 32];
+    float ref, sum;                                           // in powers of two; of this lane's positions alone
+    float scale;                                              // of the scores, log2(e) in it
+    uint32_t key_at, value_at;                                // where this lane's first fragments lie in a tile
+
+    __device__ __forceinline__ void start(int wk, float sm_scale)
+    {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) o[t] = f32x16{};
+        ref = -INFINITY;
+        sum = 0.0f;
+        scale = sm_scale * LOG2E;
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        const int krow = lane & 31;
+        key_at = (wk * G::SPAN + krow) * G::ROW_BYTES + ((half ^ G::swz(krow)) << 4);
+        const int vrow = 4 * half + ((lane & 15) >> 2);       // of eight, and the 16 bytes of a row's first 64 that hold its elements
+        const int chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        value_at = G::TILE_BYTES + (wk * G::SPAN + vrow) * G::ROW_BYTES + ((chunk ^ G::swz(vrow)) << 4) + 8 * (lane & 1);
+    }
+
+    // buf: the tile in LDS.  `seen` bit i: position i of this wave's part of the tile is attended to.
+    template <bool MASKED> __device__ __forceinline__ void tile(const char *buf, uint64_t seen)
+    {
+        f32x16 s[G::SUBS];
+#pragma unroll
+        for (int u = 0; u < G::SUBS; ++u) s[u] = f32x16{};
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+            for (int u = 0; u < G::SUBS; ++u) {
+                const x8 k = *reinterpret_cast<const x8 *>(buf + ((key_at ^ (c << 5)) + u * 32 * G::ROW_BYTES));
+                s[u] = Half<F16>::mfma(k, q[c], s[u]);
+            }
+        if (MASKED) {
+            const uint64_t mine = seen >> (4 * ((threadIdx.x & 63) >> 5));
+#pragma unroll
+            for (int u = 0; u < G::SUBS; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!((mine >> (32 * u + 8 * (i / 4) + i % 4)) & 1)) s[u][i] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < G::SUBS; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+        top = pair_max(top) * scale;
+        if (__any(top > ref + Half<F16>::SLACK)) {
+            const float next = fmaxf(ref, top);
+            const float by = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
+            ref = next;
+            sum *= by;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] *= by;
+        }
+        const float from = ref == -INFINITY ? 0.0f : Half<F16>::HEAD - ref;
+#pragma unroll
+        for (int u = 0; u < G::SUBS; ++u) {
+            float w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], scale, from));
+                sum += w[i];
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                u32x4 p[PARTS];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = w[8 * b + 2 * i], y = w[8 * b + 2 * i + 1];
+                    p[0][i] = pack2<F16>(x, y);
+                    if (PARTS == 2) p[PARTS - 1][i] = pack2<F16>(x - Half<F16>::widen((uint16_t)p[0][i]), y - Half<F16>::widen((uint16_t)(p[0][i] >> 16)));
+                }
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) {
+                    const uint32_t at = (value_at ^ (t << 6)) + (u * 32 + b * 16) * G::ROW_BYTES;
+                    const uint32_t at8 = (value_at ^ (t << 6) ^ 16) + (u * 32 + b * 16 + 8) * G::ROW_BYTES;
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at8));
+                    const x8 v = __builtin_bit_cast(x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) o[t] = Half<F16>::mfma(v, __builtin_bit_cast(x8, p[part]), o[t]);
+                }
+            }
+        }
+    }
+
+    // Whether a row with finite scores holds a value that is not finite: an infinity or NaN behind its mask came in as 0 * infinity, or
+    // large values passed fp32 ahead of the division.
+    __device__ __forceinline__ bool spoiled() const
+    {
+        float x = 0.0f;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x = fmaf(o[t][i], 0.0f, x);
+        return !(x == 0.0f) && sum - sum == 0.0f && ref > -INFINITY && ref < INFINITY;
+    }
+
+    // Result of this wave into its part of the LDS: unnormalised rows (16-byte chunks in a swizzled order), references and sums.
+    __device__ __forceinline__ void leave(char *smem)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 31, half = lane >> 5;
+        char *mine = smem + wave * 32 * D * 4;
+        sum = pair_sum(sum);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 x = {o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+                *reinterpret_cast<f32x4 *>(mine + row * D * 4 + (((8 * t + 2 * j + half) ^ (row & (D / 4 - 1))) << 4)) = x;
+            }
+        if (half == 0) {
+            float *ml = reinterpret_cast<float *>(smem + G::OFF_ML);
+            ml[wave * 32 + row] = ref;
+            ml[WAVES * 32 + wave * 32 + row] = sum;
+        }
+    }
+};
+
+// Four elements at 4 * chunk of query row `row` of the wave whose part begins at `part`.
+template <int D> __device__ __forceinline__ f32x4 left_row(const char *part, int row, int chunk)
+{
+    return *reinterpret_cast<const f32x4 *>(part + row * D * 4 + ((chunk ^ (row & (D / 4 - 1))) << 4));
+}
+
+// Rows joined over the waves that share them: eight elements at 8 * `at` of query row `row` (of 32 * WQ).
+struct Joined {
+    float ref, sum;
+    float o[8];
+};
+template <int D, int WQ> __device__ __forceinline__ Joined joined(const char *smem, int row, int at)
+{
+    typedef Geo<D, WQ> G;
+    const float *ml = reinterpret_cast<const float *>(smem + G::OFF_ML);
+    const int wq = row >> 5, in = row & 31;
+    Joined j;
+    j.ref = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < G::WK; ++k) j.ref = fmaxf(j.ref, ml[(k * WQ + wq) * 32 + in]);
+    j.sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < G::WK; ++k) {
+        const int wave = k * WQ + wq;
+        const float m = ml[wave * 32 + in];
+        if (m == -INFINITY) continue;                         // nothing was attended to (its values are zeros)
+        const float f = __builtin_amdgcn_exp2f(m - j.ref);    // (NaN where scores were)
+        j.sum = fmaf(f, ml[WAVES * 32 + wave * 32 + in], j.sum);
+        const f32x4 a = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at), b = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            j.o[i] = fmaf(f, a[i], j.o[i]);
+            j.o[4 + i] = fmaf(f, b[i], j.o[4 + i]);
+        }
+    }
+    return j;
+}
+
+// log-sum-exp of a row.
+template <bool F16> __device__ __forceinline__ float log_sum(float ref, float sum)
+{
+    return sum == 0.0f ? -INFINITY : (ref - Half<F16>::HEAD + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// Eight elements of a finished row.
+template <bool F16> __device__ __forceinline__ void store_row(float *out, void *out_lowp, int64_t element, const float (&o)[8], float by)
+{
+    if (out) {
+        const f32x4 a = {o[0] * by, o[1] * by, o[2] * by, o[3] * by}, b = {o[4] * by, o[5] * by, o[6] * by, o[7] * by};
+        *reinterpret_cast<f32x4 *>(out + element) = a;
+        *reinterpret_cast<f32x4 *>(out + element + 4) = b;
+    }
+    if (out_lowp) {
+        const u32x4 x = {pack2<F16>(o[0] * by, o[1] * by), pack2<F16>(o[2] * by, o[3] * by), pack2<F16>(o[4] * by, o[5] * by), pack2<F16>(o[6] * by, o[7] * by)};
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(out_lowp) + element) = x;
+    }
+}
+
+// Where the keys and values of one kv head lie: `count` ranks of the cache - the entries of a list of positions, of chunks or of pool slots,
+// or positions themselves - and behind them, in a tile of their own, `nodes` rows of new tokens.  A rank beyond the last one reads the last
+// one's row, an entry outside the cache the nearest row inside it: what is read always belongs to the call.
+struct CacheRows {
+    const char *k, *v;
+    int64_t stride_n, stride_page;                            // bytes
+    const int32_t *list;                                      // null: rank = position
+    const int32_t *table;                                     // the sequence's pages, or null
+    int chunk_shift, page_shift, pages;                       // pages 0: contiguous
+    int slots;                                                // positions (or pool slots) there are
+    int count;
+    const char *k_new, *v_new;
+    int nodes;
+
+    __device__ __forceinline__ int word(int rank) const { return list ? list[rank >> chunk_shift] : rank; }
+    __device__ __forceinline__ int position(int rank, int w) const
+    {
+        if (list && chunk_shift) {
+            w = min(max(w, 0), (slots - 1) >> chunk_shift);
+            w = (w << chunk_shift) | (rank & ((1 << chunk_shift) - 1));
+        }
+        return min(max(w, 0), slots - 1);
+    }
+    __device__ __forceinline__ int page(int pos) const { return table ? table[pos >> page_shift] : pages ? pos >> page_shift : 0; }
+    __device__ __forceinline__ int64_t offset(int pos, int pg) const
+    {
+        if (!pages) return pos * stride_n;
+        return min(max(pg, 0), pages - 1) * stride_page + (pos & ((1 << page_shift) - 1)) * stride_n;
+    }
+};
+
+// Tiles [first, last) of `src` for this workgroup; the tiles behind `cached` hold the new tokens.  `seen(tile, word)`: what a tile is to this
+// wave.  On return every wave is done with the tile buffers.
+template <int D, bool F16, int WQ, int PARTS, bool LISTED, typename SEEN>
+__device__ __forceinline__ void run_tiles(RowsOfWave<D, F16, WQ, PARTS> &rows, const CacheRows &src, int first, int last, int cached, char *smem, SEEN &&seen)
+{
+    typedef Geo<D, WQ> G;
+    constexpr int N = G::LOADS;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t to = lds_address(smem) + wave * 1024;
+    const int row0 = wave * G::RPI + lane / G::CHUNKS;        // this lane's first row of a tile; the others lie WAVES * RPI apart
+    int chunk[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) chunk[i] = ((lane & (G::CHUNKS - 1)) ^ G::swz(row0 + i * WAVES * G::RPI)) * 16;
+    // A tile's rows are found in up to three steps - list entries, pages, addresses - one iteration apart, so that none waits for the one
+    // before it: iteration t requests the entries of tile t + 3, the pages of t + 2 and the rows of t + 1.
+    int word[N], rank_of[N], pos[N], pg[N];
+    auto ask_words = [&](int t) {
+        if (!LISTED || t >= cached) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            rank_of[i] = min(t * G::TILE + row0 + i * WAVES * G::RPI, src.count - 1);
+            word[i] = src.word(rank_of[i]);
+        }
+    };
+    auto ask_pages = [&](int t) {
+        if (t >= cached) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (LISTED) pos[i] = src.position(rank_of[i], word[i]);
+            else pos[i] = min(t * G::TILE + row0 + i * WAVES * G::RPI, src.count - 1);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) pg[i] = src.page(pos[i]);
+    };
+    int64_t off[N];
+    auto find_rows = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            off[i] = chunk[i] + (t < cached ? src.offset(pos[i], pg[i]) : (int64_t)min(row0 + i * WAVES * G::RPI, src.nodes - 1) * G::ROW_BYTES);
+    };
+    auto ask_rows = [&](int t) {
+        const char *k = t < cached ? src.k : src.k_new, *v = t < cached ? src.v : src.v_new;
+        const uint32_t buf = to + (t & 1) * G::STAGE_BYTES;
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_to_lds(k + off[i], buf + i * WAVES * 1024);
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_to_lds(v + off[i], buf + G::TILE_BYTES + i * WAVES * 1024);
+    };
+    if (first < last) {
+        ask_words(first);
+        ask_pages(first);
+        ask_words(first + 1);
+        find_rows(first);
+        ask_pages(first + 1);
+        ask_words(first + 2);
+        ask_rows(first);
+    }
+    for (int t = first; t < last; ++t) {
+        tile_barrier();
+        if (t + 1 < last) {
+            find_rows(t + 1);
+            ask_pages(t + 2);
+            ask_words(t + 3);
+            ask_rows(t + 1);
+        }
+        uint64_t word_seen = 0;
+        const Seen what = seen(t, word_seen);
+        const char *buf = smem + (t & 1) * G::STAGE_BYTES;
+        if (what == EVERYTHING) rows.template tile<false>(buf, 0);
+        else if (what == SOME) rows.template tile<true>(buf, word_seen);
+    }
+    tile_barrier();
+}
+
+// Rows of this wave that an infinity or NaN in a place that their mask hides has spoiled (0 * infinity), or whose unnormalised values passed fp32: once
+// more, one row after the other, from what they attend to alone and with weights that add up to 1.  Runs behind leave(), over the same tiles.
+// `query(row)`: the row's query; `seen(tile, word, row)`: as above, for one row of the wave.
+template <int D, bool F16, int WQ, typename QUERY, typename SEEN>
+__device__ __forceinline__ void mend_rows(uint64_t which, float scale, const CacheRows &src, int first, int last, int cached, int wk, char *smem, QUERY query, SEEN seen)
+{
+    typedef Geo<D, WQ> G;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float *ml = reinterpret_cast<float *>(smem + G::OFF_ML) + wave * 32;
+    char *mine = smem + wave * 32 * D * 4;
+    uint32_t left = (uint32_t)which | (uint32_t)(which >> 32);
+    while (left) {
+        const int row = __ffs(left) - 1;
+        left &= left - 1;
+        const float ref = ml[row], sum = ml[WAVES * 32 + row];
+        const uint16_t *q = query(row);
+        float x[D / 64], acc[D / 64];
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            x[i] = Half<F16>::widen(q[64 * i + lane]);
+            acc[i] = 0.0f;
+        }
+        for (int t = first; t < last; ++t) {
+            uint64_t word = ~0ull;
+            if (seen(t, word, row) == NOTHING) continue;
+            for (int r = 0; r < G::SPAN; ++r) {
+                if (!((word >> r) & 1)) continue;
+                const int in = wk * G::SPAN + r;
+                int64_t off;
+                if (t < cached) {
+                    const int rank = min(t * G::TILE + in, src.count - 1);
+                    const int pos = src.position(rank, src.word(rank));
+                    off = src.offset(pos, src.page(pos));
+                } else off = (int64_t)min(in, src.nodes - 1) * G::ROW_BYTES;
+                const uint16_t *k = reinterpret_cast<const uint16_t *>((t < cached ? src.k : src.k_new) + off);
+                const uint16_t *v = reinterpret_cast<const uint16_t *>((t < cached ? src.v : src.v_new) + off);
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) s = fmaf(x[i], Half<F16>::widen(k[64 * i + lane]), s);
+#pragma unroll
+                for (int step = 32; step; step >>= 1) s += __shfl_xor(s, step);
+                const float w = __builtin_amdgcn_exp2f(fmaf(s, scale, Half<F16>::HEAD - ref)) / sum;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) acc[i] = fmaf(w, Half<F16>::widen(v[64 * i + lane]), acc[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            const int e = 64 * i + lane;
+            *reinterpret_cast<float *>(mine + row * D * 4 + (((e >> 2) ^ (row & (D / 4 - 1))) << 4) + 4 * (e & 3)) = acc[i];
+        }
+        if (lane == 0) {
+            ml[row] = ref + __builtin_amdgcn_logf(sum);
+            ml[WAVES * 32 + row] = 1.0f;
+        }
+    }
+}
+
+}  // namespace
+}  // namespace specattn
