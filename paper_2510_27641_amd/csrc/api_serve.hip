@@ -69,6 +69,15 @@ specattn_status check_pool(const int32_t *page_table, int page_size, int max_pag
     return SPECATTN_OK;
 }
 
+// Row offsets go to the kernels in units of 16 bytes in 32 bits.
+specattn_status check_reach(int64_t outer, int64_t outer_stride, int64_t inner, int64_t inner_stride)
+{
+    const __int128 reach = (__int128)(outer - 1) * outer_stride + (__int128)(inner - 1) * inner_stride;
+    if (outer_stride < 0 || inner_stride < 0) { set_error("strides must not be negative"); return SPECATTN_ESHAPE; }
+    if (reach * 2 >= ((__int128)1 << 36)) { set_error("the rows of a kv head must lie within 64 GiB of its first one"); return SPECATTN_ESHAPE; }
+    return SPECATTN_OK;
+}
+
 specattn_status check_prompt(const specattn_prompt_args *p)
 {
     if (!p) { set_error("prompt args are NULL"); return SPECATTN_EINVAL; }
@@ -90,6 +99,8 @@ specattn_status check_prompt(const specattn_prompt_args *p)
         if (p->total_kv > (1 << 30)) { set_error("more than 2^30 positions"); return SPECATTN_ESHAPE; }
     }
     if (p->kv_stride_n < p->d) { set_error("kv_stride_n is smaller than d"); return SPECATTN_ESHAPE; }
+    st = p->page_table ? check_reach(p->num_pages, p->kv_stride_page, p->page_size, p->kv_stride_n) : check_reach(1, 0, p->total_kv, p->kv_stride_n);
+    if (st != SPECATTN_OK) return st;
     return check_places({p->q, p->k, p->v, p->out, p->out_lowp}, {p->q_stride_t, p->q_stride_h, p->kv_stride_n, p->kv_stride_h, p->page_table ? p->kv_stride_page : 0});
 }
 
@@ -121,6 +132,8 @@ specattn_status check_tree(const specattn_tree_args *t)
     }
     if (t->kv_stride_n < t->d) { set_error("kv_stride_n is smaller than d"); return SPECATTN_ESHAPE; }
     const bool pool = t->page_table || t->indices_are_physical;
+    st = pool ? check_reach(t->num_pages, t->kv_stride_page, t->page_size, t->kv_stride_n) : check_reach(1, 0, t->n_max, t->kv_stride_n);
+    if (st != SPECATTN_OK) return st;
     return check_places({t->q, t->k, t->v, t->k_new, t->v_new, t->out, t->out_lowp},
                         {t->q_stride_b, t->q_stride_h, t->q_stride_t, t->kv_stride_n, t->kv_stride_h, pool ? t->kv_stride_page : t->kv_stride_b});
 }

@@ -1,16 +1,16 @@
 // Attention of many query rows per kv head (prompts, trees of drafted tokens; bf16 or fp16, d = 128 or 64): the tile loop that
 // both kernels share.
 //
-// A workgroup of four waves takes up to 32 * WQ query rows of one kv head - rows of all its query heads, which share keys and
-// values - over tiles of keys and values.  Tiles go from memory straight to LDS (16-byte chunks in a swizzled order), two
-// buffers in turn: behind one barrier per tile, the next tile is requested and this one computed.
+// A workgroup of four or eight waves takes up to 32 * WQ query rows of one kv head - rows of all its query heads, which share keys and
+// values - over tiles of 64 positions.  Tiles go from memory straight to LDS (16-byte chunks in a swizzled order), into a ring of
+// buffers: behind one barrier per tile, a tile three (d = 64: seven) ahead is requested and this one computed.
 //   S^T = K Q^T    : mfma 32x32x16, A = K fragment (ds_read_b128), B = Q fragment (registers)
 //   softmax        : one pass, a running reference per query row that follows its maximum up
 //   O^T += V^T P^T : A = V^T fragment (ds_read_b64_tr_b16), B = P
 // A query row is a column of S^T and O^T and stays in one lane and the lane 32 beyond it: the 16 scores that a lane holds of 32
 // positions are, eight by eight, the B fragment of the second product when the positions of its k-steps are numbered the same
 // way (slot 8 h + j of 16 stands for position 8 (j / 4) + 4 h + j % 4), so weights never leave their lane.
-// With WQ < 4 the waves share query rows and take different positions of a tile; their results are joined in LDS at the end.
+// With fewer query rows than the waves have room for, two waves share rows and take one half of a tile each; their results are joined in LDS at the end.
 #pragma once
 
 #include "serve.h"
@@ -29,8 +29,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int WAVES = 4;
-constexpr int THREADS = WAVES * 64;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // The element types.  Weights are taken in units of 2^ref, the row's running reference: the largest lies between 2^HEAD and 2^(HEAD + SLACK)
@@ -52,6 +50,14 @@ template <> struct Half<true> {
     static __device__ __forceinline__ float widen(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
 };
 
+// The kernel's arguments (its only ones) read once more: what follows the tile loop then does not hold registers throughout it.
+template <typename ARGS> __device__ __forceinline__ const ARGS &arguments_again()
+{
+    auto p = (const __attribute__((address_space(4))) ARGS *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const ARGS *)p;
+}
+
 // Two values in the element type, the first in the low half (round to nearest even).
 template <bool F16> __device__ __forceinline__ uint32_t pack2(float x, float y)
 {
@@ -59,21 +65,29 @@ template <bool F16> __device__ __forceinline__ uint32_t pack2(float x, float y)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, typename Half<F16>::x2));
 }
 
-template <int D, int WQ> struct Geo {
-    static constexpr int WK = WAVES / WQ;                     // waves that share query rows
-    static constexpr int SUBS = WK == 1 ? 2 : 1;              // pieces of 32 positions of a tile that a wave takes
+// A workgroup of NW waves, WQ of them side by side over query rows.
+template <int DIM, int NW_, int WQ_> struct Geo {
+    static constexpr int D = DIM, NW = NW_, WQ = WQ_;
+    static constexpr int THREADS = NW * 64;
+    static constexpr int WK = NW / WQ;                        // waves that share query rows
+    static constexpr int SUBS = 2 / WK;                       // pieces of 32 positions of a tile that a wave takes
     static constexpr int SPAN = 32 * SUBS;                    // its positions of a tile
-    static constexpr int TILE = SPAN * WK;
+    static constexpr int TILE = 64;
     static constexpr int QROWS = 32 * WQ;
     static constexpr int ROW_BYTES = D * 2;
     static constexpr int CHUNKS = ROW_BYTES / 16;             // lanes that fetch a row
     static constexpr int RPI = 64 / CHUNKS;                   // rows that a wave fetches at a time
-    static constexpr int LOADS = TILE / RPI / WAVES;          // times it does so, of keys and of values
+    static constexpr int LOADS = TILE / RPI / NW;             // times it does so, of keys and of values
     static constexpr int TILE_BYTES = TILE * ROW_BYTES;
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;        // keys, values
-    static constexpr int OFF_ML = 2 * STAGE_BYTES;            // float[2][WAVES][32]: references and sums of the waves' rows
-    static constexpr int LDS_BYTES = OFF_ML + 2 * WAVES * 32 * 4;
-    static_assert(WAVES * 32 * D * 4 <= OFF_ML, "the waves' results are laid out over the tile buffers");
+    static constexpr int STAGES = 131072 / STAGE_BYTES;       // 128 KB of tiles under way or in use: one workgroup to a CU
+    static constexpr int BATCH = 64;                          // tiles whose rows are looked up at a time
+    static constexpr int OFF_TABLE = STAGES * STAGE_BYTES;    // uint32[BATCH * TILE] where the rows lie, in units of 16 bytes
+    static constexpr int OFF_ML = OFF_TABLE + BATCH * TILE * 4;       // float[2][NW][32]: references and sums of the waves' rows
+    static constexpr int LDS_BYTES = OFF_ML + 2 * NW * 32 * 4;
+    static_assert(NW * 32 * D * 4 <= STAGES * STAGE_BYTES, "the waves' results are laid out over the tile buffers");
+    static_assert(WK == 1 || WK == 2, "a tile has two pieces of 32 positions");
+    static_assert((STAGES & (STAGES - 1)) == 0, "tiles take the buffers in turn");
     // 16-byte chunk c of row r lies in place c ^ swz(r): both the key reads (a chunk of 32 rows) and the transposing value reads (4 rows x
     // 32 bytes to 16 lanes) then spread over all banks.
     static __device__ __forceinline__ int swz(int row)
@@ -86,10 +100,17 @@ template <int D, int WQ> struct Geo {
 // makes every read of LDS wait for it; the loop's own wait stands ahead of its barrier.
 __device__ __forceinline__ void load_to_lds(const void *src, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(to) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory", "m0");
 }
-// All loads of this wave have arrived, LDS is read and written, and the other waves are here.
-__device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the last N loads of this wave have arrived, LDS is read and written, and the other waves are here.
+template <int N> __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
+// The same with the loads of `tiles` tiles of N left under way (at most MOST).
+template <int N, int MOST> __device__ __forceinline__ void tile_barrier_behind(int tiles)
+{
+    if constexpr (MOST == 0) tile_barrier<0>();
+    else if (tiles >= MOST) tile_barrier<MOST * N>();
+    else tile_barrier_behind<N, MOST - 1>(tiles);
+}
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p; }
 
 // Over the two lanes that hold a query row.
@@ -113,8 +134,8 @@ enum Seen { NOTHING = 0, EVERYTHING = 1, SOME = 2 };
 // One wave's 32 query rows.
 // PARTS: parts of the element type that a weight enters the second product in.  Where the result is asked for in that type alone, one:
 // its rounding (half a step, averaged over the row) is below the result's own.  Where it is asked for in fp32, two.
-template <int D, bool F16, int WQ, int PARTS> struct RowsOfWave {
-    typedef Geo<D, WQ> G;
+template <typename G, bool F16, int PARTS> struct RowsOfWave {
+    static constexpr int D = G::D;
     typedef typename Half<F16>::x8 x8;
     x8 q[D / 16];
     f32x16 o[D / 32];
@@ -138,7 +159,7 @@ template <int D, bool F16, int WQ, int PARTS> struct RowsOfWave {
     }
 
     // buf: the tile in LDS.  `seen` bit i: position i of this wave's part of the tile is attended to.
-    template <bool MASKED> __device__ __forceinline__ void tile(const char *buf, uint64_t seen)
+    __device__ __forceinline__ void tile(const char *buf, bool masked, uint64_t seen)
     {
         f32x16 s[G::SUBS];
 #pragma unroll
@@ -150,7 +171,7 @@ template <int D, bool F16, int WQ, int PARTS> struct RowsOfWave {
                 const x8 k = *reinterpret_cast<const x8 *>(buf + ((key_at ^ (c << 5)) + u * 32 * G::ROW_BYTES));
                 s[u] = Half<F16>::mfma(k, q[c], s[u]);
             }
-        if (MASKED) {
+        if (masked) {
             const uint64_t mine = seen >> (4 * ((threadIdx.x & 63) >> 5));
 #pragma unroll
             for (int u = 0; u < G::SUBS; ++u)
@@ -234,7 +255,7 @@ template <int D, bool F16, int WQ, int PARTS> struct RowsOfWave {
         if (half == 0) {
             float *ml = reinterpret_cast<float *>(smem + G::OFF_ML);
             ml[wave * 32 + row] = ref;
-            ml[WAVES * 32 + wave * 32 + row] = sum;
+            ml[G::NW * 32 + wave * 32 + row] = sum;
         }
     }
 };
@@ -250,9 +271,9 @@ struct Joined {
     float ref, sum;
     float o[8];
 };
-template <int D, int WQ> __device__ __forceinline__ Joined joined(const char *smem, int row, int at)
+template <typename G> __device__ __forceinline__ Joined joined(const char *smem, int row, int at)
 {
-    typedef Geo<D, WQ> G;
+    constexpr int D = G::D, WQ = G::WQ;
     const float *ml = reinterpret_cast<const float *>(smem + G::OFF_ML);
     const int wq = row >> 5, in = row & 31;
     Joined j;
@@ -268,7 +289,7 @@ template <int D, int WQ> __device__ __forceinline__ Joined joined(const char *sm
         const float m = ml[wave * 32 + in];
         if (m == -INFINITY) continue;                         // nothing was attended to (its values are zeros)
         const float f = __builtin_amdgcn_exp2f(m - j.ref);    // (NaN where scores were)
-        j.sum = fmaf(f, ml[WAVES * 32 + wave * 32 + in], j.sum);
+        j.sum = fmaf(f, ml[G::NW * 32 + wave * 32 + in], j.sum);
         const f32x4 a = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at), b = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at + 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -304,7 +325,7 @@ template <bool F16> __device__ __forceinline__ void store_row(float *out, void *
 // one's row, an entry outside the cache the nearest row inside it: what is read always belongs to the call.
 struct CacheRows {
     const char *k, *v;
-    int64_t stride_n, stride_page;                            // bytes
+    uint32_t step_n, step_page;                               // between rows and between pages, in units of 16 bytes
     const int32_t *list;                                      // null: rank = position
     const int32_t *table;                                     // the sequence's pages, or null
     int chunk_shift, page_shift, pages;                       // pages 0: contiguous
@@ -323,94 +344,93 @@ struct CacheRows {
         return min(max(w, 0), slots - 1);
     }
     __device__ __forceinline__ int page(int pos) const { return table ? table[pos >> page_shift] : pages ? pos >> page_shift : 0; }
-    __device__ __forceinline__ int64_t offset(int pos, int pg) const
+    // where a row begins, in units of 16 bytes (the host sees to it that these fit in 32 bits)
+    __device__ __forceinline__ uint32_t unit(int pos, int pg) const
     {
-        if (!pages) return pos * stride_n;
-        return min(max(pg, 0), pages - 1) * stride_page + (pos & ((1 << page_shift) - 1)) * stride_n;
+        if (!pages) return (uint32_t)pos * step_n;
+        return (uint32_t)min(max(pg, 0), pages - 1) * step_page + (uint32_t)(pos & ((1 << page_shift) - 1)) * step_n;
     }
 };
 
 // Tiles [first, last) of `src` for this workgroup; the tiles behind `cached` hold the new tokens.  `seen(tile, word)`: what a tile is to this
-// wave.  On return every wave is done with the tile buffers.
-template <int D, bool F16, int WQ, int PARTS, bool LISTED, typename SEEN>
-__device__ __forceinline__ void run_tiles(RowsOfWave<D, F16, WQ, PARTS> &rows, const CacheRows &src, int first, int last, int cached, char *smem, SEEN &&seen)
+// wave.  LOOKUP: rows are found through lists or pages, many tiles' at a time ahead of the first of them, and wait in LDS; otherwise a rank is a position
+// of a contiguous cache.  On return every wave is done with the tile buffers.
+template <typename G, bool F16, int PARTS, bool LOOKUP, typename SEEN>
+__device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, const CacheRows &src, int first, int last, int cached, char *smem, SEEN &&seen)
 {
-    typedef Geo<D, WQ> G;
-    constexpr int N = G::LOADS;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int N = G::LOADS, S = G::STAGES, STEP = G::NW * G::RPI;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t to = lds_address(smem) + wave * 1024;
-    const int row0 = wave * G::RPI + lane / G::CHUNKS;        // this lane's first row of a tile; the others lie WAVES * RPI apart
+    const int row0 = wave * G::RPI + lane / G::CHUNKS;        // this lane's first row of a tile; the others lie STEP apart
+    uint32_t *table = reinterpret_cast<uint32_t *>(smem + G::OFF_TABLE);
     int chunk[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) chunk[i] = ((lane & (G::CHUNKS - 1)) ^ G::swz(row0 + i * WAVES * G::RPI)) * 16;
-    // A tile's rows are found in up to three steps - list entries, pages, addresses - one iteration apart, so that none waits for the one
-    // before it: iteration t requests the entries of tile t + 3, the pages of t + 2 and the rows of t + 1.
-    int word[N], rank_of[N], pos[N], pg[N];
-    auto ask_words = [&](int t) {
-        if (!LISTED || t >= cached) return;
+    for (int i = 0; i < N; ++i) chunk[i] = ((lane & (G::CHUNKS - 1)) ^ G::swz(row0 + i * STEP)) * 16;
+    // (what was asked for so far is waited for here: left to the place where it is used first, the wait would stand inside the loop)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            rank_of[i] = min(t * G::TILE + row0 + i * WAVES * G::RPI, src.count - 1);
-            word[i] = src.word(rank_of[i]);
-        }
-    };
-    auto ask_pages = [&](int t) {
-        if (t >= cached) return;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (LISTED) pos[i] = src.position(rank_of[i], word[i]);
-            else pos[i] = min(t * G::TILE + row0 + i * WAVES * G::RPI, src.count - 1);
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) pg[i] = src.page(pos[i]);
-    };
-    int64_t off[N];
-    auto find_rows = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            off[i] = chunk[i] + (t < cached ? src.offset(pos[i], pg[i]) : (int64_t)min(row0 + i * WAVES * G::RPI, src.nodes - 1) * G::ROW_BYTES);
-    };
-    auto ask_rows = [&](int t) {
-        const char *k = t < cached ? src.k : src.k_new, *v = t < cached ? src.v : src.v_new;
-        const uint32_t buf = to + (t & 1) * G::STAGE_BYTES;
-#pragma unroll
-        for (int i = 0; i < N; ++i) load_to_lds(k + off[i], buf + i * WAVES * 1024);
-#pragma unroll
-        for (int i = 0; i < N; ++i) load_to_lds(v + off[i], buf + G::TILE_BYTES + i * WAVES * 1024);
-    };
-    if (first < last) {
-        ask_words(first);
-        ask_pages(first);
-        ask_words(first + 1);
-        find_rows(first);
-        ask_pages(first + 1);
-        ask_words(first + 2);
-        ask_rows(first);
+    for (int c = 0; c < G::D / 16; ++c) {
+        u32x4 x = __builtin_bit_cast(u32x4, rows.q[c]);
+        asm volatile("" : "+v"(x));
+        rows.q[c] = __builtin_bit_cast(typename Half<F16>::x8, x);
     }
-    for (int t = first; t < last; ++t) {
-        tile_barrier();
-        if (t + 1 < last) {
-            find_rows(t + 1);
-            ask_pages(t + 2);
-            ask_words(t + 3);
-            ask_rows(t + 1);
+    for (int base = first; base < last; base += G::BATCH) {
+        const int end = min(last, base + G::BATCH);
+        if (LOOKUP) {
+            constexpr int E = G::BATCH * G::TILE / G::THREADS;
+            const int from = base * G::TILE, n = (min(end, cached) - base) * G::TILE;
+            int at[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (i * G::THREADS < n) at[i] = src.word(min(from + i * G::THREADS + tid, src.count - 1));
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (i * G::THREADS < n) at[i] = src.position(min(from + i * G::THREADS + tid, src.count - 1), at[i]);
+            int page[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (i * G::THREADS < n) page[i] = src.page(at[i]);
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (i * G::THREADS < n) table[i * G::THREADS + tid] = src.unit(at[i], page[i]);
+            __syncthreads();
         }
-        uint64_t word_seen = 0;
-        const Seen what = seen(t, word_seen);
-        const char *buf = smem + (t & 1) * G::STAGE_BYTES;
-        if (what == EVERYTHING) rows.template tile<false>(buf, 0);
-        else if (what == SOME) rows.template tile<true>(buf, word_seen);
+        auto ask = [&](int t) {
+            uint32_t unit[N];
+            const bool old = t < cached;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int row = row0 + i * STEP;
+                if (!old) unit[i] = (uint32_t)min(row, max(src.nodes, 1) - 1) * (G::ROW_BYTES / 16);
+                else if (LOOKUP) unit[i] = table[(t - base) * G::TILE + row];
+                else unit[i] = src.unit(min(t * G::TILE + row, src.count - 1), 0);
+            }
+            const char *k = old ? src.k : src.k_new, *v = old ? src.v : src.v_new;
+            const uint32_t buf = to + (t & (S - 1)) * G::STAGE_BYTES;
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_to_lds(k + ((uint64_t)unit[i] * 16 + chunk[i]), buf + i * G::NW * 1024);
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_to_lds(v + ((uint64_t)unit[i] * 16 + chunk[i]), buf + G::TILE_BYTES + i * G::NW * 1024);
+        };
+        for (int t = base; t < min(end, base + S - 1); ++t) ask(t);
+        for (int t = base; t < end; ++t) {
+            tile_barrier_behind<2 * N, S - 2>(min(end - 1 - t, S - 2));
+            if (t + S - 1 < end) ask(t + S - 1);
+            uint64_t word = 0;
+            const Seen what = seen(t, word);
+            const char *buf = smem + (t & (S - 1)) * G::STAGE_BYTES;
+            if (what != NOTHING) rows.tile(buf, what == SOME, word);
+        }
+        tile_barrier<0>();
     }
-    tile_barrier();
 }
 
 // Rows of this wave that an infinity or NaN in a place that their mask hides has spoiled (0 * infinity), or whose unnormalised values passed fp32: once
 // more, one row after the other, from what they attend to alone and with weights that add up to 1.  Runs behind leave(), over the same tiles.
 // `query(row)`: the row's query; `seen(tile, word, row)`: as above, for one row of the wave.
-template <int D, bool F16, int WQ, typename QUERY, typename SEEN>
+template <typename G, bool F16, typename QUERY, typename SEEN>
 __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const CacheRows &src, int first, int last, int cached, int wk, char *smem, QUERY query, SEEN seen)
 {
-    typedef Geo<D, WQ> G;
+    constexpr int D = G::D;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float *ml = reinterpret_cast<float *>(smem + G::OFF_ML) + wave * 32;
     char *mine = smem + wave * 32 * D * 4;
@@ -418,7 +438,7 @@ __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const Cac
     while (left) {
         const int row = __ffs(left) - 1;
         left &= left - 1;
-        const float ref = ml[row], sum = ml[WAVES * 32 + row];
+        const float ref = ml[row], sum = ml[G::NW * 32 + row];
         const uint16_t *q = query(row);
         float x[D / 64], acc[D / 64];
 #pragma unroll
@@ -436,7 +456,7 @@ __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const Cac
                 if (t < cached) {
                     const int rank = min(t * G::TILE + in, src.count - 1);
                     const int pos = src.position(rank, src.word(rank));
-                    off = src.offset(pos, src.page(pos));
+                    off = (int64_t)src.unit(pos, src.page(pos)) * 16;
                 } else off = (int64_t)min(in, src.nodes - 1) * G::ROW_BYTES;
                 const uint16_t *k = reinterpret_cast<const uint16_t *>((t < cached ? src.k : src.k_new) + off);
                 const uint16_t *v = reinterpret_cast<const uint16_t *>((t < cached ? src.v : src.v_new) + off);
@@ -457,9 +477,58 @@ __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const Cac
         }
         if (lane == 0) {
             ml[row] = ref + __builtin_amdgcn_logf(sum);
-            ml[WAVES * 32 + row] = 1.0f;
+            ml[G::NW * 32 + row] = 1.0f;
         }
     }
+}
+
+// Query row `c` of partial results in slots slot .. slot + n - 1 ([slot][qrows][D] unnormalised, references and sums [slot][2][qrows]), joined by one
+// wave: D / 8 lanes take a slot's row, eight elements each, and 512 / D slots at a time go side by side; the order of all sums is
+// fixed.  Every lane gets the total and the elements of its place.
+template <int D> __device__ __forceinline__ Joined joined_slots(const float *rows, const float *ml, int64_t slot, int n, int qrows, int c)
+{
+    constexpr int LANES = D / 8, SIDE = 64 / LANES;
+    const int lane = threadIdx.x & 63, e = lane % LANES, side = lane / LANES;
+    Joined j;
+    j.ref = -INFINITY;
+    for (int i = lane; i < n; i += 64) j.ref = fmaxf(j.ref, ml[(slot + i) * 2 * qrows + c]);
+#pragma unroll
+    for (int step = 32; step; step >>= 1) j.ref = fmaxf(j.ref, __shfl_xor(j.ref, step));
+    j.sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
+    constexpr int U = 4;                                      // slots that a lane asks for together
+    for (int i0 = side; i0 < n; i0 += U * SIDE) {
+        f32x4 x[U], y[U];
+        float m[U], l[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = slot + min(i0 + u * SIDE, n - 1);
+            const float *p = rows + (at * qrows + c) * D + 8 * e;
+            m[u] = ml[at * 2 * qrows + c];
+            l[u] = ml[at * 2 * qrows + qrows + c];
+            x[u] = *reinterpret_cast<const f32x4 *>(p);
+            y[u] = *reinterpret_cast<const f32x4 *>(p + 4);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * SIDE >= n || m[u] == -INFINITY) continue;
+            const float f = __builtin_amdgcn_exp2f(m[u] - j.ref);
+            j.sum = fmaf(f, l[u], j.sum);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                j.o[i] = fmaf(f, x[u][i], j.o[i]);
+                j.o[4 + i] = fmaf(f, y[u][i], j.o[4 + i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int step = LANES; step < 64; step *= 2) {
+        j.sum += __shfl_xor(j.sum, step);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) j.o[i] += __shfl_xor(j.o[i], step);
+    }
+    return j;
 }
 
 }  // namespace

@@ -24,7 +24,8 @@ struct PromptArgs {
     void *out_lowp;
     float *slots, *slots_ml;                                  // partial results, as in the tree kernel; slot = unit * parts + part
     int64_t q_t, q_h;                                         // elements
-    int64_t kv_n, kv_h, kv_page;                              // bytes
+    int64_t kv_n, kv_h;                                       // bytes
+    uint32_t step_n, step_page;                               // between rows and pages, in units of 16 bytes
     FastDivisor per_g;
     int B, H_q, H_kv, G, total_q, total_kv, pages, page_shift, max_pages, parts;
     float sm_scale;
@@ -50,7 +51,7 @@ __device__ __forceinline__ Sequence sequence(const PromptArgs &a, int b)
 }
 
 // Unit `index` of a kv head: its sequence, and its number within it (the last one first); false behind the last unit.
-template <int QROWS> __device__ __forceinline__ bool find_unit(const PromptArgs &a, int index, int &b, int &tile, int *wave_sums)
+template <int QROWS, int THREADS> __device__ __forceinline__ bool find_unit(const PromptArgs &a, int index, int &b, int &tile, int *wave_sums)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     __shared__ int found[2];
@@ -67,7 +68,7 @@ template <int QROWS> __device__ __forceinline__ bool find_unit(const PromptArgs 
         if (lane == 63) wave_sums[wave] = up;
         __syncthreads();
         int all = 0, ahead = before + up - n;
-        for (int w = 0; w < WAVES; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             if (w < wave) ahead += wave_sums[w];
             all += wave_sums[w];
         }
@@ -84,16 +85,40 @@ template <int QROWS> __device__ __forceinline__ bool find_unit(const PromptArgs 
     return b >= 0;
 }
 
-template <int D, bool F16, int WQ, int PARTS>
-__global__ __launch_bounds__(THREADS, 2) void prompt_kernel(PromptArgs a)
+__device__ __forceinline__ CacheRows cache_rows(const PromptArgs &a, const Sequence &s, int b, int h)
 {
-    typedef Geo<D, WQ> G;
+    CacheRows src{};
+    const int64_t from = h * a.kv_h + (a.pages ? 0 : (int64_t)s.kv0 * a.kv_n);
+    src.k = a.k + from;
+    src.v = a.v + from;
+    src.step_n = a.step_n; src.step_page = a.step_page;
+    src.table = a.pages ? a.page_table + (int64_t)b * a.max_pages : nullptr;
+    src.page_shift = a.page_shift; src.pages = a.pages;
+    src.slots = max(s.kv_len, 1);
+    src.count = s.kv_len;
+    return src;
+}
+
+// A finished row: query row qr of a sequence's kv head h, elements 8 e .. 8 e + 7.
+template <int D, bool F16> __device__ __forceinline__ void finish_row(const PromptArgs &a, const Joined &j, int q0, int h, int qr, int e)
+{
+    const bool none = j.sum == 0.0f;
+    const int t = a.per_g.divide(qr);
+    const int64_t to = (int64_t)(q0 + t) * a.H_q + h * a.G + qr - t * a.G;
+    store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, j.o, none ? 0.0f : 1.0f / j.sum);
+    if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(j.ref, j.sum);
+}
+
+template <int D, bool F16, int NW, int WQ, int PARTS, bool PAGED>
+__global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a)
+{
+    typedef Geo<D, NW, WQ> G;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    __shared__ int wave_sums[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int wave_sums[NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int index = blockIdx.x / a.H_kv, h = blockIdx.x - index * a.H_kv;
     int b, tile;
-    if (!find_unit<G::QROWS>(a, index, b, tile, wave_sums)) return;
+    if (!find_unit<G::QROWS, G::THREADS>(a, index, b, tile, wave_sums)) return;
     const Sequence s = sequence(a, b);
     const int queries = s.q_len * a.G;                        // below 2^31: so are total_q * H_q
     const int ahead = s.kv_len - s.q_len;                     // token t sees positions up to t + ahead
@@ -103,33 +128,24 @@ __global__ __launch_bounds__(THREADS, 2) void prompt_kernel(PromptArgs a)
     const int part = blockIdx.y;
     const int first = (int)((int64_t)n * part / a.parts), last = (int)((int64_t)n * (part + 1) / a.parts);
 
-    CacheRows src{};
-    const int64_t from = a.pages ? 0 : (int64_t)s.kv0 * a.kv_n;
-    src.k = a.k + h * a.kv_h + from;
-    src.v = a.v + h * a.kv_h + from;
-    src.stride_n = a.kv_n; src.stride_page = a.kv_page;
-    src.table = a.pages ? a.page_table + (int64_t)b * a.max_pages : nullptr;
-    src.page_shift = a.page_shift; src.pages = a.pages;
-    src.slots = max(s.kv_len, 1);
-    src.count = s.kv_len;
-
+    const CacheRows src = cache_rows(a, s, b, h);
     const int wq = wave % WQ, wk = wave / WQ;
-    RowsOfWave<D, F16, WQ, PARTS> rows;
+    RowsOfWave<G, F16, PARTS> rows;
     rows.start(wk, a.sm_scale);
     const int q0 = unit_q0 + wq * 32;
-    auto token = [&](int i) { return a.per_g.divide(min(q0 + i, queries - 1)); };
-    auto query = [&](int i) -> const uint16_t * {
+    auto token = [q0, queries](const PromptArgs &a, int i) { return a.per_g.divide(min(q0 + i, queries - 1)); };
+    auto query = [q0, queries, s, h](const PromptArgs &a, int i) -> const uint16_t * {
         const int c = min(q0 + i, queries - 1), t = a.per_g.divide(c);
         return a.q + (int64_t)(s.q0 + t) * a.q_t + (h * a.G + c - t * a.G) * a.q_h;
     };
-    const uint16_t *mine = query(lane & 31);
+    const uint16_t *mine = query(a, lane & 31);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) rows.q[c] = *reinterpret_cast<const typename Half<F16>::x8 *>(mine + (2 * c + (lane >> 5)) * 8);
     // positions that this lane's row sees, and the fewest and most that a row of the wave does
-    const int sees = max(token(lane & 31) + ahead + 1, 0);
+    const int sees = max(token(a, lane & 31) + ahead + 1, 0);
     const bool live = q0 < queries;
-    const int fewest = __builtin_amdgcn_readfirstlane(max(token(0) + ahead + 1, 0)), most = __builtin_amdgcn_readfirstlane(max(token(31) + ahead + 1, 0));
-    run_tiles<D, F16, WQ, PARTS, false>(rows, src, first, last, n, smem, [&](int t, uint64_t &word) {
+    const int fewest = __builtin_amdgcn_readfirstlane(max(token(a, 0) + ahead + 1, 0)), most = __builtin_amdgcn_readfirstlane(max(token(a, 31) + ahead + 1, 0));
+    run_tiles<G, F16, PARTS, PAGED>(rows, src, first, last, n, smem, [&](int t, uint64_t &word) {
         const int at = t * G::TILE + wk * G::SPAN;
         if (!live || at >= most) return NOTHING;
         if (at + G::SPAN <= fewest) return EVERYTHING;
@@ -138,105 +154,83 @@ __global__ __launch_bounds__(THREADS, 2) void prompt_kernel(PromptArgs a)
     });
     const uint64_t bad = __ballot(live && rows.spoiled());
     rows.leave(smem);
-    if (bad)
-        mend_rows<D, F16, WQ>(bad, rows.scale, src, first, last, n, wk, smem, query, [&](int t, uint64_t &word, int i) {
-            word = low_bits(max(token(i) + ahead + 1, 0) - t * G::TILE - wk * G::SPAN);
+    const PromptArgs &o = arguments_again<PromptArgs>();
+    if (bad) {
+        const CacheRows old = cache_rows(o, s, b, h);
+        mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, n, wk, smem, [&](int i) { return query(o, i); }, [&](int t, uint64_t &word, int i) {
+            word = low_bits(max(token(o, i) + ahead + 1, 0) - t * G::TILE - wk * G::SPAN);
             return SOME;
         });
+    }
     __syncthreads();
     constexpr int LANES = D / 8;
     const int e = tid % LANES;
-    for (int c = tid / LANES; c < G::QROWS; c += THREADS / LANES) {
+    for (int c = tid / LANES; c < G::QROWS; c += G::THREADS / LANES) {
         const int qr = unit_q0 + c;
         if (qr >= queries) break;
-        const Joined j = joined<D, WQ>(smem, c, e);
-        if (a.parts == 1) {
-            const bool none = j.sum == 0.0f;
-            const int t = a.per_g.divide(qr);
-            const int64_t to = (int64_t)(s.q0 + t) * a.H_q + h * a.G + qr - t * a.G;
-            store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, j.o, none ? 0.0f : 1.0f / j.sum);
-            if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(j.ref, j.sum);
-        } else {
-            const int64_t slot = (int64_t)blockIdx.x * a.parts + part;
-            float *o = a.slots + (slot * G::QROWS + c) * D + 8 * e;
-            *reinterpret_cast<f32x4 *>(o) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
-            *reinterpret_cast<f32x4 *>(o + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
+        const Joined j = joined<G>(smem, c, e);
+        if (o.parts == 1) finish_row<D, F16>(o, j, s.q0, h, qr, e);
+        else {
+            const int64_t slot = (int64_t)blockIdx.x * o.parts + part;
+            float *x = o.slots + (slot * G::QROWS + c) * D + 8 * e;
+            *reinterpret_cast<f32x4 *>(x) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
+            *reinterpret_cast<f32x4 *>(x + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
             if (e == 0) {
-                a.slots_ml[slot * 2 * G::QROWS + c] = j.ref;
-                a.slots_ml[slot * 2 * G::QROWS + G::QROWS + c] = j.sum;
+                o.slots_ml[slot * 2 * G::QROWS + c] = j.ref;
+                o.slots_ml[slot * 2 * G::QROWS + G::QROWS + c] = j.sum;
             }
         }
     }
 }
 
-// The parts of a unit joined, in order.
-template <int D, bool F16, int QROWS> __global__ __launch_bounds__(THREADS) void prompt_merge_kernel(PromptArgs a)
+// The parts of a unit joined, in order; a wave for each query row.
+template <int D, bool F16, int QROWS> __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a)
 {
-    __shared__ int wave_sums[WAVES];
+    __shared__ int wave_sums[4];
     const int index = blockIdx.x / a.H_kv, h = blockIdx.x - index * a.H_kv;
     int b, tile;
-    if (!find_unit<QROWS>(a, index, b, tile, wave_sums)) return;
+    if (!find_unit<QROWS, 256>(a, index, b, tile, wave_sums)) return;
     const Sequence s = sequence(a, b);
-    constexpr int LANES = D / 8;
-    const int c = blockIdx.y * (THREADS / LANES) + threadIdx.x / LANES, e = threadIdx.x % LANES;
+    const int c = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int qr = tile * QROWS + c;
     if (c >= QROWS || qr >= s.q_len * a.G) return;
-    float ref = -INFINITY;
-    const int64_t slot0 = (int64_t)blockIdx.x * a.parts;
-    for (int w = 0; w < a.parts; ++w) ref = fmaxf(ref, a.slots_ml[(slot0 + w) * 2 * QROWS + c]);
-    float sum = 0.0f, o[8] = {};
-    for (int w = 0; w < a.parts; ++w) {
-        const int64_t slot = slot0 + w;
-        const float m = a.slots_ml[slot * 2 * QROWS + c];
-        if (m == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(m - ref);
-        sum = fmaf(f, a.slots_ml[slot * 2 * QROWS + QROWS + c], sum);
-        const float *p = a.slots + (slot * QROWS + c) * D + 8 * e;
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(p), y = *reinterpret_cast<const f32x4 *>(p + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            o[i] = fmaf(f, x[i], o[i]);
-            o[4 + i] = fmaf(f, y[i], o[4 + i]);
-        }
-    }
-    const bool none = sum == 0.0f;
-    const int t = a.per_g.divide(qr);
-    const int64_t to = (int64_t)(s.q0 + t) * a.H_q + h * a.G + qr - t * a.G;
-    store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, o, none ? 0.0f : 1.0f / sum);
-    if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(ref, sum);
+    const Joined j = joined_slots<D>(a.slots, a.slots_ml, (int64_t)blockIdx.x * a.parts, a.parts, QROWS, c);
+    if (lane < D / 8) finish_row<D, F16>(a, j, s.q0, h, qr, lane);
 }
 
 typedef void (*PromptKernel)(PromptArgs);
-template <int D, bool F16, int PARTS> PromptKernel by_waves(int wq)
+// Workgroups by query rows: 64 of them to four waves, 256 to eight.
+template <int D, bool F16, int PARTS> PromptKernel by_rows(int qrows, bool paged)
 {
-    return wq == 1 ? prompt_kernel<D, F16, 1, PARTS> : prompt_kernel<D, F16, 4, PARTS>;
+    if (paged) return qrows == 64 ? prompt_kernel<D, F16, 4, 2, PARTS, true> : prompt_kernel<D, F16, 8, 8, PARTS, true>;
+    return qrows == 64 ? prompt_kernel<D, F16, 4, 2, PARTS, false> : prompt_kernel<D, F16, 8, 8, PARTS, false>;
 }
-template <int D, bool F16> PromptKernel by_parts(int parts, int wq) { return parts == 1 ? by_waves<D, F16, 1>(wq) : by_waves<D, F16, 2>(wq); }
-PromptKernel variant(int d, bool f16, int parts, int wq)
+template <int D, bool F16> PromptKernel by_parts(int parts, int qrows, bool paged) { return parts == 1 ? by_rows<D, F16, 1>(qrows, paged) : by_rows<D, F16, 2>(qrows, paged); }
+PromptKernel variant(int d, bool f16, int parts, int qrows, bool paged)
 {
-    return d == 128 ? (f16 ? by_parts<128, true>(parts, wq) : by_parts<128, false>(parts, wq)) : (f16 ? by_parts<64, true>(parts, wq) : by_parts<64, false>(parts, wq));
+    return d == 128 ? (f16 ? by_parts<128, true>(parts, qrows, paged) : by_parts<128, false>(parts, qrows, paged))
+                    : (f16 ? by_parts<64, true>(parts, qrows, paged) : by_parts<64, false>(parts, qrows, paged));
 }
-PromptKernel merge_variant(int d, bool f16, int wq)
+template <int D, bool F16> PromptKernel merge_by_rows(int qrows) { return qrows == 64 ? prompt_merge_kernel<D, F16, 64> : prompt_merge_kernel<D, F16, 256>; }
+PromptKernel merge_variant(int d, bool f16, int qrows)
 {
-    if (d == 128) return f16 ? (wq == 1 ? prompt_merge_kernel<128, true, 32> : prompt_merge_kernel<128, true, 128>) : (wq == 1 ? prompt_merge_kernel<128, false, 32> : prompt_merge_kernel<128, false, 128>);
-    return f16 ? (wq == 1 ? prompt_merge_kernel<64, true, 32> : prompt_merge_kernel<64, true, 128>) : (wq == 1 ? prompt_merge_kernel<64, false, 32> : prompt_merge_kernel<64, false, 128>);
+    return d == 128 ? (f16 ? merge_by_rows<128, true>(qrows) : merge_by_rows<128, false>(qrows)) : (f16 ? merge_by_rows<64, true>(qrows) : merge_by_rows<64, false>(qrows));
 }
-size_t lds_size(int d, int wq)
+size_t lds_size(int d, int qrows)
 {
-    if (d == 128) return wq == 1 ? Geo<128, 1>::LDS_BYTES : Geo<128, 4>::LDS_BYTES;
-    return wq == 1 ? Geo<64, 1>::LDS_BYTES : Geo<64, 4>::LDS_BYTES;
+    return d == 128 ? (qrows == 64 ? Geo<128, 4, 2>::LDS_BYTES : Geo<128, 8, 8>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2>::LDS_BYTES : Geo<64, 8, 8>::LDS_BYTES);
 }
 size_t a256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// How a call is cut: waves over query rows, workgroups per kv head at most (no length is known on the host), parts of a unit.
-struct Cut { int wq, units, parts; };
+// How a call is cut: query rows of a unit, workgroups per kv head at most (no length is known on the host), parts of a unit.
+struct Cut { int qrows, units, parts; };
 Cut cut(const specattn_prompt_args *p)
 {
     Cut c;
     const int64_t queries = (int64_t)p->total_q * (p->H_q / p->H_kv);
-    c.wq = queries <= (int64_t)32 * p->B ? 1 : 4;
-    c.units = (int)(queries / (32 * c.wq) + p->B);
-    const int64_t all = (int64_t)c.units * p->H_kv, wanted = 2 * cu_count();
+    c.qrows = queries <= (int64_t)64 * p->B ? 64 : 256;
+    c.units = (int)(queries / c.qrows + p->B);
+    const int64_t all = (int64_t)c.units * p->H_kv, wanted = cu_count();
     // positions that a sequence has at most, in tiles
     const int64_t reach = p->page_table ? (int64_t)p->max_pages_per_seq * p->page_size : p->total_kv;
     c.parts = (int)std::min<int64_t>(std::max<int64_t>(wanted / all, 1), std::max<int64_t>(reach / 512, 1));
@@ -249,7 +243,7 @@ size_t prompt_workspace_bytes(const specattn_prompt_args *p)
 {
     const Cut c = cut(p);
     if (c.parts == 1) return 0;
-    const size_t rows = (size_t)c.units * p->H_kv * c.parts * 32 * c.wq;
+    const size_t rows = (size_t)c.units * p->H_kv * c.parts * c.qrows;
     return a256(rows * p->d * sizeof(float)) + a256(rows * 2 * sizeof(float));
 }
 
@@ -266,10 +260,10 @@ specattn_status prompt_configure()
     }
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return SPECATTN_OK;
-    for (int k = 0; k < 16; ++k) {
-        const int d = k & 1 ? 128 : 64, wq = k & 8 ? 4 : 1;
-        const size_t bytes = lds_size(d, wq);
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, wq)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
+    for (int k = 0; k < 32; ++k) {
+        const int d = k & 1 ? 128 : 64, qrows = k & 8 ? 256 : 64;
+        const size_t bytes = lds_size(d, qrows);
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, qrows, k & 16)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
             (void)hipGetLastError();
             set_error("cannot reserve %zu bytes of LDS", bytes);
             return SPECATTN_EHIP;
@@ -290,7 +284,8 @@ specattn_status launch_prompt(const specattn_prompt_args *p, hipStream_t stream)
     a.page_table = p->page_table; a.seq_lens = p->seq_lens;
     a.out = p->out; a.lse = p->lse; a.out_lowp = p->out_lowp;
     a.q_t = p->q_stride_t; a.q_h = p->q_stride_h;
-    a.kv_n = p->kv_stride_n * 2; a.kv_h = p->kv_stride_h * 2; a.kv_page = p->kv_stride_page * 2;
+    a.kv_n = p->kv_stride_n * 2; a.kv_h = p->kv_stride_h * 2;
+    a.step_n = (uint32_t)(p->kv_stride_n / 8); a.step_page = (uint32_t)(p->kv_stride_page / 8);
     a.B = p->B; a.H_q = p->H_q; a.H_kv = p->H_kv; a.G = p->H_q / p->H_kv;
     a.per_g = FastDivisor(a.G);
     a.total_q = p->total_q; a.total_kv = p->total_kv;
@@ -300,15 +295,14 @@ specattn_status launch_prompt(const specattn_prompt_args *p, hipStream_t stream)
     a.sm_scale = p->sm_scale > 0.0f ? p->sm_scale : 1.0f / std::sqrt((float)p->d);
     const Cut c = cut(p);
     a.parts = c.parts;
-    const size_t rows = (size_t)c.units * p->H_kv * c.parts * 32 * c.wq;
+    const size_t rows = (size_t)c.units * p->H_kv * c.parts * c.qrows;
     a.slots = static_cast<float *>(p->workspace);
     a.slots_ml = reinterpret_cast<float *>(static_cast<char *>(p->workspace) + a256(rows * p->d * sizeof(float)));
     const bool f16 = p->dtype == SPECATTN_F16;
-    variant(p->d, f16, p->out ? 2 : 1, c.wq)<<<dim3(c.units * p->H_kv, c.parts), THREADS, lds_size(p->d, c.wq), stream>>>(a);
+    variant(p->d, f16, p->out ? 2 : 1, c.qrows, p->page_table)<<<dim3(c.units * p->H_kv, c.parts), c.qrows == 64 ? 256 : 512, lds_size(p->d, c.qrows), stream>>>(a);
     st = check_launch("prompt_kernel");
     if (st != SPECATTN_OK || c.parts == 1) return st;
-    const int per = THREADS / (p->d / 8);
-    merge_variant(p->d, f16, c.wq)<<<dim3(c.units * p->H_kv, (32 * c.wq + per - 1) / per), THREADS, 0, stream>>>(a);
+    merge_variant(p->d, f16, c.qrows)<<<dim3(c.units * p->H_kv, c.qrows / 4), 256, 0, stream>>>(a);
     return check_launch("prompt_merge_kernel");
 }
 

@@ -28,7 +28,8 @@ struct TreeArgs {
     float *slots_ml;
     int2 *parts;                                              // [unit] first and last share of the unit
     int64_t q_b, q_h, q_t;                                    // elements
-    int64_t kv_b, kv_h, kv_n, kv_page;                        // bytes
+    int64_t kv_b, kv_h;                                       // bytes
+    uint32_t step_n, step_page;                               // between rows and pages of the cache, in units of 16 bytes
     int64_t idx_stride;
     FastDivisor per_h, per_t;
     int H_q, H_kv, T, G, n_max, slots_per_row, pages, page_shift, max_pages, chunk_shift, capacity, physical;
@@ -54,9 +55,40 @@ __device__ __forceinline__ int count_of(const TreeArgs &a, int r, int b)
     const int cut = (int)min(max(end - len, (int64_t)0), (int64_t)1 << a.chunk_shift);
     return (c << a.chunk_shift) - cut;
 }
-template <int TILE> __device__ __forceinline__ int tiles_of(int count, int nodes)
+__device__ __forceinline__ int tiles_of(int count, int nodes)
 {
-    return max((count + TILE - 1) / TILE + (nodes > 0), 1);    // (a row without any still has to be written)
+    return max((count + 63) / 64 + (nodes > 0), 1);           // (a row without any still has to be written)
+}
+
+// A row's keys and values.
+template <int D> __device__ __forceinline__ CacheRows cache_rows(const TreeArgs &a, int row, int b, int h)
+{
+    CacheRows src;
+    const int64_t head = h * a.kv_h + (a.pages ? 0 : b * a.kv_b);
+    src.k = a.k + head;
+    src.v = a.v + head;
+    src.step_n = a.step_n; src.step_page = a.step_page;
+    src.list = a.indices ? a.indices + row * a.idx_stride : nullptr;
+    src.table = a.page_table && !a.physical ? a.page_table + (int64_t)b * a.max_pages : nullptr;
+    src.chunk_shift = a.chunk_shift; src.page_shift = a.page_shift; src.pages = a.pages;
+    src.slots = a.slots_per_row;
+    src.count = count_of(a, row, b);
+    src.k_new = a.k_new + (int64_t)row * a.T * D * 2;
+    src.v_new = a.v_new + (int64_t)row * a.T * D * 2;
+    src.nodes = nodes_of(a, b);
+    return src;
+}
+
+// A finished row: query row qr of kv head h, elements 8 e .. 8 e + 7.
+template <int D, bool F16> __device__ __forceinline__ void finish_row(const TreeArgs &a, const Joined &j, int b, int h, int qr, int nodes, int e)
+{
+    const bool none = qr - a.per_t.divide(qr) * a.T >= nodes || j.sum == 0.0f;
+    const int64_t to = ((int64_t)b * a.H_q + h * a.G) * a.T + qr;
+    float o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = none ? 0.0f : j.o[i];
+    store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, o, none ? 0.0f : 1.0f / j.sum);
+    if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(j.ref, j.sum);
 }
 
 struct Shares {
@@ -66,14 +98,15 @@ struct Shares {
     __device__ __forceinline__ int of(int64_t tile) const { return (int)(((tile + 1) * n - 1) / total); }
 };
 
-template <int D, bool F16, int WQ, int PARTS>
-__global__ __launch_bounds__(THREADS, 2) void tree_kernel(TreeArgs a)
+template <int D, bool F16, int NW, int WQ, int PARTS>
+__global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
 {
-    typedef Geo<D, WQ> G;
+    typedef Geo<D, NW, WQ> G;
+    constexpr int THREADS = G::THREADS;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     int *prefix = reinterpret_cast<int *>(smem + G::LDS_BYTES);       // [rows + 1] tiles ahead of a row
-    __shared__ int wave_sums[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int wave_sums[NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     {
         const int per = (a.rows + THREADS - 1) / THREADS;
         int mine = 0;
@@ -81,7 +114,7 @@ __global__ __launch_bounds__(THREADS, 2) void tree_kernel(TreeArgs a)
             const int r = tid * per + i;
             if (r >= a.rows) break;
             const int b = a.per_h.divide(a.row0 + r);
-            const int n = tiles_of<G::TILE>(count_of(a, a.row0 + r, b), nodes_of(a, b)) * a.blocks;
+            const int n = tiles_of(count_of(a, a.row0 + r, b), nodes_of(a, b)) * a.blocks;
             prefix[r + 1] = n;
             mine += n;
         }
@@ -100,7 +133,8 @@ __global__ __launch_bounds__(THREADS, 2) void tree_kernel(TreeArgs a)
         __syncthreads();
     }
     Shares shares;
-    shares.total = prefix[a.rows];
+    auto tiles_before = [&](int row) { return __builtin_amdgcn_readfirstlane(prefix[row]); };
+    shares.total = tiles_before(a.rows);
     shares.n = (int)min((int64_t)gridDim.x, max(shares.total / MIN_TILES, (int64_t)1));
     const int share = blockIdx.x;
     if (share >= shares.n) return;
@@ -109,50 +143,41 @@ __global__ __launch_bounds__(THREADS, 2) void tree_kernel(TreeArgs a)
     int r = 0;                                                // the row that the share begins in
     for (int lo = 0, hi = a.rows; hi - lo > 1;) {
         const int mid = (lo + hi) >> 1;
-        if (prefix[mid] <= at) lo = mid; else hi = mid;
+        if (tiles_before(mid) <= at) lo = mid; else hi = mid;
         r = lo;
     }
     const int wq = wave % WQ, wk = wave / WQ;
     const int queries = a.G * a.T;
     while (at < end) {
-        while (prefix[r + 1] <= at) ++r;
-        const int n = (prefix[r + 1] - prefix[r]) / a.blocks;         // tiles of each of the row's units
-        const int block = (int)(at - prefix[r]) / n;
-        const int64_t unit_at = prefix[r] + (int64_t)block * n;
+        const TreeArgs &a = arguments_again<TreeArgs>();
+        while (tiles_before(r + 1) <= at) ++r;
+        const int row_at = tiles_before(r), n = (tiles_before(r + 1) - row_at) / a.blocks;   // tiles of each of the row's units
+        const int block = (int)(at - row_at) / n;
+        const int64_t unit_at = row_at + (int64_t)block * n;
         const int first = (int)(at - unit_at), last = (int)min((int64_t)n, end - unit_at);
         const int unit = r * a.blocks + block;
         const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
-        CacheRows src;
-        src.k = a.k + h * a.kv_h + (a.pages ? 0 : b * a.kv_b);
-        src.v = a.v + h * a.kv_h + (a.pages ? 0 : b * a.kv_b);
-        src.stride_n = a.kv_n; src.stride_page = a.kv_page;
-        src.list = a.indices ? a.indices + row * a.idx_stride : nullptr;
-        src.table = a.page_table && !a.physical ? a.page_table + (int64_t)b * a.max_pages : nullptr;
-        src.chunk_shift = a.chunk_shift; src.page_shift = a.page_shift; src.pages = a.pages;
-        src.slots = a.slots_per_row;
-        src.count = count_of(a, row, b);
-        src.k_new = a.k_new + (int64_t)row * a.T * D * 2;
-        src.v_new = a.v_new + (int64_t)row * a.T * D * 2;
-        src.nodes = nodes_of(a, b);
+        const CacheRows src = cache_rows<D>(a, row, b, h);
         const int cached = (src.count + G::TILE - 1) / G::TILE;
 
-        RowsOfWave<D, F16, WQ, PARTS> rows;
+        RowsOfWave<G, F16, PARTS> rows;
         rows.start(wk, a.sm_scale);
         const int q0 = block * G::QROWS + wq * 32;
-        auto query = [&](int i) -> const uint16_t * {
+        auto query = [q0, queries, b, h](const TreeArgs &a, int i) -> const uint16_t * {
             const int c = min(q0 + i, queries - 1), g = a.per_t.divide(c);
             return a.q + b * a.q_b + (h * a.G + g) * a.q_h + (c - g * a.T) * a.q_t;
         };
-        const uint16_t *mine = query(lane & 31);
+        auto node_seen = [q0, queries, b](const TreeArgs &a, int nodes, int i) -> uint64_t {      // nodes that query row i of this wave attends to
+            const int c = min(q0 + i, queries - 1), t = c - a.per_t.divide(c) * a.T;
+            return t < nodes ? a.masks[(int64_t)b * a.T + t] & low_bits(nodes) : 0;
+        };
+        const uint16_t *mine = query(a, lane & 31);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) rows.q[c] = *reinterpret_cast<const typename Half<F16>::x8 *>(mine + (2 * c + (lane >> 5)) * 8);
-        auto node_seen = [&](int i) -> uint64_t {             // nodes that query row i of this wave attends to
-            const int c = min(q0 + i, queries - 1), t = c - a.per_t.divide(c) * a.T;
-            return t < src.nodes ? a.masks[(int64_t)b * a.T + t] & low_bits(src.nodes) : 0;
-        };
         const bool live = q0 < queries;                       // (a wave without query rows only fetches)
-        const uint64_t my_nodes = last > cached ? node_seen(lane & 31) >> (wk * G::SPAN) : 0;
-        run_tiles<D, F16, WQ, PARTS, true>(rows, src, first, last, cached, smem, [&](int t, uint64_t &word) {
+        const uint64_t my_nodes = last > cached ? node_seen(a, src.nodes, lane & 31) >> (wk * G::SPAN) : 0;
+        // (a row without anything has a tile in the line all the same, which holds nothing to read)
+        run_tiles<G, F16, PARTS, true>(rows, src, first, src.nodes > 0 ? last : min(last, cached), cached, smem, [&](int t, uint64_t &word) {
             if (!live) return NOTHING;
             if (t >= cached) {
                 if (wk * G::SPAN >= src.nodes) return NOTHING;
@@ -167,41 +192,33 @@ __global__ __launch_bounds__(THREADS, 2) void tree_kernel(TreeArgs a)
         });
         const uint64_t bad = __ballot(live && rows.spoiled());
         rows.leave(smem);
-        if (bad)
-            mend_rows<D, F16, WQ>(bad, rows.scale, src, first, last, cached, wk, smem, query, [&](int t, uint64_t &word, int i) {
-                if (t >= cached) {
-                    word = wk * G::SPAN >= 64 ? 0 : node_seen(i) >> (wk * G::SPAN);
-                    return SOME;
-                }
-                word = low_bits(src.count - t * G::TILE - wk * G::SPAN);
+        const TreeArgs &o = arguments_again<TreeArgs>();
+        if (bad) {
+            const CacheRows old = cache_rows<D>(o, row, b, h);
+            mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, cached, wk, smem, [&](int i) { return query(o, i); }, [&](int t, uint64_t &word, int i) {
+                word = t >= cached ? node_seen(o, old.nodes, i) >> (wk * G::SPAN) : low_bits(old.count - t * G::TILE - wk * G::SPAN);
                 return SOME;
             });
+        }
         __syncthreads();
         const bool whole = first == 0 && last == n;
         const int64_t slot = share + unit;
-        if (first == 0 && tid == 0) a.parts[unit] = make_int2(share, shares.of(unit_at + n - 1));
+        const int nodes = nodes_of(o, b);
+        if (first == 0 && tid == 0) o.parts[unit] = make_int2(share, shares.of(unit_at + n - 1));
         constexpr int LANES = D / 8;                          // that a row takes, eight elements each
         const int e = tid % LANES;
         for (int c = tid / LANES; c < G::QROWS; c += THREADS / LANES) {
             const int qr = block * G::QROWS + c;
             if (qr >= queries) break;
-            const Joined j = joined<D, WQ>(smem, c, e);
-            const int g = a.per_t.divide(qr);
-            if (whole) {
-                const bool none = (qr - g * a.T) >= src.nodes || j.sum == 0.0f;
-                const int64_t to = ((int64_t)b * a.H_q + h * a.G) * a.T + qr;
-                float o[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = none ? 0.0f : j.o[i];
-                store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, o, none ? 0.0f : 1.0f / j.sum);
-                if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(j.ref, j.sum);
-            } else {
-                float *o = a.slots + (slot * G::QROWS + c) * D + 8 * e;
-                *reinterpret_cast<f32x4 *>(o) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
-                *reinterpret_cast<f32x4 *>(o + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
+            const Joined j = joined<G>(smem, c, e);
+            if (whole) finish_row<D, F16>(o, j, b, h, qr, nodes, e);
+            else {
+                float *x = o.slots + (slot * G::QROWS + c) * D + 8 * e;
+                *reinterpret_cast<f32x4 *>(x) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
+                *reinterpret_cast<f32x4 *>(x + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
                 if (e == 0) {
-                    a.slots_ml[slot * 2 * G::QROWS + c] = j.ref;
-                    a.slots_ml[slot * 2 * G::QROWS + G::QROWS + c] = j.sum;
+                    o.slots_ml[slot * 2 * G::QROWS + c] = j.ref;
+                    o.slots_ml[slot * 2 * G::QROWS + G::QROWS + c] = j.sum;
                 }
             }
         }
@@ -210,84 +227,55 @@ __global__ __launch_bounds__(THREADS, 2) void tree_kernel(TreeArgs a)
     }
 }
 
-// Units that several shares worked on: their partial results joined, in the order of the shares.
-template <int D, bool F16, int QROWS> __global__ __launch_bounds__(THREADS) void tree_merge_kernel(TreeArgs a)
+// Units that several shares worked on: their partial results joined, in the order of the shares; a wave for each query row.
+template <int D, bool F16> __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int qrows)
 {
     const int unit = blockIdx.x;
     const int2 parts = a.parts[unit];
     if (parts.x == parts.y) return;
-    constexpr int LANES = D / 8;
     const int r = unit / a.blocks, block = unit - r * a.blocks;
     const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
-    const int c = blockIdx.y * (THREADS / LANES) + threadIdx.x / LANES, e = threadIdx.x % LANES;
-    const int qr = block * QROWS + c;
-    if (c >= QROWS || qr >= a.G * a.T) return;
-    float ref = -INFINITY;
-    for (int w = parts.x; w <= parts.y; ++w) ref = fmaxf(ref, a.slots_ml[(int64_t)(w + unit) * 2 * QROWS + c]);
-    float sum = 0.0f, o[8] = {};
-    for (int w = parts.x; w <= parts.y; ++w) {
-        const int64_t slot = w + unit;
-        const float m = a.slots_ml[slot * 2 * QROWS + c];
-        if (m == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(m - ref);
-        sum = fmaf(f, a.slots_ml[slot * 2 * QROWS + QROWS + c], sum);
-        const float *p = a.slots + (slot * QROWS + c) * D + 8 * e;
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(p), y = *reinterpret_cast<const f32x4 *>(p + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            o[i] = fmaf(f, x[i], o[i]);
-            o[4 + i] = fmaf(f, y[i], o[4 + i]);
-        }
-    }
-    const int g = a.per_t.divide(qr);
-    const bool none = (qr - g * a.T) >= nodes_of(a, b) || sum == 0.0f;
-    if (none)
-        for (int i = 0; i < 8; ++i) o[i] = 0.0f;
-    const int64_t to = ((int64_t)b * a.H_q + h * a.G) * a.T + qr;
-    store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, o, none ? 0.0f : 1.0f / sum);
-    if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(ref, sum);
+    const int c = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int qr = block * qrows + c;
+    if (c >= qrows || qr >= a.G * a.T) return;
+    const Joined j = joined_slots<D>(a.slots, a.slots_ml, parts.x + unit, parts.y - parts.x + 1, qrows, c);
+    if (lane < D / 8) finish_row<D, F16>(a, j, b, h, qr, nodes_of(a, b), lane);
 }
 
-// Waves over the query rows: as many as the rows fill, the others share rows and take positions.
-int row_waves(int queries) { return queries <= 32 ? 1 : queries <= 64 ? 2 : 4; }
+// Workgroups by query rows: 64 of them to four waves, 128 to eight (two share rows), 256 to eight.
+int rows_per_unit(int queries) { return queries <= 64 ? 64 : queries <= 128 ? 128 : 256; }
 
 typedef void (*TreeKernel)(TreeArgs);
-template <int D, bool F16, int PARTS> TreeKernel by_waves(int wq)
+template <int D, bool F16, int PARTS> TreeKernel by_rows(int qrows)
 {
-    return wq == 1 ? tree_kernel<D, F16, 1, PARTS> : wq == 2 ? tree_kernel<D, F16, 2, PARTS> : tree_kernel<D, F16, 4, PARTS>;
+    return qrows == 64 ? tree_kernel<D, F16, 4, 2, PARTS> : qrows == 128 ? tree_kernel<D, F16, 8, 4, PARTS> : tree_kernel<D, F16, 8, 8, PARTS>;
 }
-template <int D, bool F16> TreeKernel by_parts(int parts, int wq) { return parts == 1 ? by_waves<D, F16, 1>(wq) : by_waves<D, F16, 2>(wq); }
-TreeKernel variant(int d, bool f16, int parts, int wq)
+template <int D, bool F16> TreeKernel by_parts(int parts, int qrows) { return parts == 1 ? by_rows<D, F16, 1>(qrows) : by_rows<D, F16, 2>(qrows); }
+TreeKernel variant(int d, bool f16, int parts, int qrows)
 {
-    return d == 128 ? (f16 ? by_parts<128, true>(parts, wq) : by_parts<128, false>(parts, wq)) : (f16 ? by_parts<64, true>(parts, wq) : by_parts<64, false>(parts, wq));
+    return d == 128 ? (f16 ? by_parts<128, true>(parts, qrows) : by_parts<128, false>(parts, qrows))
+                    : (f16 ? by_parts<64, true>(parts, qrows) : by_parts<64, false>(parts, qrows));
 }
-template <int D, bool F16> TreeKernel merge_by_waves(int wq) { return wq == 1 ? tree_merge_kernel<D, F16, 32> : wq == 2 ? tree_merge_kernel<D, F16, 64> : tree_merge_kernel<D, F16, 128>; }
-TreeKernel merge_variant(int d, bool f16, int wq)
+size_t lds_size(int d, int qrows, int rows)
 {
-    return d == 128 ? (f16 ? merge_by_waves<128, true>(wq) : merge_by_waves<128, false>(wq)) : (f16 ? merge_by_waves<64, true>(wq) : merge_by_waves<64, false>(wq));
+    const size_t tiles = d == 128 ? (qrows == 64 ? Geo<128, 4, 2>::LDS_BYTES : Geo<128, 8, 4>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2>::LDS_BYTES : Geo<64, 8, 4>::LDS_BYTES);
+    return tiles + (size_t)(rows + 1) * 4;
 }
-size_t tile_lds(int d, int wq)
-{
-    if (d == 128) return wq == 1 ? Geo<128, 1>::LDS_BYTES : wq == 2 ? Geo<128, 2>::LDS_BYTES : Geo<128, 4>::LDS_BYTES;
-    return wq == 1 ? Geo<64, 1>::LDS_BYTES : wq == 2 ? Geo<64, 2>::LDS_BYTES : Geo<64, 4>::LDS_BYTES;
-}
-size_t lds_size(int d, int wq, int rows) { return tile_lds(d, wq) + (size_t)(rows + 1) * 4; }
 size_t a256(size_t x) { return (x + 255) & ~(size_t)255; }
-int workgroups(int d, int wq) { return cu_count() * (d == 128 && wq == 1 ? 1 : 2); }
 
 struct Layout { size_t parts, rows, ml; };
-Layout layout(int d, int wq, int units)
+Layout layout(int d, int qrows, int units)
 {
-    const size_t slots = (size_t)workgroups(d, wq) + units;
-    return {a256((size_t)units * sizeof(int2)), slots * 32 * wq * d * sizeof(float), a256(slots * 2 * 32 * wq * sizeof(float))};
+    const size_t slots = (size_t)cu_count() + units;
+    return {a256((size_t)units * sizeof(int2)), slots * qrows * d * sizeof(float), a256(slots * 2 * qrows * sizeof(float))};
 }
 
 }  // namespace
 
 size_t tree_workspace_bytes(const specattn_tree_args *t)
 {
-    const int queries = t->H_q / t->H_kv * t->T, wq = row_waves(queries), blocks = (queries + 32 * wq - 1) / (32 * wq);
-    const Layout l = layout(t->d, wq, (int)std::min<int64_t>((int64_t)t->B * t->H_kv, MAX_UNITS) * blocks);
+    const int queries = t->H_q / t->H_kv * t->T, qrows = rows_per_unit(queries), blocks = (queries + qrows - 1) / qrows;
+    const Layout l = layout(t->d, qrows, (int)std::min<int64_t>((int64_t)t->B * t->H_kv, MAX_UNITS) * blocks);
     return l.parts + l.rows + l.ml;
 }
 
@@ -305,9 +293,9 @@ specattn_status tree_configure()
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return SPECATTN_OK;
     for (int k = 0; k < 24; ++k) {
-        const int d = k & 1 ? 128 : 64, wq = 1 << (k >> 3);
-        const size_t bytes = lds_size(d, wq, MAX_UNITS);
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, wq)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
+        const int d = k & 1 ? 128 : 64, qrows = 64 << (k >> 3);
+        const size_t bytes = lds_size(d, qrows, MAX_UNITS);
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, qrows)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
             (void)hipGetLastError();
             set_error("cannot reserve %zu bytes of LDS", bytes);
             return SPECATTN_EHIP;
@@ -329,7 +317,8 @@ specattn_status launch_tree(const specattn_tree_args *t, hipStream_t stream)
     a.indices = t->indices; a.counts = t->counts; a.page_table = t->page_table;
     a.out = t->out; a.lse = t->lse; a.out_lowp = t->out_lowp;
     a.q_b = t->q_stride_b; a.q_h = t->q_stride_h; a.q_t = t->q_stride_t;
-    a.kv_b = t->kv_stride_b * 2; a.kv_h = t->kv_stride_h * 2; a.kv_n = t->kv_stride_n * 2; a.kv_page = t->kv_stride_page * 2;
+    a.kv_b = t->kv_stride_b * 2; a.kv_h = t->kv_stride_h * 2;
+    a.step_n = (uint32_t)(t->kv_stride_n / 8); a.step_page = (uint32_t)(t->kv_stride_page / 8);
     a.idx_stride = t->idx_stride_row;
     a.per_h = FastDivisor(t->H_kv); a.per_t = FastDivisor(t->T);
     a.H_q = t->H_q; a.H_kv = t->H_kv; a.T = t->T; a.G = t->H_q / t->H_kv; a.n_max = t->n_max;
@@ -342,22 +331,22 @@ specattn_status launch_tree(const specattn_tree_args *t, hipStream_t stream)
     a.chunk_shift = t->chunk_size > 1 ? log2i(t->chunk_size) : 0;
     a.capacity = t->idx_capacity;
     a.sm_scale = t->sm_scale > 0.0f ? t->sm_scale : 1.0f / std::sqrt((float)t->d);
-    const int queries = a.G * a.T, wq = row_waves(queries), rows = t->B * t->H_kv;
-    a.blocks = (queries + 32 * wq - 1) / (32 * wq);
+    const int queries = a.G * a.T, qrows = rows_per_unit(queries), rows = t->B * t->H_kv;
+    a.blocks = (queries + qrows - 1) / qrows;
     const bool f16 = t->dtype == SPECATTN_F16;
-    const Layout l = layout(t->d, wq, std::min(rows, MAX_UNITS) * a.blocks);
+    const Layout l = layout(t->d, qrows, std::min(rows, MAX_UNITS) * a.blocks);
     char *ws = static_cast<char *>(t->workspace);
     a.parts = reinterpret_cast<int2 *>(ws);
     a.slots = reinterpret_cast<float *>(ws + l.parts);
     a.slots_ml = reinterpret_cast<float *>(ws + l.parts + l.rows);
     const int64_t most = t->indices ? (int64_t)t->idx_capacity << a.chunk_shift : t->n_max;
     for (a.row0 = 0; a.row0 < rows; a.row0 += a.rows) {
-        a.rows = (int)std::min<int64_t>({rows - a.row0, MAX_UNITS, (int64_t)(1 << 30) / (a.blocks * (most / 32 + 2))});     // tiles are counted in 31 bits
-        variant(t->d, f16, t->out ? 2 : 1, wq)<<<workgroups(t->d, wq), THREADS, lds_size(t->d, wq, a.rows), stream>>>(a);
+        a.rows = (int)std::min<int64_t>({rows - a.row0, MAX_UNITS, (int64_t)(1 << 30) / (a.blocks * (most / 64 + 2))});     // tiles are counted in 31 bits
+        variant(t->d, f16, t->out ? 2 : 1, qrows)<<<cu_count(), qrows == 64 ? 256 : 512, lds_size(t->d, qrows, a.rows), stream>>>(a);
         st = check_launch("tree_kernel");
         if (st != SPECATTN_OK) return st;
-        const int per = THREADS / (t->d / 8);
-        merge_variant(t->d, f16, wq)<<<dim3(a.rows * a.blocks, (32 * wq + per - 1) / per), THREADS, 0, stream>>>(a);
+        const auto merge = t->d == 128 ? (f16 ? tree_merge_kernel<128, true> : tree_merge_kernel<128, false>) : (f16 ? tree_merge_kernel<64, true> : tree_merge_kernel<64, false>);
+        merge<<<dim3(a.rows * a.blocks, (std::min(queries, qrows) + 3) / 4), 256, 0, stream>>>(a, qrows);
         st = check_launch("tree_merge_kernel");
         if (st != SPECATTN_OK) return st;
     }
