@@ -3,7 +3,7 @@
 //
 // A workgroup of four or eight waves takes up to 32 * WQ query rows of one kv head - rows of all its query heads, which share keys and
 // values - over tiles of 64 positions.  Tiles go from memory straight to LDS (16-byte chunks in a swizzled order), into a ring of
-// buffers: behind one barrier per tile, a tile three (d = 64: seven) ahead is requested and this one computed.
+// buffers, three tiles (d = 64: seven) ahead of their turn.
 //   S^T = K Q^T    : mfma 32x32x16, A = K fragment (ds_read_b128), B = Q fragment (registers)
 //   softmax        : one pass, a running reference per query row that follows its maximum up
 //   O^T += V^T P^T : A = V^T fragment (ds_read_b64_tr_b16), B = P
@@ -104,7 +104,9 @@ __device__ __forceinline__ void load_to_lds(const void *src, uint32_t to)
 }
 // All but the last N loads of this wave have arrived, LDS is read and written, and the other waves are here.
 template <int N> __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
-// The same with the loads of `tiles` tiles of N left under way (at most MOST).
+// The other waves are here; loads under way stay so.
+__device__ __forceinline__ void tile_barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// As tile_barrier with the loads of `tiles` tiles of N left under way (at most MOST).
 template <int N, int MOST> __device__ __forceinline__ void tile_barrier_behind(int tiles)
 {
     if constexpr (MOST == 0) tile_barrier<0>();
@@ -128,9 +130,6 @@ __device__ __forceinline__ float pair_sum(float x)
 // The low `n` bits (none below 1, all from 64 on).
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
-// What a tile is to a wave.
-enum Seen { NOTHING = 0, EVERYTHING = 1, SOME = 2 };
-
 // One wave's 32 query rows.
 // PARTS: parts of the element type that a weight enters the second product in.  Where the result is asked for in that type alone, one:
 // its rounding (half a step, averaged over the row) is below the result's own.  Where it is asked for in fp32, two.
@@ -139,6 +138,8 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
     typedef typename Half<F16>::x8 x8;
     x8 q[D / 16];
     f32x16 o[D / 32];
+    f32x16 s[G::SUBS];                                        // scores of a tile
+    u32x4 p[G::SUBS][2][PARTS];                               // weights of a tile, in the element type
     float ref, sum;                                           // in powers of two; of this lane's positions alone
     float scale;                                              // of the scores, log2(e) in it
     uint32_t key_at, value_at;                                // where this lane's first fragments lie in a tile
@@ -158,21 +159,87 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
         value_at = G::TILE_BYTES + (wk * G::SPAN + vrow) * G::ROW_BYTES + ((chunk ^ G::swz(vrow)) << 4) + 8 * (lane & 1);
     }
 
-    // buf: the tile in LDS.  `seen` bit i: position i of this wave's part of the tile is attended to.
-    __device__ __forceinline__ void tile(const char *buf, bool masked, uint64_t seen)
+    // Fragments are asked for four at a time, a step of four products ahead of their use; the compiler, left alone, asks for each where it is
+    // needed and waits.
+    struct Four { x8 f[4]; };
+    static constexpr int ADD_STEPS = G::SUBS * 2 * (D / 32) / 4, SCORE_STEPS = G::SUBS * (D / 16) / 4;
+    __device__ __forceinline__ Four values(const char *buf, int step) const
     {
-        f32x16 s[G::SUBS];
+        Four x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = step * 4 + i, t = n % (D / 32), b = n / (D / 32);        // 32 elements, 16 positions
+            const uint32_t at = (value_at ^ (t << 6)) + b * 16 * G::ROW_BYTES;
+            const uint32_t at8 = (value_at ^ (t << 6) ^ 16) + (b * 16 + 8) * G::ROW_BYTES;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at8));
+            x.f[i] = __builtin_bit_cast(x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        return x;
+    }
+    __device__ __forceinline__ Four keys(const char *buf, int step) const
+    {
+        Four x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = step * 4 + i, u = n % G::SUBS, c = n / G::SUBS;
+            x.f[i] = *reinterpret_cast<const x8 *>(buf + ((key_at ^ (c << 5)) + u * 32 * G::ROW_BYTES));
+        }
+        return x;
+    }
+    __device__ __forceinline__ void add_step(const Four &x, int step)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = step * 4 + i, t = n % (D / 32), b = n / (D / 32);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) o[t] = Half<F16>::mfma(x.f[i], __builtin_bit_cast(x8, p[b / 2][b % 2][part]), o[t]);
+        }
+    }
+    __device__ __forceinline__ void score_step(const Four &x, int step)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = step * 4 + i, u = n % G::SUBS, c = n / G::SUBS;
+            s[u] = Half<F16>::mfma(x.f[i], q[c], s[u]);
+        }
+    }
+    // Scores of the tile at buf (LDS).
+    __device__ __forceinline__ void score(const char *buf)
+    {
 #pragma unroll
         for (int u = 0; u < G::SUBS; ++u) s[u] = f32x16{};
+        Four ready = keys(buf, 0);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c)
+        for (int step = 0; step < SCORE_STEPS; ++step) {
+            Four next = ready;
+            if (step + 1 < SCORE_STEPS) next = keys(buf, step + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            score_step(ready, step);
+            __builtin_amdgcn_sched_barrier(0);
+            ready = next;
+        }
+    }
+    // Weighted values of the tile at buf; its first fragments are in `ready`.
+    __device__ __forceinline__ void add(const char *buf, Four ready)
+    {
 #pragma unroll
-            for (int u = 0; u < G::SUBS; ++u) {
-                const x8 k = *reinterpret_cast<const x8 *>(buf + ((key_at ^ (c << 5)) + u * 32 * G::ROW_BYTES));
-                s[u] = Half<F16>::mfma(k, q[c], s[u]);
-            }
-        if (masked) {
-            const uint64_t mine = seen >> (4 * ((threadIdx.x & 63) >> 5));
+        for (int step = 0; step < ADD_STEPS; ++step) {
+            Four next = ready;
+            if (step + 1 < ADD_STEPS) next = values(buf, step + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            add_step(ready, step);
+            __builtin_amdgcn_sched_barrier(0);
+            ready = next;
+        }
+    }
+
+    // Scores of tile t into weights.
+    template <typename SEEN> __device__ __forceinline__ void weigh(SEEN &&seen, int t)
+    {
+        uint64_t word = 0;
+        if (!seen(t, word)) {
+            const uint64_t mine = word >> (4 * ((threadIdx.x & 63) >> 5));
 #pragma unroll
             for (int u = 0; u < G::SUBS; ++u)
 #pragma unroll
@@ -205,25 +272,14 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
                 sum += w[i];
             }
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                u32x4 p[PARTS];
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float x = w[8 * b + 2 * i], y = w[8 * b + 2 * i + 1];
-                    p[0][i] = pack2<F16>(x, y);
-                    if (PARTS == 2) p[PARTS - 1][i] = pack2<F16>(x - Half<F16>::widen((uint16_t)p[0][i]), y - Half<F16>::widen((uint16_t)(p[0][i] >> 16)));
+                    p[u][b][0][i] = pack2<F16>(x, y);
+                    if (PARTS == 2)
+                        p[u][b][PARTS - 1][i] = pack2<F16>(x - Half<F16>::widen((uint16_t)p[u][b][0][i]), y - Half<F16>::widen((uint16_t)(p[u][b][0][i] >> 16)));
                 }
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    const uint32_t at = (value_at ^ (t << 6)) + (u * 32 + b * 16) * G::ROW_BYTES;
-                    const uint32_t at8 = (value_at ^ (t << 6) ^ 16) + (u * 32 + b * 16 + 8) * G::ROW_BYTES;
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at));
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at8));
-                    const x8 v = __builtin_bit_cast(x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                    for (int part = 0; part < PARTS; ++part) o[t] = Half<F16>::mfma(v, __builtin_bit_cast(x8, p[part]), o[t]);
-                }
-            }
         }
     }
 
@@ -352,11 +408,11 @@ struct CacheRows {
     }
 };
 
-// Tiles [first, last) of `src` for this workgroup; the tiles behind `cached` hold the new tokens.  `seen(tile, word)`: what a tile is to this
-// wave.  LOOKUP: rows are found through lists or pages, many tiles' at a time ahead of the first of them, and wait in LDS; otherwise a rank is a position
+// Tiles [first, last) of the rows that `where()` tells (asked again for every batch of tiles, so that not all of it is held throughout) for this workgroup, of which this wave computes those below `own`; the tiles behind `cached` hold the new tokens.
+// `seen(tile, word)`: whether this wave's rows see all of its part of the tile; if not, word has a bit for each position that this lane's row sees.  LOOKUP: rows are found through lists or pages, many tiles' at a time ahead of the first of them, and wait in LDS; otherwise a rank is a position
 // of a contiguous cache.  On return every wave is done with the tile buffers.
-template <typename G, bool F16, int PARTS, bool LOOKUP, typename SEEN>
-__device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, const CacheRows &src, int first, int last, int cached, char *smem, SEEN &&seen)
+template <typename G, bool F16, int PARTS, bool LOOKUP, typename WHERE, typename SEEN>
+__device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, WHERE &&where, int first, int last, int cached, int own, char *smem, SEEN &&seen)
 {
     constexpr int N = G::LOADS, S = G::STAGES, STEP = G::NW * G::RPI;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -375,6 +431,7 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, const
     }
     for (int base = first; base < last; base += G::BATCH) {
         const int end = min(last, base + G::BATCH);
+        const CacheRows src = where();
         if (LOOKUP) {
             constexpr int E = G::BATCH * G::TILE / G::THREADS;
             const int from = base * G::TILE, n = (min(end, cached) - base) * G::TILE;
@@ -412,21 +469,28 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, const
             for (int i = 0; i < N; ++i) load_to_lds(v + ((uint64_t)unit[i] * 16 + chunk[i]), buf + G::TILE_BYTES + i * G::NW * 1024);
         };
         for (int t = base; t < min(end, base + S - 1); ++t) ask(t);
-        for (int t = base; t < end; ++t) {
+        const int mine = min(end, own);                       // tiles that this wave has rows for
+        auto top = [&](int t) {
             tile_barrier_behind<2 * N, S - 2>(min(end - 1 - t, S - 2));
             if (t + S - 1 < end) ask(t + S - 1);
-            uint64_t word = 0;
-            const Seen what = seen(t, word);
+        };
+        int t = base;
+        for (; t < mine; ++t) {
+            top(t);
             const char *buf = smem + (t & (S - 1)) * G::STAGE_BYTES;
-            if (what != NOTHING) rows.tile(buf, what == SOME, word);
+            rows.score(buf);
+            const auto ready = rows.values(buf, 0);
+            rows.weigh(seen, t);
+            rows.add(buf, ready);
         }
+        for (; t < end; ++t) top(t);
         tile_barrier<0>();
     }
 }
 
 // Rows of this wave that an infinity or NaN in a place that their mask hides has spoiled (0 * infinity), or whose unnormalised values passed fp32: once
 // more, one row after the other, from what they attend to alone and with weights that add up to 1.  Runs behind leave(), over the same tiles.
-// `query(row)`: the row's query; `seen(tile, word, row)`: as above, for one row of the wave.
+// `query(row)`: the row's query; `seen(tile, row)`: the positions that a row of the wave sees.
 template <typename G, bool F16, typename QUERY, typename SEEN>
 __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const CacheRows &src, int first, int last, int cached, int wk, char *smem, QUERY query, SEEN seen)
 {
@@ -447,8 +511,7 @@ __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const Cac
             acc[i] = 0.0f;
         }
         for (int t = first; t < last; ++t) {
-            uint64_t word = ~0ull;
-            if (seen(t, word, row) == NOTHING) continue;
+            const uint64_t word = seen(t, row);
             for (int r = 0; r < G::SPAN; ++r) {
                 if (!((word >> r) & 1)) continue;
                 const int in = wk * G::SPAN + r;

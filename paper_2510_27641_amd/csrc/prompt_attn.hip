@@ -128,7 +128,6 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a)
     const int part = blockIdx.y;
     const int first = (int)((int64_t)n * part / a.parts), last = (int)((int64_t)n * (part + 1) / a.parts);
 
-    const CacheRows src = cache_rows(a, s, b, h);
     const int wq = wave % WQ, wk = wave / WQ;
     RowsOfWave<G, F16, PARTS> rows;
     rows.start(wk, a.sm_scale);
@@ -145,21 +144,19 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a)
     const int sees = max(token(a, lane & 31) + ahead + 1, 0);
     const bool live = q0 < queries;
     const int fewest = __builtin_amdgcn_readfirstlane(max(token(a, 0) + ahead + 1, 0)), most = __builtin_amdgcn_readfirstlane(max(token(a, 31) + ahead + 1, 0));
-    run_tiles<G, F16, PARTS, PAGED>(rows, src, first, last, n, smem, [&](int t, uint64_t &word) {
+    const int own = live ? min(last, (max(most - wk * G::SPAN, 0) + G::TILE - 1) / G::TILE) : first;
+    run_tiles<G, F16, PARTS, PAGED>(rows, [&]() { return cache_rows(arguments_again<PromptArgs>(), s, b, h); }, first, last, n, own, smem, [&](int t, uint64_t &word) {
         const int at = t * G::TILE + wk * G::SPAN;
-        if (!live || at >= most) return NOTHING;
-        if (at + G::SPAN <= fewest) return EVERYTHING;
         word = low_bits(sees - at);
-        return SOME;
+        return at + G::SPAN <= fewest;
     });
     const uint64_t bad = __ballot(live && rows.spoiled());
     rows.leave(smem);
     const PromptArgs &o = arguments_again<PromptArgs>();
     if (bad) {
         const CacheRows old = cache_rows(o, s, b, h);
-        mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, n, wk, smem, [&](int i) { return query(o, i); }, [&](int t, uint64_t &word, int i) {
-            word = low_bits(max(token(o, i) + ahead + 1, 0) - t * G::TILE - wk * G::SPAN);
-            return SOME;
+        mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, n, wk, smem, [&](int i) { return query(o, i); }, [&](int t, int i) {
+            return low_bits(max(token(o, i) + ahead + 1, 0) - t * G::TILE - wk * G::SPAN);
         });
     }
     __syncthreads();

@@ -72,10 +72,8 @@ template <int D> __device__ __forceinline__ CacheRows cache_rows(const TreeArgs 
     src.table = a.page_table && !a.physical ? a.page_table + (int64_t)b * a.max_pages : nullptr;
     src.chunk_shift = a.chunk_shift; src.page_shift = a.page_shift; src.pages = a.pages;
     src.slots = a.slots_per_row;
-    src.count = count_of(a, row, b);
     src.k_new = a.k_new + (int64_t)row * a.T * D * 2;
     src.v_new = a.v_new + (int64_t)row * a.T * D * 2;
-    src.nodes = nodes_of(a, b);
     return src;
 }
 
@@ -91,11 +89,21 @@ template <int D, bool F16> __device__ __forceinline__ void finish_row(const Tree
     if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(j.ref, j.sum);
 }
 
+// The line of tiles in n shares, the first `more` of them one tile longer than `each`.
 struct Shares {
-    int64_t total;
-    int n;
-    __device__ __forceinline__ int64_t begin(int w) const { return w * total / n; }
-    __device__ __forceinline__ int of(int64_t tile) const { return (int)(((tile + 1) * n - 1) / total); }
+    int n, each, more;
+    __device__ __forceinline__ Shares(int total, int most)
+    {
+        n = min(most, max(total / MIN_TILES, 1));
+        each = (int)((uint32_t)total / (uint32_t)n);
+        more = total - each * n;
+    }
+    __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int of(int tile) const
+    {
+        const int longer = more * (each + 1);
+        return tile < longer ? (int)((uint32_t)tile / (uint32_t)(each + 1)) : more + (int)((uint32_t)(tile - longer) / (uint32_t)max(each, 1));
+    }
 };
 
 template <int D, bool F16, int NW, int WQ, int PARTS>
@@ -132,14 +140,12 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         if (tid == 0) prefix[0] = 0;
         __syncthreads();
     }
-    Shares shares;
     auto tiles_before = [&](int row) { return __builtin_amdgcn_readfirstlane(prefix[row]); };
-    shares.total = tiles_before(a.rows);
-    shares.n = (int)min((int64_t)gridDim.x, max(shares.total / MIN_TILES, (int64_t)1));
+    const Shares shares(tiles_before(a.rows), gridDim.x);
     const int share = blockIdx.x;
     if (share >= shares.n) return;
-    int64_t at = shares.begin(share);
-    const int64_t end = shares.begin(share + 1);
+    int at = shares.begin(share);
+    const int end = shares.begin(share + 1);
     int r = 0;                                                // the row that the share begins in
     for (int lo = 0, hi = a.rows; hi - lo > 1;) {
         const int mid = (lo + hi) >> 1;
@@ -151,14 +157,14 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
     while (at < end) {
         const TreeArgs &a = arguments_again<TreeArgs>();
         while (tiles_before(r + 1) <= at) ++r;
-        const int row_at = tiles_before(r), n = (tiles_before(r + 1) - row_at) / a.blocks;   // tiles of each of the row's units
-        const int block = (int)(at - row_at) / n;
-        const int64_t unit_at = row_at + (int64_t)block * n;
-        const int first = (int)(at - unit_at), last = (int)min((int64_t)n, end - unit_at);
+        const int row_at = tiles_before(r), n = (int)((uint32_t)(tiles_before(r + 1) - row_at) / (uint32_t)a.blocks);   // tiles of each of the row's units
+        const int block = (int)((uint32_t)(at - row_at) / (uint32_t)n);
+        const int unit_at = row_at + block * n;
+        const int first = at - unit_at, last = min(n, end - unit_at);
         const int unit = r * a.blocks + block;
         const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
-        const CacheRows src = cache_rows<D>(a, row, b, h);
-        const int cached = (src.count + G::TILE - 1) / G::TILE;
+        const int count = count_of(a, row, b), nodes = nodes_of(a, b);
+        const int cached = (count + G::TILE - 1) / G::TILE;
 
         RowsOfWave<G, F16, PARTS> rows;
         rows.start(wk, a.sm_scale);
@@ -175,35 +181,32 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) rows.q[c] = *reinterpret_cast<const typename Half<F16>::x8 *>(mine + (2 * c + (lane >> 5)) * 8);
         const bool live = q0 < queries;                       // (a wave without query rows only fetches)
-        const uint64_t my_nodes = last > cached ? node_seen(a, src.nodes, lane & 31) >> (wk * G::SPAN) : 0;
+        const uint64_t my_nodes = last > cached ? node_seen(a, nodes, lane & 31) >> (wk * G::SPAN) : 0;
         // (a row without anything has a tile in the line all the same, which holds nothing to read)
-        run_tiles<G, F16, PARTS, true>(rows, src, first, src.nodes > 0 ? last : min(last, cached), cached, smem, [&](int t, uint64_t &word) {
-            if (!live) return NOTHING;
-            if (t >= cached) {
-                if (wk * G::SPAN >= src.nodes) return NOTHING;
-                word = my_nodes;
-                return SOME;
-            }
-            const int in = src.count - t * G::TILE - wk * G::SPAN;
-            if (in >= G::SPAN) return EVERYTHING;
-            if (in <= 0) return NOTHING;
-            word = low_bits(in);
-            return SOME;
+        const int stop = nodes > 0 ? last : min(last, cached);
+        auto where = [&]() {
+            CacheRows src = cache_rows<D>(arguments_again<TreeArgs>(), row, b, h);
+            src.count = count;
+            src.nodes = nodes;
+            return src;
+        };
+        run_tiles<G, F16, PARTS, true>(rows, where, first, stop, cached, live ? stop : first, smem, [&](int t, uint64_t &word) {
+            const int in = count - t * G::TILE - wk * G::SPAN;
+            word = t < cached ? low_bits(in) : my_nodes;
+            return t < cached && in >= G::SPAN;
         });
         const uint64_t bad = __ballot(live && rows.spoiled());
         rows.leave(smem);
         const TreeArgs &o = arguments_again<TreeArgs>();
         if (bad) {
-            const CacheRows old = cache_rows<D>(o, row, b, h);
-            mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, cached, wk, smem, [&](int i) { return query(o, i); }, [&](int t, uint64_t &word, int i) {
-                word = t >= cached ? node_seen(o, old.nodes, i) >> (wk * G::SPAN) : low_bits(old.count - t * G::TILE - wk * G::SPAN);
-                return SOME;
+            const CacheRows old = where();
+            mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, cached, wk, smem, [&](int i) { return query(o, i); }, [&](int t, int i) {
+                return t >= cached ? node_seen(o, old.nodes, i) >> (wk * G::SPAN) : low_bits(old.count - t * G::TILE - wk * G::SPAN);
             });
         }
         __syncthreads();
         const bool whole = first == 0 && last == n;
         const int64_t slot = share + unit;
-        const int nodes = nodes_of(o, b);
         if (first == 0 && tid == 0) o.parts[unit] = make_int2(share, shares.of(unit_at + n - 1));
         constexpr int LANES = D / 8;                          // that a row takes, eight elements each
         const int e = tid % LANES;
