@@ -3,7 +3,7 @@
 //
 // A workgroup of four or eight waves takes up to 32 * WQ query rows of one kv head - rows of all its query heads, which share keys and
 // values - over tiles of 64 positions.  Tiles go from memory straight to LDS (16-byte chunks in a swizzled order), into a ring of
-// buffers, three tiles (d = 64: seven) ahead of their turn.
+// buffers, two tiles (d = 64: six) ahead of their turn.
 //   S^T = K Q^T    : mfma 32x32x16, A = K fragment (ds_read_b128), B = Q fragment (registers)
 //   softmax        : one pass, a running reference per query row that follows its maximum up
 //   O^T += V^T P^T : A = V^T fragment (ds_read_b64_tr_b16), B = P
@@ -88,11 +88,11 @@ template <int DIM, int NW_, int WQ_> struct Geo {
     static_assert(NW * 32 * D * 4 <= STAGES * STAGE_BYTES, "the waves' results are laid out over the tile buffers");
     static_assert(WK == 1 || WK == 2, "a tile has two pieces of 32 positions");
     static_assert((STAGES & (STAGES - 1)) == 0, "tiles take the buffers in turn");
-    // 16-byte chunk c of row r lies in place c ^ swz(r): both the key reads (a chunk of 32 rows) and the transposing value reads (4 rows x
-    // 32 bytes to 16 lanes) then spread over all banks.
+    // 16-byte chunk c of row r lies in place c ^ swz(r): both the key reads (a chunk of 16 rows at a time) and the transposing value reads (64 bytes
+    // of 4 rows at a time) then spread over all banks.
     static __device__ __forceinline__ int swz(int row)
     {
-        return D == 128 ? ((row & 7) << 1) | ((row >> 3) & 1) : (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
+        return (D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2) | ((row >> 2) & 3);
     }
 };
 
@@ -170,7 +170,7 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
         for (int i = 0; i < 4; ++i) {
             const int n = step * 4 + i, t = n % (D / 32), b = n / (D / 32);        // 32 elements, 16 positions
             const uint32_t at = (value_at ^ (t << 6)) + b * 16 * G::ROW_BYTES;
-            const uint32_t at8 = (value_at ^ (t << 6) ^ 16) + (b * 16 + 8) * G::ROW_BYTES;
+            const uint32_t at8 = (value_at ^ (t << 6) ^ 32) + (b * 16 + 8) * G::ROW_BYTES;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at));
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(buf + at8));
             x.f[i] = __builtin_bit_cast(x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -204,34 +204,45 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
             s[u] = Half<F16>::mfma(x.f[i], q[c], s[u]);
         }
     }
-    // Scores of the tile at buf (LDS).
-    __device__ __forceinline__ void score(const char *buf)
+    // Weighted values of the tile at `before`, then scores of the one at `now`; the first two steps' fragments are in x.
+    struct Ready { Four x[2]; };
+    template <bool ADD, bool SCORE> __device__ __forceinline__ Four fragments(const char *before, const char *now, int step) const
     {
+        return step < (ADD ? ADD_STEPS : 0) ? values(before, step) : keys(now, step - (ADD ? ADD_STEPS : 0));
+    }
+    template <bool ADD, bool SCORE> __device__ __forceinline__ void multiply(const char *before, const char *now, Ready ready)
+    {
+        if (SCORE) {
 #pragma unroll
-        for (int u = 0; u < G::SUBS; ++u) s[u] = f32x16{};
-        Four ready = keys(buf, 0);
+            for (int u = 0; u < G::SUBS; ++u) s[u] = f32x16{};
+        }
+        constexpr int A = ADD ? ADD_STEPS : 0, ALL = A + (SCORE ? SCORE_STEPS : 0);
+        Four x[3] = {ready.x[0], ready.x[1], ready.x[1]};
+        if (ADD && SCORE && A < 2) x[1] = keys(now, 0);
+        if (!ADD && ALL > 1) x[1] = keys(now, 1);
 #pragma unroll
-        for (int step = 0; step < SCORE_STEPS; ++step) {
-            Four next = ready;
-            if (step + 1 < SCORE_STEPS) next = keys(buf, step + 1);
+        for (int step = 0; step < ALL; ++step) {
+            if (step + 2 < ALL) x[(step + 2) % 3] = fragments<ADD, SCORE>(before, now, step + 2);
             __builtin_amdgcn_sched_barrier(0);
-            score_step(ready, step);
+            if (step < A) add_step(x[step % 3], step);
+            else score_step(x[step % 3], step - A);
             __builtin_amdgcn_sched_barrier(0);
-            ready = next;
         }
     }
-    // Weighted values of the tile at buf; its first fragments are in `ready`.
-    __device__ __forceinline__ void add(const char *buf, Four ready)
+    // The fragments of its first steps that lie in the tile before.
+    __device__ __forceinline__ Ready first_values(const char *before) const
     {
-#pragma unroll
-        for (int step = 0; step < ADD_STEPS; ++step) {
-            Four next = ready;
-            if (step + 1 < ADD_STEPS) next = values(buf, step + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            add_step(ready, step);
-            __builtin_amdgcn_sched_barrier(0);
-            ready = next;
-        }
+        Ready r;
+        r.x[0] = values(before, 0);
+        r.x[1] = ADD_STEPS > 1 ? values(before, 1) : r.x[0];
+        return r;
+    }
+    __device__ __forceinline__ Ready first_keys(const char *now) const
+    {
+        Ready r;
+        r.x[0] = keys(now, 0);
+        r.x[1] = r.x[0];
+        return r;
     }
 
     // Scores of tile t into weights.
@@ -416,6 +427,7 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, WHERE
 {
     constexpr int N = G::LOADS, S = G::STAGES, STEP = G::NW * G::RPI;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = wave >> 2;
     const uint32_t to = lds_address(smem) + wave * 1024;
     const int row0 = wave * G::RPI + lane / G::CHUNKS;        // this lane's first row of a tile; the others lie STEP apart
     uint32_t *table = reinterpret_cast<uint32_t *>(smem + G::OFF_TABLE);
@@ -468,22 +480,46 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, WHERE
 #pragma unroll
             for (int i = 0; i < N; ++i) load_to_lds(v + ((uint64_t)unit[i] * 16 + chunk[i]), buf + G::TILE_BYTES + i * G::NW * 1024);
         };
-        for (int t = base; t < min(end, base + S - 1); ++t) ask(t);
+        for (int t = base; t < min(end, base + S - 2); ++t) ask(t);
+        // The two waves of a SIMD take turns with its matrix cores: while one multiplies - values of the tile before, scores of this one - the
+        // other turns its scores into weights, and a barrier changes them over.  The second group is half a tile behind the first.
         const int mine = min(end, own);                       // tiles that this wave has rows for
+        auto turn = [&]() { if (G::NW > 4) tile_barrier_lds(); };
         auto top = [&](int t) {
-            tile_barrier_behind<2 * N, S - 2>(min(end - 1 - t, S - 2));
-            if (t + S - 1 < end) ask(t + S - 1);
+            if (t >= end) {
+                turn();
+                return;
+            }
+            tile_barrier_behind<2 * N, S - 3>(min(end - 1 - t, S - 3));
+            if (t + S - 2 < end) ask(t + S - 2);
         };
+        auto before_products = [&](int t) { if (group == 0) top(t); else turn(); };
+        auto before_weights = [&](int t) { if (group == 0) turn(); else top(t + 1); };
+        auto at = [&](int t) { return smem + (t & (S - 1)) * G::STAGE_BYTES; };
         int t = base;
-        for (; t < mine; ++t) {
-            top(t);
-            const char *buf = smem + (t & (S - 1)) * G::STAGE_BYTES;
-            rows.score(buf);
-            const auto ready = rows.values(buf, 0);
+        if (group) top(t);
+        before_products(t);
+        if (t < mine) {
+            rows.template multiply<false, true>(nullptr, at(t), rows.first_keys(at(t)));
+            before_weights(t);
             rows.weigh(seen, t);
-            rows.add(buf, ready);
+            for (++t; t < mine; ++t) {
+                const auto ready = rows.first_values(at(t - 1));
+                before_products(t);
+                rows.template multiply<true, true>(at(t - 1), at(t), ready);
+                before_weights(t);
+                rows.weigh(seen, t);
+            }
+            const auto ready = rows.first_values(at(t - 1));
+            before_products(t);
+            rows.template multiply<true, false>(at(t - 1), nullptr, ready);
         }
-        for (; t < end; ++t) top(t);
+        for (;;) {
+            if (t >= end) break;
+            before_weights(t);
+            before_products(++t);
+        }
+        if (group == 0) turn();
         tile_barrier<0>();
     }
 }
