@@ -3,7 +3,7 @@
 //
 // A workgroup of four or eight waves takes up to 32 * WQ query rows of one kv head - rows of all its query heads, which share keys and
 // values - over tiles of 64 positions.  Tiles go from memory straight to LDS (16-byte chunks in a swizzled order), into a ring of
-// buffers, two tiles (d = 64: six) ahead of their turn.
+// buffers, three tiles (d = 64: seven) ahead of their turn.
 //   S^T = K Q^T    : mfma 32x32x16, A = K fragment (ds_read_b128), B = Q fragment (registers)
 //   softmax        : one pass, a running reference per query row that follows its maximum up
 //   O^T += V^T P^T : A = V^T fragment (ds_read_b64_tr_b16), B = P
@@ -65,8 +65,8 @@ template <bool F16> __device__ __forceinline__ uint32_t pack2(float x, float y)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, typename Half<F16>::x2));
 }
 
-// A workgroup of NW waves, WQ of them side by side over query rows.
-template <int DIM, int NW_, int WQ_> struct Geo {
+// A workgroup of NW waves, WQ of them side by side over query rows, with a ring of RING KB of tiles.
+template <int DIM, int NW_, int WQ_, int RING> struct Geo {
     static constexpr int D = DIM, NW = NW_, WQ = WQ_;
     static constexpr int THREADS = NW * 64;
     static constexpr int WK = NW / WQ;                        // waves that share query rows
@@ -80,16 +80,17 @@ template <int DIM, int NW_, int WQ_> struct Geo {
     static constexpr int LOADS = TILE / RPI / NW;             // times it does so, of keys and of values
     static constexpr int TILE_BYTES = TILE * ROW_BYTES;
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;        // keys, values
-    static constexpr int STAGES = 131072 / STAGE_BYTES;       // 128 KB of tiles under way or in use: one workgroup to a CU
-    static constexpr int BATCH = 64;                          // tiles whose rows are looked up at a time
+    static constexpr int STAGES = RING * 1024 / STAGE_BYTES;  // tiles under way or in use
+    static constexpr int BATCH = RING / 2;                    // tiles whose rows are looked up at a time
+    static constexpr int PER_CU = RING > 64 ? 1 : 2;          // workgroups that share a CU and its LDS
     static constexpr int OFF_TABLE = STAGES * STAGE_BYTES;    // uint32[BATCH * TILE] where the rows lie, in units of 16 bytes
     static constexpr int OFF_ML = OFF_TABLE + BATCH * TILE * 4;       // float[2][NW][32]: references and sums of the waves' rows
     static constexpr int LDS_BYTES = OFF_ML + 2 * NW * 32 * 4;
     static_assert(NW * 32 * D * 4 <= STAGES * STAGE_BYTES, "the waves' results are laid out over the tile buffers");
     static_assert(WK == 1 || WK == 2, "a tile has two pieces of 32 positions");
     static_assert((STAGES & (STAGES - 1)) == 0, "tiles take the buffers in turn");
-    // 16-byte chunk c of row r lies in place c ^ swz(r): both the key reads (a chunk of 16 rows at a time) and the transposing value reads (64 bytes
-    // of 4 rows at a time) then spread over all banks.
+    // 16-byte chunk c of row r lies in place c ^ swz(r): both the key reads (a chunk of 32 rows) and the transposing value reads (4 rows x
+    // 32 bytes to 16 lanes) then spread over all banks.
     static __device__ __forceinline__ int swz(int row)
     {
         return (D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2) | ((row >> 2) & 3);
@@ -204,45 +205,34 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
             s[u] = Half<F16>::mfma(x.f[i], q[c], s[u]);
         }
     }
-    // Weighted values of the tile at `before`, then scores of the one at `now`; the first two steps' fragments are in x.
-    struct Ready { Four x[2]; };
-    template <bool ADD, bool SCORE> __device__ __forceinline__ Four fragments(const char *before, const char *now, int step) const
+    // Scores of the tile at buf (LDS).
+    __device__ __forceinline__ void score(const char *buf)
     {
-        return step < (ADD ? ADD_STEPS : 0) ? values(before, step) : keys(now, step - (ADD ? ADD_STEPS : 0));
-    }
-    template <bool ADD, bool SCORE> __device__ __forceinline__ void multiply(const char *before, const char *now, Ready ready)
-    {
-        if (SCORE) {
 #pragma unroll
-            for (int u = 0; u < G::SUBS; ++u) s[u] = f32x16{};
-        }
-        constexpr int A = ADD ? ADD_STEPS : 0, ALL = A + (SCORE ? SCORE_STEPS : 0);
-        Four x[3] = {ready.x[0], ready.x[1], ready.x[1]};
-        if (ADD && SCORE && A < 2) x[1] = keys(now, 0);
-        if (!ADD && ALL > 1) x[1] = keys(now, 1);
+        for (int u = 0; u < G::SUBS; ++u) s[u] = f32x16{};
+        Four ready = keys(buf, 0);
 #pragma unroll
-        for (int step = 0; step < ALL; ++step) {
-            if (step + 2 < ALL) x[(step + 2) % 3] = fragments<ADD, SCORE>(before, now, step + 2);
+        for (int step = 0; step < SCORE_STEPS; ++step) {
+            Four next = ready;
+            if (step + 1 < SCORE_STEPS) next = keys(buf, step + 1);
             __builtin_amdgcn_sched_barrier(0);
-            if (step < A) add_step(x[step % 3], step);
-            else score_step(x[step % 3], step - A);
+            score_step(ready, step);
             __builtin_amdgcn_sched_barrier(0);
+            ready = next;
         }
     }
-    // The fragments of its first steps that lie in the tile before.
-    __device__ __forceinline__ Ready first_values(const char *before) const
+    // Weighted values of the tile at buf; its first fragments are in `ready`.
+    __device__ __forceinline__ void add(const char *buf, Four ready)
     {
-        Ready r;
-        r.x[0] = values(before, 0);
-        r.x[1] = ADD_STEPS > 1 ? values(before, 1) : r.x[0];
-        return r;
-    }
-    __device__ __forceinline__ Ready first_keys(const char *now) const
-    {
-        Ready r;
-        r.x[0] = keys(now, 0);
-        r.x[1] = r.x[0];
-        return r;
+#pragma unroll
+        for (int step = 0; step < ADD_STEPS; ++step) {
+            Four next = ready;
+            if (step + 1 < ADD_STEPS) next = values(buf, step + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            add_step(ready, step);
+            __builtin_amdgcn_sched_barrier(0);
+            ready = next;
+        }
     }
 
     // Scores of tile t into weights.
@@ -344,6 +334,17 @@ template <typename G> __device__ __forceinline__ Joined joined(const char *smem,
     const float *ml = reinterpret_cast<const float *>(smem + G::OFF_ML);
     const int wq = row >> 5, in = row & 31;
     Joined j;
+    if constexpr (G::WK == 1) {
+        j.ref = ml[wq * 32 + in];
+        j.sum = ml[G::NW * 32 + wq * 32 + in];
+        const f32x4 a = left_row<D>(smem + wq * 32 * D * 4, in, 2 * at), b = left_row<D>(smem + wq * 32 * D * 4, in, 2 * at + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            j.o[i] = a[i];
+            j.o[4 + i] = b[i];
+        }
+        return j;
+    }
     j.ref = -INFINITY;
 #pragma unroll
     for (int k = 0; k < G::WK; ++k) j.ref = fmaxf(j.ref, ml[(k * WQ + wq) * 32 + in]);
@@ -365,6 +366,28 @@ template <typename G> __device__ __forceinline__ Joined joined(const char *smem,
         }
     }
     return j;
+}
+
+// Calls emit(row, Joined, eight) for all query rows of the workgroup, a lane for every eight elements.  Rows that no waves share are taken by the wave
+// that left them; for the others all waves have to be here first.
+template <typename G, typename EMIT> __device__ __forceinline__ void emit_rows(const char *smem, EMIT &&emit)
+{
+    constexpr int LANES = G::D / 8;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if constexpr (G::WK == 1) {
+#pragma unroll 4
+        for (int k = 0; k < 32 * LANES / 64; ++k) {
+            const int row = wave * 32 + k * (64 / LANES) + lane / LANES;
+            emit(row, joined<G>(smem, row, lane % LANES), lane % LANES);
+        }
+    } else {
+        __syncthreads();
+#pragma unroll 2
+        for (int k = 0; k < G::QROWS * LANES / G::THREADS; ++k) {
+            const int row = k * (G::THREADS / LANES) + tid / LANES;
+            emit(row, joined<G>(smem, row, tid % LANES), tid % LANES);
+        }
+    }
 }
 
 // log-sum-exp of a row.
@@ -427,20 +450,12 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, WHERE
 {
     constexpr int N = G::LOADS, S = G::STAGES, STEP = G::NW * G::RPI;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int group = wave >> 2;
     const uint32_t to = lds_address(smem) + wave * 1024;
     const int row0 = wave * G::RPI + lane / G::CHUNKS;        // this lane's first row of a tile; the others lie STEP apart
     uint32_t *table = reinterpret_cast<uint32_t *>(smem + G::OFF_TABLE);
     int chunk[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) chunk[i] = ((lane & (G::CHUNKS - 1)) ^ G::swz(row0 + i * STEP)) * 16;
-    // (what was asked for so far is waited for here: left to the place where it is used first, the wait would stand inside the loop)
-#pragma unroll
-    for (int c = 0; c < G::D / 16; ++c) {
-        u32x4 x = __builtin_bit_cast(u32x4, rows.q[c]);
-        asm volatile("" : "+v"(x));
-        rows.q[c] = __builtin_bit_cast(typename Half<F16>::x8, x);
-    }
     for (int base = first; base < last; base += G::BATCH) {
         const int end = min(last, base + G::BATCH);
         const CacheRows src = where();
@@ -480,46 +495,29 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, WHERE
 #pragma unroll
             for (int i = 0; i < N; ++i) load_to_lds(v + ((uint64_t)unit[i] * 16 + chunk[i]), buf + G::TILE_BYTES + i * G::NW * 1024);
         };
-        for (int t = base; t < min(end, base + S - 2); ++t) ask(t);
-        // The two waves of a SIMD take turns with its matrix cores: while one multiplies - values of the tile before, scores of this one - the
-        // other turns its scores into weights, and a barrier changes them over.  The second group is half a tile behind the first.
+        for (int t = base; t < min(end, base + S - 1); ++t) ask(t);
+        // (the queries are waited for here: left to the place where they are used first, the wait would stand inside the loop)
+#pragma unroll
+        for (int c = 0; c < G::D / 16; ++c) {
+            u32x4 x = __builtin_bit_cast(u32x4, rows.q[c]);
+            asm volatile("" : "+v"(x));
+            rows.q[c] = __builtin_bit_cast(typename Half<F16>::x8, x);
+        }
         const int mine = min(end, own);                       // tiles that this wave has rows for
-        auto turn = [&]() { if (G::NW > 4) tile_barrier_lds(); };
         auto top = [&](int t) {
-            if (t >= end) {
-                turn();
-                return;
-            }
-            tile_barrier_behind<2 * N, S - 3>(min(end - 1 - t, S - 3));
-            if (t + S - 2 < end) ask(t + S - 2);
+            tile_barrier_behind<2 * N, S - 2>(min(end - 1 - t, S - 2));
+            if (t + S - 1 < end) ask(t + S - 1);
         };
-        auto before_products = [&](int t) { if (group == 0) top(t); else turn(); };
-        auto before_weights = [&](int t) { if (group == 0) turn(); else top(t + 1); };
-        auto at = [&](int t) { return smem + (t & (S - 1)) * G::STAGE_BYTES; };
         int t = base;
-        if (group) top(t);
-        before_products(t);
-        if (t < mine) {
-            rows.template multiply<false, true>(nullptr, at(t), rows.first_keys(at(t)));
-            before_weights(t);
+        for (; t < mine; ++t) {
+            top(t);
+            const char *buf = smem + (t & (S - 1)) * G::STAGE_BYTES;
+            rows.score(buf);
+            const auto ready = rows.values(buf, 0);
             rows.weigh(seen, t);
-            for (++t; t < mine; ++t) {
-                const auto ready = rows.first_values(at(t - 1));
-                before_products(t);
-                rows.template multiply<true, true>(at(t - 1), at(t), ready);
-                before_weights(t);
-                rows.weigh(seen, t);
-            }
-            const auto ready = rows.first_values(at(t - 1));
-            before_products(t);
-            rows.template multiply<true, false>(at(t - 1), nullptr, ready);
+            rows.add(buf, ready);
         }
-        for (;;) {
-            if (t >= end) break;
-            before_weights(t);
-            before_products(++t);
-        }
-        if (group == 0) turn();
+        for (; t < end; ++t) top(t);
         tile_barrier<0>();
     }
 }
@@ -578,6 +576,18 @@ __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const Cac
             ml[row] = ref + __builtin_amdgcn_logf(sum);
             ml[G::NW * 32 + row] = 1.0f;
         }
+    }
+}
+
+// Eight elements of a partial result.
+template <int D> __device__ __forceinline__ void leave_slot(float *rows, float *ml, int64_t slot, int qrows, int c, int e, const Joined &j)
+{
+    float *x = rows + (slot * qrows + c) * D + 8 * e;
+    *reinterpret_cast<f32x4 *>(x) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
+    *reinterpret_cast<f32x4 *>(x + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
+    if (e == 0) {
+        ml[slot * 2 * qrows + c] = j.ref;
+        ml[slot * 2 * qrows + qrows + c] = j.sum;
     }
 }
 

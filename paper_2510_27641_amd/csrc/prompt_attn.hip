@@ -50,31 +50,80 @@ __device__ __forceinline__ Sequence sequence(const PromptArgs &a, int b)
     return s;
 }
 
-// Unit `index` of a kv head: its sequence, and its number within it (the last one first); false behind the last unit.
-template <int QROWS, int THREADS> __device__ __forceinline__ bool find_unit(const PromptArgs &a, int index, int &b, int &tile, int *wave_sums)
+// The largest of a wave's values, none of them negative (steps as in wave_inclusive_sum).
+__device__ __forceinline__ int wave_largest(int v)
+{
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// Unit `index` of a kv head: its sequence, and its number within it; false behind the last unit.  Of up to 64 sequences, units that see the most come
+// first, whatever sequence they belong to, so that what is left at the end is short: unit (b, i) is of rank i + (what its sequence has in
+// the cache ahead of its queries, in units), ranks are taken from the highest down and within a rank sequences in order.  More sequences follow
+// each other, the last unit of each first.
+template <int QROWS, int THREADS> __device__ __forceinline__ bool find_unit(const PromptArgs &a, int index, int &b, int &tile, Sequence &s, int *lds)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    __shared__ int found[2];
-    int before = 0;
+    constexpr int W = THREADS / 64;
+    int *found = lds + W;                                     // [6]
+    if (a.B == 1) {
+        s = sequence(a, 0);
+        const int n = (int)(((int64_t)s.q_len * a.G + QROWS - 1) / QROWS);
+        b = 0;
+        tile = n - 1 - index;
+        return tile >= 0;
+    }
+    if (a.B <= 64) {                                          // every wave for itself, a lane to a sequence
+        Sequence mine{};
+        int n = 0, r = 0;
+        if (lane < a.B) {
+            mine = sequence(a, lane);
+            n = (int)(((int64_t)mine.q_len * a.G + QROWS - 1) / QROWS);
+            r = (int)min((int64_t)max(mine.kv_len - mine.q_len, 0) * a.G / QROWS, (int64_t)1 << 28);
+        }
+        auto units_from = [&](int rank) { return __builtin_amdgcn_readlane(wave_inclusive_sum(min(max(n + r - rank, 0), n)), 63); };
+        if (index >= units_from(0)) return false;
+        int lo = 0;
+        for (int hi = wave_largest(n ? r + n : 0); hi - lo > 1;) {
+            const int mid = lo + (hi - lo) / 2;
+            if (units_from(mid) > index) lo = mid; else hi = mid;
+        }
+        const int nth = index - units_from(lo + 1);
+        const uint64_t there = __ballot(r <= lo && lo < r + n);
+        const uint64_t it = __ballot(((there >> lane) & 1) && __popcll(there & ((1ull << lane) - 1)) == nth);
+        b = __builtin_ctzll(it);
+        tile = lo - __builtin_amdgcn_readlane(r, b);
+        s.q0 = __builtin_amdgcn_readlane(mine.q0, b); s.q_len = __builtin_amdgcn_readlane(mine.q_len, b);
+        s.kv0 = __builtin_amdgcn_readlane(mine.kv0, b); s.kv_len = __builtin_amdgcn_readlane(mine.kv_len, b);
+        return true;
+    }
     if (tid == 0) found[0] = -1;
+    int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += THREADS) {
+        Sequence mine{};
         int n = 0;
         if (b0 + tid < a.B) {
-            const int q0 = min(max(a.q_starts[b0 + tid], 0), a.total_q);
-            n = (int)(((int64_t)max(min(a.q_starts[b0 + tid + 1], a.total_q) - q0, 0) * a.G + QROWS - 1) / QROWS);
+            mine = sequence(a, b0 + tid);
+            n = (int)(((int64_t)mine.q_len * a.G + QROWS - 1) / QROWS);
         }
         const int up = wave_inclusive_sum(n);
         __syncthreads();
-        if (lane == 63) wave_sums[wave] = up;
+        if (lane == 63) lds[wave] = up;
         __syncthreads();
         int all = 0, ahead = before + up - n;
-        for (int w = 0; w < THREADS / 64; ++w) {
-            if (w < wave) ahead += wave_sums[w];
-            all += wave_sums[w];
+        for (int w = 0; w < W; ++w) {
+            if (w < wave) ahead += lds[w];
+            all += lds[w];
         }
         if (index >= ahead && index < ahead + n) {
             found[0] = b0 + tid;
             found[1] = n - 1 - (index - ahead);
+            found[2] = mine.q0; found[3] = mine.q_len; found[4] = mine.kv0; found[5] = mine.kv_len;
         }
         before += all;
         if (index < before) break;
@@ -82,6 +131,8 @@ template <int QROWS, int THREADS> __device__ __forceinline__ bool find_unit(cons
     __syncthreads();
     b = __builtin_amdgcn_readfirstlane(found[0]);
     tile = __builtin_amdgcn_readfirstlane(found[1]);
+    s.q0 = __builtin_amdgcn_readfirstlane(found[2]); s.q_len = __builtin_amdgcn_readfirstlane(found[3]);
+    s.kv0 = __builtin_amdgcn_readfirstlane(found[4]); s.kv_len = __builtin_amdgcn_readfirstlane(found[5]);
     return b >= 0;
 }
 
@@ -112,14 +163,14 @@ template <int D, bool F16> __device__ __forceinline__ void finish_row(const Prom
 template <int D, bool F16, int NW, int WQ, int PARTS, bool PAGED>
 __global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a)
 {
-    typedef Geo<D, NW, WQ> G;
+    typedef Geo<D, NW, WQ, 128> G;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    __shared__ int wave_sums[NW];
+    __shared__ int lds[NW + 6];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int index = blockIdx.x / a.H_kv, h = blockIdx.x - index * a.H_kv;
     int b, tile;
-    if (!find_unit<G::QROWS, G::THREADS>(a, index, b, tile, wave_sums)) return;
-    const Sequence s = sequence(a, b);
+    Sequence s;
+    if (!find_unit<G::QROWS, G::THREADS>(a, index, b, tile, s, lds)) return;
     const int queries = s.q_len * a.G;                        // below 2^31: so are total_q * H_q
     const int ahead = s.kv_len - s.q_len;                     // token t sees positions up to t + ahead
     const int unit_q0 = tile * G::QROWS;
@@ -159,35 +210,23 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a)
             return low_bits(max(token(o, i) + ahead + 1, 0) - t * G::TILE - wk * G::SPAN);
         });
     }
-    __syncthreads();
-    constexpr int LANES = D / 8;
-    const int e = tid % LANES;
-    for (int c = tid / LANES; c < G::QROWS; c += G::THREADS / LANES) {
+    const int64_t slot = (int64_t)blockIdx.x * o.parts + part;
+    emit_rows<G>(smem, [&](int c, const Joined &j, int e) {
         const int qr = unit_q0 + c;
-        if (qr >= queries) break;
-        const Joined j = joined<G>(smem, c, e);
+        if (qr >= queries) return;
         if (o.parts == 1) finish_row<D, F16>(o, j, s.q0, h, qr, e);
-        else {
-            const int64_t slot = (int64_t)blockIdx.x * o.parts + part;
-            float *x = o.slots + (slot * G::QROWS + c) * D + 8 * e;
-            *reinterpret_cast<f32x4 *>(x) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
-            *reinterpret_cast<f32x4 *>(x + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
-            if (e == 0) {
-                o.slots_ml[slot * 2 * G::QROWS + c] = j.ref;
-                o.slots_ml[slot * 2 * G::QROWS + G::QROWS + c] = j.sum;
-            }
-        }
-    }
+        else leave_slot<D>(o.slots, o.slots_ml, slot, G::QROWS, c, e, j);
+    });
 }
 
 // The parts of a unit joined, in order; a wave for each query row.
 template <int D, bool F16, int QROWS> __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a)
 {
-    __shared__ int wave_sums[4];
+    __shared__ int lds[4 + 6];
     const int index = blockIdx.x / a.H_kv, h = blockIdx.x - index * a.H_kv;
     int b, tile;
-    if (!find_unit<QROWS, 256>(a, index, b, tile, wave_sums)) return;
-    const Sequence s = sequence(a, b);
+    Sequence s;
+    if (!find_unit<QROWS, 256>(a, index, b, tile, s, lds)) return;
     const int c = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int qr = tile * QROWS + c;
     if (c >= QROWS || qr >= s.q_len * a.G) return;
@@ -215,7 +254,7 @@ PromptKernel merge_variant(int d, bool f16, int qrows)
 }
 size_t lds_size(int d, int qrows)
 {
-    return d == 128 ? (qrows == 64 ? Geo<128, 4, 2>::LDS_BYTES : Geo<128, 8, 8>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2>::LDS_BYTES : Geo<64, 8, 8>::LDS_BYTES);
+    return d == 128 ? (qrows == 64 ? Geo<128, 4, 2, 128>::LDS_BYTES : Geo<128, 8, 8, 128>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2, 128>::LDS_BYTES : Geo<64, 8, 8, 128>::LDS_BYTES);
 }
 size_t a256(size_t x) { return (x + 255) & ~(size_t)255; }
 

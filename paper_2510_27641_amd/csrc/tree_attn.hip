@@ -109,7 +109,7 @@ struct Shares {
 template <int D, bool F16, int NW, int WQ, int PARTS>
 __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
 {
-    typedef Geo<D, NW, WQ> G;
+    typedef Geo<D, NW, WQ, 128> G;
     constexpr int THREADS = G::THREADS;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     int *prefix = reinterpret_cast<int *>(smem + G::LDS_BYTES);       // [rows + 1] tiles ahead of a row
@@ -204,27 +204,15 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
                 return t >= cached ? node_seen(o, old.nodes, i) >> (wk * G::SPAN) : low_bits(old.count - t * G::TILE - wk * G::SPAN);
             });
         }
-        __syncthreads();
         const bool whole = first == 0 && last == n;
         const int64_t slot = share + unit;
         if (first == 0 && tid == 0) o.parts[unit] = make_int2(share, shares.of(unit_at + n - 1));
-        constexpr int LANES = D / 8;                          // that a row takes, eight elements each
-        const int e = tid % LANES;
-        for (int c = tid / LANES; c < G::QROWS; c += THREADS / LANES) {
+        emit_rows<G>(smem, [&](int c, const Joined &j, int e) {
             const int qr = block * G::QROWS + c;
-            if (qr >= queries) break;
-            const Joined j = joined<G>(smem, c, e);
+            if (qr >= queries) return;
             if (whole) finish_row<D, F16>(o, j, b, h, qr, nodes, e);
-            else {
-                float *x = o.slots + (slot * G::QROWS + c) * D + 8 * e;
-                *reinterpret_cast<f32x4 *>(x) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
-                *reinterpret_cast<f32x4 *>(x + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
-                if (e == 0) {
-                    o.slots_ml[slot * 2 * G::QROWS + c] = j.ref;
-                    o.slots_ml[slot * 2 * G::QROWS + G::QROWS + c] = j.sum;
-                }
-            }
-        }
+            else leave_slot<D>(o.slots, o.slots_ml, slot, G::QROWS, c, e, j);
+        });
         __syncthreads();                                      // the tile buffers are free again
         at = unit_at + last;
     }
@@ -261,7 +249,7 @@ TreeKernel variant(int d, bool f16, int parts, int qrows)
 }
 size_t lds_size(int d, int qrows, int rows)
 {
-    const size_t tiles = d == 128 ? (qrows == 64 ? Geo<128, 4, 2>::LDS_BYTES : Geo<128, 8, 4>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2>::LDS_BYTES : Geo<64, 8, 4>::LDS_BYTES);
+    const size_t tiles = d == 128 ? (qrows == 64 ? Geo<128, 4, 2, 128>::LDS_BYTES : Geo<128, 8, 4, 128>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2, 128>::LDS_BYTES : Geo<64, 8, 4, 128>::LDS_BYTES);
     return tiles + (size_t)(rows + 1) * 4;
 }
 size_t a256(size_t x) { return (x + 255) & ~(size_t)255; }
