@@ -1,10 +1,10 @@
 // Causal attention over packed prompts of different lengths (Eq. 1; the prefill whose keys and values the selection later chooses from), alone or
 // behind a prefix that the cache holds.
 //
-// A unit is 128 query rows - tokens times query heads - of one kv head of a sequence: row i of a sequence stands for token i / G and head
-// i % G, so that the heads that share keys and values meet them together, and a unit's rows end within 128 / G positions of each other.
-// Units of a kv head follow each other in steps of H_kv workgroups, which keeps a head's keys and values on few XCDs, and the last tokens
-// of a sequence, which see the most, come first.  Where there are too few units for the GPU, each one's tiles are cut into parts, and
+// A unit is 256 query rows (128 or 64 in small calls) - tokens times query heads - of one kv head of a sequence: row i of a sequence stands for
+// token i / G and head i % G, so that the heads that share keys and values meet them together, and a unit's rows end within 256 / G positions
+// of each other.  Units of a kv head follow each other in steps of H_kv workgroups, which keeps a head's keys and values on few XCDs, and
+// units that see the most come first.  Where there are too few units for the GPU, each one's tiles are cut into parts, and
 // prompt_merge_kernel joins their partial results in order.
 #include "attn_rows.h"
 #include "checks.h"
@@ -161,9 +161,9 @@ template <int D, bool F16> __device__ __forceinline__ void finish_row(const Prom
 }
 
 template <int D, bool F16, int NW, int WQ, int PARTS, bool PAGED>
-__global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a)
+__global__ __launch_bounds__(NW * 64, WQ == 2 ? 1 : 2) void prompt_kernel(PromptArgs a)
 {
-    typedef Geo<D, NW, WQ, 128> G;
+    typedef Geo<D, NW, WQ, WQ == 4 ? 64 : 128> G;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     __shared__ int lds[NW + 6];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -235,11 +235,11 @@ template <int D, bool F16, int QROWS> __global__ __launch_bounds__(256) void pro
 }
 
 typedef void (*PromptKernel)(PromptArgs);
-// Workgroups by query rows: 64 of them to four waves, 256 to eight.
+// Workgroups by query rows: 64 of them to four waves, two of which share them; 128 to four waves, two workgroups to a CU; 256 to eight.
 template <int D, bool F16, int PARTS> PromptKernel by_rows(int qrows, bool paged)
 {
-    if (paged) return qrows == 64 ? prompt_kernel<D, F16, 4, 2, PARTS, true> : prompt_kernel<D, F16, 8, 8, PARTS, true>;
-    return qrows == 64 ? prompt_kernel<D, F16, 4, 2, PARTS, false> : prompt_kernel<D, F16, 8, 8, PARTS, false>;
+    if (paged) return qrows == 64 ? prompt_kernel<D, F16, 4, 2, PARTS, true> : qrows == 128 ? prompt_kernel<D, F16, 4, 4, PARTS, true> : prompt_kernel<D, F16, 8, 8, PARTS, true>;
+    return qrows == 64 ? prompt_kernel<D, F16, 4, 2, PARTS, false> : qrows == 128 ? prompt_kernel<D, F16, 4, 4, PARTS, false> : prompt_kernel<D, F16, 8, 8, PARTS, false>;
 }
 template <int D, bool F16> PromptKernel by_parts(int parts, int qrows, bool paged) { return parts == 1 ? by_rows<D, F16, 1>(qrows, paged) : by_rows<D, F16, 2>(qrows, paged); }
 PromptKernel variant(int d, bool f16, int parts, int qrows, bool paged)
@@ -247,15 +247,13 @@ PromptKernel variant(int d, bool f16, int parts, int qrows, bool paged)
     return d == 128 ? (f16 ? by_parts<128, true>(parts, qrows, paged) : by_parts<128, false>(parts, qrows, paged))
                     : (f16 ? by_parts<64, true>(parts, qrows, paged) : by_parts<64, false>(parts, qrows, paged));
 }
-template <int D, bool F16> PromptKernel merge_by_rows(int qrows) { return qrows == 64 ? prompt_merge_kernel<D, F16, 64> : prompt_merge_kernel<D, F16, 256>; }
+template <int D, bool F16> PromptKernel merge_by_rows(int qrows) { return qrows == 64 ? prompt_merge_kernel<D, F16, 64> : qrows == 128 ? prompt_merge_kernel<D, F16, 128> : prompt_merge_kernel<D, F16, 256>; }
 PromptKernel merge_variant(int d, bool f16, int qrows)
 {
     return d == 128 ? (f16 ? merge_by_rows<128, true>(qrows) : merge_by_rows<128, false>(qrows)) : (f16 ? merge_by_rows<64, true>(qrows) : merge_by_rows<64, false>(qrows));
 }
-size_t lds_size(int d, int qrows)
-{
-    return d == 128 ? (qrows == 64 ? Geo<128, 4, 2, 128>::LDS_BYTES : Geo<128, 8, 8, 128>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2, 128>::LDS_BYTES : Geo<64, 8, 8, 128>::LDS_BYTES);
-}
+template <int D> size_t lds_of(int qrows) { return qrows == 64 ? Geo<D, 4, 2, 128>::LDS_BYTES : qrows == 128 ? Geo<D, 4, 4, 64>::LDS_BYTES : Geo<D, 8, 8, 128>::LDS_BYTES; }
+size_t lds_size(int d, int qrows) { return d == 128 ? lds_of<128>(qrows) : lds_of<64>(qrows); }
 size_t a256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // How a call is cut: query rows of a unit, workgroups per kv head at most (no length is known on the host), parts of a unit.
@@ -264,11 +262,13 @@ Cut cut(const specattn_prompt_args *p)
 {
     Cut c;
     const int64_t queries = (int64_t)p->total_q * (p->H_q / p->H_kv);
-    c.qrows = queries <= (int64_t)64 * p->B ? 64 : 256;
-    c.units = (int)(queries / c.qrows + p->B);
-    const int64_t all = (int64_t)c.units * p->H_kv, wanted = cu_count();
-    // positions that a sequence has at most, in tiles
+    // Few positions to a sequence: two workgroups of 128 rows to a CU, so that one computes while the other sets up or writes out; many: 256 rows that
+    // share what is fetched.  us with 128 / 256 rows, 32 heads over 8: 512 tokens 17.7 / 21.5, 1024 29 / 36, 2048 60 / 65, 4096 154 / 148, 8192 568 / 565,
+    // 32768 8550 / 8150; 24 sequences of 32 to 2048 189 / 202; 4 x 512 behind 4096 to 16384 (64 heads) 861 / 823.  (In pages the table says how many there can be.)
     const int64_t reach = p->page_table ? (int64_t)p->max_pages_per_seq * p->page_size : p->total_kv;
+    c.qrows = queries <= (int64_t)64 * p->B ? 64 : (p->page_table ? reach : reach / p->B) < 3000 ? 128 : 256;
+    c.units = (int)(queries / c.qrows + p->B);
+    const int64_t all = (int64_t)c.units * p->H_kv, wanted = cu_count() * (c.qrows == 128 ? 2 : 1);
     c.parts = (int)std::min<int64_t>(std::max<int64_t>(wanted / all, 1), std::max<int64_t>(reach / 512, 1));
     return c;
 }
@@ -296,10 +296,10 @@ specattn_status prompt_configure()
     }
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return SPECATTN_OK;
-    for (int k = 0; k < 32; ++k) {
-        const int d = k & 1 ? 128 : 64, qrows = k & 8 ? 256 : 64;
+    for (int k = 0; k < 48; ++k) {
+        const int d = k & 1 ? 128 : 64, qrows = 64 << (k >> 4);
         const size_t bytes = lds_size(d, qrows);
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, qrows, k & 16)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, qrows, k & 8)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
             (void)hipGetLastError();
             set_error("cannot reserve %zu bytes of LDS", bytes);
             return SPECATTN_EHIP;
@@ -335,7 +335,7 @@ specattn_status launch_prompt(const specattn_prompt_args *p, hipStream_t stream)
     a.slots = static_cast<float *>(p->workspace);
     a.slots_ml = reinterpret_cast<float *>(static_cast<char *>(p->workspace) + a256(rows * p->d * sizeof(float)));
     const bool f16 = p->dtype == SPECATTN_F16;
-    variant(p->d, f16, p->out ? 2 : 1, c.qrows, p->page_table)<<<dim3(c.units * p->H_kv, c.parts), c.qrows == 64 ? 256 : 512, lds_size(p->d, c.qrows), stream>>>(a);
+    variant(p->d, f16, p->out ? 2 : 1, c.qrows, p->page_table)<<<dim3(c.units * p->H_kv, c.parts), c.qrows == 256 ? 512 : 256, lds_size(p->d, c.qrows), stream>>>(a);
     st = check_launch("prompt_kernel");
     if (st != SPECATTN_OK || c.parts == 1) return st;
     merge_variant(p->d, f16, c.qrows)<<<dim3(c.units * p->H_kv, c.qrows / 4), 256, 0, stream>>>(a);
