@@ -591,54 +591,115 @@ template <int D> __device__ __forceinline__ void leave_slot(float *rows, float *
     }
 }
 
-// Query row `c` of partial results in slots slot .. slot + n - 1 ([slot][qrows][D] unnormalised, references and sums [slot][2][qrows]), joined by one
-// wave: D / 8 lanes take a slot's row, eight elements each, and 512 / D slots at a time go side by side; the order of all sums is
-// fixed.  Every lane gets the total and the elements of its place.
-template <int D> __device__ __forceinline__ Joined joined_slots(const float *rows, const float *ml, int64_t slot, int n, int qrows, int c)
-{
-    constexpr int LANES = D / 8, SIDE = 64 / LANES;
-    const int lane = threadIdx.x & 63, e = lane % LANES, side = lane / LANES;
-    Joined j;
-    j.ref = -INFINITY;
-    for (int i = lane; i < n; i += 64) j.ref = fmaxf(j.ref, ml[(slot + i) * 2 * qrows + c]);
+constexpr int MERGE_ROWS = 4;                                 // query rows that a wave joins where they come from few slots
+
+// Query rows of partial results in slots slot .. slot + n - 1 ([slot][qrows][D] unnormalised, references and sums [slot][2][qrows]), joined by one
+// wave: D / 8 lanes take a slot's row, eight elements each, and 512 / D slots go side by side; the order of all sums is fixed.  Every lane gets the
+// total and the elements of its place.
+template <int D> struct Slots {
+    static constexpr int LANES = D / 8, SIDE = 64 / LANES;
+    const float *rows, *ml;
+    int64_t slot;
+    int n, qrows;
+
+    __device__ __forceinline__ void together(Joined &j) const // over the slots that lie side by side
+    {
 #pragma unroll
-    for (int step = 32; step; step >>= 1) j.ref = fmaxf(j.ref, __shfl_xor(j.ref, step));
-    j.sum = 0.0f;
+        for (int step = LANES; step < 64; step *= 2) {
+            j.sum += __shfl_xor(j.sum, step);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
-    constexpr int U = 4;                                      // slots that a lane asks for together
-    for (int i0 = side; i0 < n; i0 += U * SIDE) {
-        f32x4 x[U], y[U];
-        float m[U], l[U];
+            for (int i = 0; i < 8; ++i) j.o[i] += __shfl_xor(j.o[i], step);
+        }
+    }
+    // Up to SIDE slots: N rows' loads under way together.
+    template <int N> __device__ __forceinline__ void few(const int (&c)[N], Joined (&j)[N]) const
+    {
+        const int lane = threadIdx.x & 63, e = lane % LANES, side = lane / LANES;
+        const int64_t at = slot + min(side, n - 1);
+        f32x4 x[N], y[N];
+        float m[N], l[N];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = slot + min(i0 + u * SIDE, n - 1);
-            const float *p = rows + (at * qrows + c) * D + 8 * e;
-            m[u] = ml[at * 2 * qrows + c];
-            l[u] = ml[at * 2 * qrows + qrows + c];
-            x[u] = *reinterpret_cast<const f32x4 *>(p);
-            y[u] = *reinterpret_cast<const f32x4 *>(p + 4);
+        for (int k = 0; k < N; ++k) {
+            m[k] = ml[at * 2 * qrows + c[k]];
+            l[k] = ml[at * 2 * qrows + qrows + c[k]];
+            x[k] = *reinterpret_cast<const f32x4 *>(rows + (at * qrows + c[k]) * D + 8 * e);
+            y[k] = *reinterpret_cast<const f32x4 *>(rows + (at * qrows + c[k]) * D + 8 * e + 4);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (i0 + u * SIDE >= n || m[u] == -INFINITY) continue;
-            const float f = __builtin_amdgcn_exp2f(m[u] - j.ref);
-            j.sum = fmaf(f, l[u], j.sum);
+        for (int k = 0; k < N; ++k) {
+            const float mine = side < n ? m[k] : -INFINITY;
+            j[k].ref = mine;
+#pragma unroll
+            for (int step = LANES; step < 64; step *= 2) j[k].ref = fmaxf(j[k].ref, __shfl_xor(j[k].ref, step));
+            const float f = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - j[k].ref);
+            const bool some = mine != -INFINITY;              // (nothing attended to: zeros)
+            j[k].sum = some ? f * l[k] : 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                j.o[i] = fmaf(f, x[u][i], j.o[i]);
-                j.o[4 + i] = fmaf(f, y[u][i], j.o[4 + i]);
+                j[k].o[i] = some ? f * x[k][i] : 0.0f;
+                j[k].o[4 + i] = some ? f * y[k][i] : 0.0f;
             }
+            together(j[k]);
         }
     }
+    __device__ __forceinline__ Joined many(int c) const
+    {
+        const int lane = threadIdx.x & 63, e = lane % LANES, side = lane / LANES;
+        Joined j;
+        j.ref = -INFINITY;
+        for (int i = lane; i < n; i += 64) j.ref = fmaxf(j.ref, ml[(slot + i) * 2 * qrows + c]);
 #pragma unroll
-    for (int step = LANES; step < 64; step *= 2) {
-        j.sum += __shfl_xor(j.sum, step);
+        for (int step = 32; step; step >>= 1) j.ref = fmaxf(j.ref, __shfl_xor(j.ref, step));
+        j.sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) j.o[i] += __shfl_xor(j.o[i], step);
+        for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
+        constexpr int U = 4;                                  // slots that a lane asks for together
+        for (int i0 = side; i0 < n; i0 += U * SIDE) {
+            f32x4 x[U], y[U];
+            float m[U], l[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t at = slot + min(i0 + u * SIDE, n - 1);
+                const float *p = rows + (at * qrows + c) * D + 8 * e;
+                m[u] = ml[at * 2 * qrows + c];
+                l[u] = ml[at * 2 * qrows + qrows + c];
+                x[u] = *reinterpret_cast<const f32x4 *>(p);
+                y[u] = *reinterpret_cast<const f32x4 *>(p + 4);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * SIDE >= n || m[u] == -INFINITY) continue;
+                const float f = __builtin_amdgcn_exp2f(m[u] - j.ref);
+                j.sum = fmaf(f, l[u], j.sum);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    j.o[i] = fmaf(f, x[u][i], j.o[i]);
+                    j.o[4 + i] = fmaf(f, y[u][i], j.o[4 + i]);
+                }
+            }
+        }
+        together(j);
+        return j;
     }
-    return j;
-}
-
+    // What wave `w` of as many as there are rows does: the row of its number, or, where so few slots are joined that loads are short, MERGE_ROWS of
+    // them (and the last waves none).  done(row, Joined) is called for each.
+    template <typename DONE> __device__ __forceinline__ void join(int w, int all, DONE &&done) const
+    {
+        if (n > SIDE) {
+            if (w < all) done(w, many(w));
+            return;
+        }
+        const int c0 = w * MERGE_ROWS;
+        if (c0 >= all) return;
+        int c[MERGE_ROWS];
+        Joined j[MERGE_ROWS];
+#pragma unroll
+        for (int k = 0; k < MERGE_ROWS; ++k) c[k] = min(c0 + k, all - 1);
+        few(c, j);
+#pragma unroll
+        for (int k = 0; k < MERGE_ROWS; ++k)
+            if (c0 + k < all) done(c0 + k, j[k]);
+    }
+};
 }  // namespace
 }  // namespace specattn

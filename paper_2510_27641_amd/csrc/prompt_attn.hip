@@ -219,7 +219,7 @@ __global__ __launch_bounds__(NW * 64, WQ == 2 ? 1 : 2) void prompt_kernel(Prompt
     });
 }
 
-// The parts of a unit joined, in order; a wave for each query row.
+// The parts of a unit joined, in order.
 template <int D, bool F16, int QROWS> __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a)
 {
     __shared__ int lds[4 + 6];
@@ -227,11 +227,11 @@ template <int D, bool F16, int QROWS> __global__ __launch_bounds__(256) void pro
     int b, tile;
     Sequence s;
     if (!find_unit<QROWS, 256>(a, index, b, tile, s, lds)) return;
-    const int c = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int qr = tile * QROWS + c;
-    if (c >= QROWS || qr >= s.q_len * a.G) return;
-    const Joined j = joined_slots<D>(a.slots, a.slots_ml, (int64_t)blockIdx.x * a.parts, a.parts, QROWS, c);
-    if (lane < D / 8) finish_row<D, F16>(a, j, s.q0, h, qr, lane);
+    const int lane = threadIdx.x & 63, queries = s.q_len * a.G;
+    const Slots<D> slots = {a.slots, a.slots_ml, (int64_t)blockIdx.x * a.parts, a.parts, QROWS};
+    slots.join(blockIdx.y * 4 + (threadIdx.x >> 6), min(QROWS, queries - tile * QROWS), [&](int c, const Joined &j) {
+        if (lane < D / 8) finish_row<D, F16>(a, j, s.q0, h, tile * QROWS + c, lane);
+    });
 }
 
 typedef void (*PromptKernel)(PromptArgs);

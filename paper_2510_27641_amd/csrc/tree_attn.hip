@@ -15,7 +15,10 @@ namespace specattn {
 namespace {
 
 constexpr int MAX_UNITS = 2048;                               // rows (b, h) per launch: their prefix of tiles lies in LDS
-constexpr int MIN_TILES = 2;                                  // of a share: a partial result costs about as much as a tile
+constexpr int MIN_TILES = 2;                                  // of a share
+constexpr int FEW = 64;                                       // rows that a wave scans by itself
+constexpr int WHOLE_TILES = 8;                                // units of up to so many are not cut: joining them takes a second launch
+constexpr int SETUP = 4;                                      // what a unit costs beside its tiles
 
 struct TreeArgs {
     const uint16_t *q;
@@ -34,6 +37,7 @@ struct TreeArgs {
     FastDivisor per_h, per_t;
     int H_q, H_kv, T, G, n_max, slots_per_row, pages, page_shift, max_pages, chunk_shift, capacity, physical;
     int row0, rows, blocks;                                   // this launch's rows (b, h), and units per row
+    int whole;                                                // 1: a workgroup to a unit
     float sm_scale;
 };
 
@@ -89,20 +93,54 @@ template <int D, bool F16> __device__ __forceinline__ void finish_row(const Tree
     if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(j.ref, j.sum);
 }
 
-// The line of tiles in n shares, the first `more` of them one tile longer than `each`.
-struct Shares {
-    int n, each, more;
-    __device__ __forceinline__ Shares(int total, int most)
+// The line of all units' tiles, cut into n shares.  Picking a unit up and putting its result down costs a share about as much as a few tiles: a
+// unit takes `setup` places ahead of its tiles, and a cut that would fall there, or close to a unit's ends, is made between the units
+// instead, so that no partial results are left for little.
+struct Line {
+    const int *prefix;                                        // [rows + 1] tiles of the units of the rows ahead of a row (LDS), or null:
+    int ahead;                                                // of up to FEW rows, those ahead of row `lane`
+    int rows, blocks, tiles, n, setup, each, more, slack;
+    __device__ __forceinline__ Line(const int *prefix_, int ahead_, int tiles_, int rows_, int blocks_, int most)
+        : prefix(prefix_), ahead(ahead_), rows(rows_), blocks(blocks_), tiles(tiles_)
     {
-        n = min(most, max(total / MIN_TILES, 1));
+        n = min(most, max(tiles / MIN_TILES, 1));
+        setup = min(SETUP, (int)((uint32_t)tiles / (uint32_t)n) / 4);
+        const int total = tiles + setup * rows * blocks;
         each = (int)((uint32_t)total / (uint32_t)n);
         more = total - each * n;
+        slack = each / 8;
     }
-    __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
-    __device__ __forceinline__ int of(int tile) const
+    __device__ __forceinline__ int row_at(int r) const
+    {
+        const int before = r == rows ? tiles : prefix ? __builtin_amdgcn_readfirstlane(prefix[r]) : __builtin_amdgcn_readlane(ahead, r);
+        return before + setup * r * blocks;
+    }
+    __device__ __forceinline__ int row_of(int place) const
+    {
+        const int lane = threadIdx.x & 63;
+        if (!prefix) return __popcll(__ballot(lane < rows && ahead + setup * lane * blocks <= place)) - 1;
+        int lo = 0;
+        for (int hi = rows; hi - lo > 1;) {
+            const int mid = (lo + hi) >> 1;
+            if (row_at(mid) <= place) lo = mid; else hi = mid;
+        }
+        return lo;
+    }
+    __device__ __forceinline__ int begin(int w) const         // where share w begins
+    {
+        const int place = w * each + min(w, more);
+        if (w == 0 || w == n) return place;
+        const int r = row_of(place), at = row_at(r), per = (int)((uint32_t)(row_at(r + 1) - at) / (uint32_t)blocks);
+        const int in = (int)((uint32_t)(place - at) % (uint32_t)per);
+        return in <= setup + slack ? place - in : per - in <= slack ? place + per - in : place;
+    }
+    __device__ __forceinline__ int of(int place) const        // the share that a place lies in
     {
         const int longer = more * (each + 1);
-        return tile < longer ? (int)((uint32_t)tile / (uint32_t)(each + 1)) : more + (int)((uint32_t)(tile - longer) / (uint32_t)max(each, 1));
+        int w = place < longer ? (int)((uint32_t)place / (uint32_t)(each + 1)) : more + (int)((uint32_t)(place - longer) / (uint32_t)max(each, 1));
+        while (w > 0 && place < begin(w)) --w;
+        while (w + 1 < n && place >= begin(w + 1)) ++w;
+        return w;
     }
 };
 
@@ -112,10 +150,21 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
     typedef Geo<D, NW, WQ, 128> G;
     constexpr int THREADS = G::THREADS;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    int *prefix = reinterpret_cast<int *>(smem + G::LDS_BYTES);       // [rows + 1] tiles ahead of a row
-    __shared__ int wave_sums[NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    {
+    int *prefix = reinterpret_cast<int *>(smem + G::LDS_BYTES);       // [rows + 1] tiles ahead of a row
+    int ahead = 0, tiles = 0;
+    if (!a.whole && a.rows <= FEW) {                          // every wave for itself, a lane to a row
+        int n = 0;
+        if (lane < a.rows) {
+            const int b = a.per_h.divide(a.row0 + lane);
+            n = tiles_of(count_of(a, a.row0 + lane, b), nodes_of(a, b)) * a.blocks;
+        }
+        const int up = wave_inclusive_sum(n);
+        ahead = up - n;
+        tiles = __builtin_amdgcn_readlane(up, 63);
+        prefix = nullptr;
+    } else if (!a.whole) {
+        __shared__ int wave_sums[NW];
         const int per = (a.rows + THREADS - 1) / THREADS;
         int mine = 0;
         for (int i = 0; i < per; ++i) {
@@ -139,32 +188,43 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         }
         if (tid == 0) prefix[0] = 0;
         __syncthreads();
+        tiles = __builtin_amdgcn_readfirstlane(prefix[a.rows]);
     }
-    auto tiles_before = [&](int row) { return __builtin_amdgcn_readfirstlane(prefix[row]); };
-    const Shares shares(tiles_before(a.rows), gridDim.x);
+    const Line line(prefix, ahead, tiles, a.rows, a.blocks, gridDim.x);
     const int share = blockIdx.x;
-    if (share >= shares.n) return;
-    int at = shares.begin(share);
-    const int end = shares.begin(share + 1);
-    int r = 0;                                                // the row that the share begins in
-    for (int lo = 0, hi = a.rows; hi - lo > 1;) {
-        const int mid = (lo + hi) >> 1;
-        if (tiles_before(mid) <= at) lo = mid; else hi = mid;
-        r = lo;
+    int at = 0, end = 1, r = 0;
+    if (!a.whole) {
+        if (share >= line.n) return;
+        at = line.begin(share);
+        end = line.begin(share + 1);
+        r = line.row_of(at);
     }
     const int wq = wave % WQ, wk = wave / WQ;
     const int queries = a.G * a.T;
     while (at < end) {
         const TreeArgs &a = arguments_again<TreeArgs>();
-        while (tiles_before(r + 1) <= at) ++r;
-        const int row_at = tiles_before(r), n = (int)((uint32_t)(tiles_before(r + 1) - row_at) / (uint32_t)a.blocks);   // tiles of each of the row's units
-        const int block = (int)((uint32_t)(at - row_at) / (uint32_t)n);
-        const int unit_at = row_at + block * n;
-        const int first = at - unit_at, last = min(n, end - unit_at);
+        int block, unit_at = 0, tiles_at = 0, n = 0, first = 0, last = 0;
+        if (a.whole) {
+            r = (int)((uint32_t)share / (uint32_t)a.blocks);
+            block = share - r * a.blocks;
+            at = 1;
+        } else {
+            while (line.row_at(r + 1) <= at) ++r;
+            const int row_at = line.row_at(r), per = (int)((uint32_t)(line.row_at(r + 1) - row_at) / (uint32_t)a.blocks);
+            n = per - line.setup;
+            block = (int)((uint32_t)(at - row_at) / (uint32_t)per);
+            unit_at = row_at + block * per;
+            tiles_at = unit_at + line.setup;
+            first = max(at - tiles_at, 0);
+            last = min(n, end - tiles_at);
+            at = unit_at + per;
+            if (last <= first) continue;
+        }
         const int unit = r * a.blocks + block;
         const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
         const int count = count_of(a, row, b), nodes = nodes_of(a, b);
         const int cached = (count + G::TILE - 1) / G::TILE;
+        if (a.whole) last = n = tiles_of(count, nodes);
 
         RowsOfWave<G, F16, PARTS> rows;
         rows.start(wk, a.sm_scale);
@@ -206,7 +266,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         }
         const bool whole = first == 0 && last == n;
         const int64_t slot = share + unit;
-        if (first == 0 && tid == 0) o.parts[unit] = make_int2(share, shares.of(unit_at + n - 1));
+        if (first == 0 && tid == 0 && !o.whole) o.parts[unit] = make_int2(share, line.of(tiles_at + n - 1));
         emit_rows<G>(smem, [&](int c, const Joined &j, int e) {
             const int qr = block * G::QROWS + c;
             if (qr >= queries) return;
@@ -214,11 +274,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
             else leave_slot<D>(o.slots, o.slots_ml, slot, G::QROWS, c, e, j);
         });
         __syncthreads();                                      // the tile buffers are free again
-        at = unit_at + last;
     }
 }
 
-// Units that several shares worked on: their partial results joined, in the order of the shares; a wave for each query row.
+// Units that several shares worked on: their partial results joined, in the order of the shares.
 template <int D, bool F16> __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int qrows)
 {
     const int unit = blockIdx.x;
@@ -226,20 +285,21 @@ template <int D, bool F16> __global__ __launch_bounds__(256) void tree_merge_ker
     if (parts.x == parts.y) return;
     const int r = unit / a.blocks, block = unit - r * a.blocks;
     const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
-    const int c = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int qr = block * qrows + c;
-    if (c >= qrows || qr >= a.G * a.T) return;
-    const Joined j = joined_slots<D>(a.slots, a.slots_ml, parts.x + unit, parts.y - parts.x + 1, qrows, c);
-    if (lane < D / 8) finish_row<D, F16>(a, j, b, h, qr, nodes_of(a, b), lane);
+    const int lane = threadIdx.x & 63, nodes = nodes_of(a, b), queries = a.G * a.T;
+    const Slots<D> slots = {a.slots, a.slots_ml, (int64_t)parts.x + unit, parts.y - parts.x + 1, qrows};
+    slots.join(blockIdx.y * 4 + (threadIdx.x >> 6), min(qrows, queries - block * qrows), [&](int c, const Joined &j) {
+        if (lane < D / 8) finish_row<D, F16>(a, j, b, h, block * qrows + c, nodes, lane);
+    });
 }
 
-// Workgroups by query rows: 64 of them to four waves, 128 to eight (two share rows), 256 to eight.
-int rows_per_unit(int queries) { return queries <= 64 ? 64 : queries <= 128 ? 128 : 256; }
+// Query rows of a unit: 64 for four waves, two of which share rows, or 256 for eight.  (us with 8 x 32 tokens over 7500 of 32768 positions, 128
+// rows to a kv head: two workgroups of four waves with 128 rows each 91, one of eight waves, half of which only fetch, 80.)
+int rows_per_unit(int queries) { return queries <= 64 ? 64 : 256; }
 
 typedef void (*TreeKernel)(TreeArgs);
 template <int D, bool F16, int PARTS> TreeKernel by_rows(int qrows)
 {
-    return qrows == 64 ? tree_kernel<D, F16, 4, 2, PARTS> : qrows == 128 ? tree_kernel<D, F16, 8, 4, PARTS> : tree_kernel<D, F16, 8, 8, PARTS>;
+    return qrows == 64 ? tree_kernel<D, F16, 4, 2, PARTS> : tree_kernel<D, F16, 8, 8, PARTS>;
 }
 template <int D, bool F16> TreeKernel by_parts(int parts, int qrows) { return parts == 1 ? by_rows<D, F16, 1>(qrows) : by_rows<D, F16, 2>(qrows); }
 TreeKernel variant(int d, bool f16, int parts, int qrows)
@@ -247,11 +307,8 @@ TreeKernel variant(int d, bool f16, int parts, int qrows)
     return d == 128 ? (f16 ? by_parts<128, true>(parts, qrows) : by_parts<128, false>(parts, qrows))
                     : (f16 ? by_parts<64, true>(parts, qrows) : by_parts<64, false>(parts, qrows));
 }
-size_t lds_size(int d, int qrows, int rows)
-{
-    const size_t tiles = d == 128 ? (qrows == 64 ? Geo<128, 4, 2, 128>::LDS_BYTES : Geo<128, 8, 4, 128>::LDS_BYTES) : (qrows == 64 ? Geo<64, 4, 2, 128>::LDS_BYTES : Geo<64, 8, 4, 128>::LDS_BYTES);
-    return tiles + (size_t)(rows + 1) * 4;
-}
+template <int D> size_t lds_of(int qrows) { return qrows == 64 ? Geo<D, 4, 2, 128>::LDS_BYTES : Geo<D, 8, 8, 128>::LDS_BYTES; }
+size_t lds_size(int d, int qrows, int rows) { return (d == 128 ? lds_of<128>(qrows) : lds_of<64>(qrows)) + (size_t)(rows + 1) * 4; }
 size_t a256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct Layout { size_t parts, rows, ml; };
@@ -283,8 +340,8 @@ specattn_status tree_configure()
     }
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return SPECATTN_OK;
-    for (int k = 0; k < 24; ++k) {
-        const int d = k & 1 ? 128 : 64, qrows = 64 << (k >> 3);
+    for (int k = 0; k < 16; ++k) {
+        const int d = k & 1 ? 128 : 64, qrows = k & 8 ? 256 : 64;
         const size_t bytes = lds_size(d, qrows, MAX_UNITS);
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, qrows)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
             (void)hipGetLastError();
@@ -333,9 +390,14 @@ specattn_status launch_tree(const specattn_tree_args *t, hipStream_t stream)
     const int64_t most = t->indices ? (int64_t)t->idx_capacity << a.chunk_shift : t->n_max;
     for (a.row0 = 0; a.row0 < rows; a.row0 += a.rows) {
         a.rows = (int)std::min<int64_t>({rows - a.row0, MAX_UNITS, (int64_t)(1 << 30) / (a.blocks * (most / 64 + 2))});     // tiles are counted in 31 bits
-        variant(t->d, f16, t->out ? 2 : 1, qrows)<<<cu_count(), qrows == 64 ? 256 : 512, lds_size(t->d, qrows, a.rows), stream>>>(a);
+        const int64_t tiles = (most + 63) / 64 + 1;           // of a unit, at most
+        a.whole = tiles <= WHOLE_TILES;
+        const int units = a.rows * a.blocks;
+        const int grid = a.whole ? units : (int)std::min<int64_t>(cu_count(), (units * tiles + MIN_TILES - 1) / MIN_TILES);
+        variant(t->d, f16, t->out ? 2 : 1, qrows)<<<grid, qrows == 256 ? 512 : 256, lds_size(t->d, qrows, a.rows), stream>>>(a);
         st = check_launch("tree_kernel");
         if (st != SPECATTN_OK) return st;
+        if (a.whole) continue;
         const auto merge = t->d == 128 ? (f16 ? tree_merge_kernel<128, true> : tree_merge_kernel<128, false>) : (f16 ? tree_merge_kernel<64, true> : tree_merge_kernel<64, false>);
         merge<<<dim3(a.rows * a.blocks, (std::min(queries, qrows) + 3) / 4), 256, 0, stream>>>(a, qrows);
         st = check_launch("tree_merge_kernel");
