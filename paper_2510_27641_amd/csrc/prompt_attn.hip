@@ -50,18 +50,6 @@ __device__ __forceinline__ Sequence sequence(const PromptArgs &a, int b)
     return s;
 }
 
-// The largest of a wave's values, none of them negative (steps as in wave_inclusive_sum).
-__device__ __forceinline__ int wave_largest(int v)
-{
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
-    return __builtin_amdgcn_readlane(v, 63);
-}
-
 // Unit `index` of a kv head: its sequence, and its number within it; false behind the last unit.  Of up to 64 sequences, units that see the most come
 // first, whatever sequence they belong to, so that what is left at the end is short: unit (b, i) is of rank i + (what its sequence has in
 // the cache ahead of its queries, in units), ranks are taken from the highest down and within a rank sequences in order.  More sequences follow

@@ -15,7 +15,7 @@ namespace specattn {
 namespace {
 
 constexpr int MAX_UNITS = 2048;                               // rows (b, h) per launch: their prefix of tiles lies in LDS
-constexpr int MIN_TILES = 2;                                  // of a share
+constexpr int MIN_TILES = 4;                                  // of a share
 constexpr int FEW = 64;                                       // rows that a wave scans by itself
 constexpr int WHOLE_TILES = 8;                                // units of up to so many are not cut: joining them takes a second launch
 constexpr int SETUP = 4;                                      // what a unit costs beside its tiles
@@ -95,16 +95,20 @@ template <int D, bool F16> __device__ __forceinline__ void finish_row(const Tree
 
 // The line of all units' tiles, cut into n shares.  Picking a unit up and putting its result down costs a share about as much as a few tiles: a
 // unit takes `setup` places ahead of its tiles, and a cut that would fall there, or close to a unit's ends, is made between the units
-// instead, so that no partial results are left for little.
+// instead, so that no partial results are left for little.  Where there are no more units than workgroups, and the largest is not much longer than a
+// share would be, every unit is a share.
 struct Line {
     const int *prefix;                                        // [rows + 1] tiles of the units of the rows ahead of a row (LDS), or null:
     int ahead;                                                // of up to FEW rows, those ahead of row `lane`
     int rows, blocks, tiles, n, setup, each, more, slack;
-    __device__ __forceinline__ Line(const int *prefix_, int ahead_, int tiles_, int rows_, int blocks_, int most)
+    bool direct;
+    __device__ __forceinline__ Line(const int *prefix_, int ahead_, int tiles_, int largest, int rows_, int blocks_, int most)
         : prefix(prefix_), ahead(ahead_), rows(rows_), blocks(blocks_), tiles(tiles_)
     {
         n = min(most, max(tiles / MIN_TILES, 1));
         setup = min(SETUP, (int)((uint32_t)tiles / (uint32_t)n) / 4);
+        direct = rows * blocks <= most && largest <= (int)((uint32_t)tiles / (uint32_t)n) + 2 * SETUP;
+        if (direct) n = rows * blocks;
         const int total = tiles + setup * rows * blocks;
         each = (int)((uint32_t)total / (uint32_t)n);
         more = total - each * n;
@@ -119,12 +123,12 @@ struct Line {
     {
         const int lane = threadIdx.x & 63;
         if (!prefix) return __popcll(__ballot(lane < rows && ahead + setup * lane * blocks <= place)) - 1;
-        int lo = 0;
-        for (int hi = rows; hi - lo > 1;) {
-            const int mid = (lo + hi) >> 1;
-            if (row_at(mid) <= place) lo = mid; else hi = mid;
-        }
-        return lo;
+        // every `step`th row first, then those in between
+        const int step = (rows + 63) >> 6;
+        const int coarse = min(lane * step, rows - 1);
+        const int from = (__popcll(__ballot(lane * step < rows && prefix[coarse] + setup * coarse * blocks <= place)) - 1) * step;
+        const int fine = min(from + lane, rows - 1);
+        return from + __popcll(__ballot(lane < step && from + lane < rows && prefix[fine] + setup * fine * blocks <= place)) - 1;
     }
     __device__ __forceinline__ int begin(int w) const         // where share w begins
     {
@@ -152,19 +156,21 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int *prefix = reinterpret_cast<int *>(smem + G::LDS_BYTES);       // [rows + 1] tiles ahead of a row
-    int ahead = 0, tiles = 0;
+    int ahead = 0, tiles = 0, largest = 0, counts = 0;        // (counts: of up to FEW rows, that of row `lane`)
     if (!a.whole && a.rows <= FEW) {                          // every wave for itself, a lane to a row
         int n = 0;
         if (lane < a.rows) {
             const int b = a.per_h.divide(a.row0 + lane);
-            n = tiles_of(count_of(a, a.row0 + lane, b), nodes_of(a, b)) * a.blocks;
+            counts = count_of(a, a.row0 + lane, b);
+            n = tiles_of(counts, nodes_of(a, b)) * a.blocks;
         }
         const int up = wave_inclusive_sum(n);
         ahead = up - n;
+        largest = wave_largest(n);
         tiles = __builtin_amdgcn_readlane(up, 63);
         prefix = nullptr;
     } else if (!a.whole) {
-        __shared__ int wave_sums[NW];
+        __shared__ int wave_sums[NW], wave_most[NW];
         const int per = (a.rows + THREADS - 1) / THREADS;
         int mine = 0;
         for (int i = 0; i < per; ++i) {
@@ -174,10 +180,16 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
             const int n = tiles_of(count_of(a, a.row0 + r, b), nodes_of(a, b)) * a.blocks;
             prefix[r + 1] = n;
             mine += n;
+            largest = max(largest, n);
         }
         const int up = wave_inclusive_sum(mine);
-        if (lane == 63) wave_sums[wave] = up;
+        largest = wave_largest(largest);
+        if (lane == 63) {
+            wave_sums[wave] = up;
+            wave_most[wave] = largest;
+        }
         __syncthreads();
+        for (int w = 0; w < NW; ++w) largest = max(largest, __builtin_amdgcn_readfirstlane(wave_most[w]));
         int before = up - mine;
         for (int w = 0; w < wave; ++w) before += wave_sums[w];
         for (int i = 0; i < per; ++i) {
@@ -190,11 +202,12 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         __syncthreads();
         tiles = __builtin_amdgcn_readfirstlane(prefix[a.rows]);
     }
-    const Line line(prefix, ahead, tiles, a.rows, a.blocks, gridDim.x);
+    const Line line(prefix, ahead, tiles, (int)((uint32_t)largest / (uint32_t)a.blocks), a.rows, a.blocks, gridDim.x);
+    const bool by_unit = a.whole || line.direct;
     const int share = blockIdx.x;
     int at = 0, end = 1, r = 0;
-    if (!a.whole) {
-        if (share >= line.n) return;
+    if (!a.whole && share >= line.n) return;
+    if (!by_unit) {
         at = line.begin(share);
         end = line.begin(share + 1);
         r = line.row_of(at);
@@ -204,7 +217,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
     while (at < end) {
         const TreeArgs &a = arguments_again<TreeArgs>();
         int block, unit_at = 0, tiles_at = 0, n = 0, first = 0, last = 0;
-        if (a.whole) {
+        if (by_unit) {
             r = (int)((uint32_t)share / (uint32_t)a.blocks);
             block = share - r * a.blocks;
             at = 1;
@@ -222,9 +235,9 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         }
         const int unit = r * a.blocks + block;
         const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
-        const int count = count_of(a, row, b), nodes = nodes_of(a, b);
+        const int count = !a.whole && a.rows <= FEW ? __builtin_amdgcn_readlane(counts, r) : count_of(a, row, b), nodes = nodes_of(a, b);
         const int cached = (count + G::TILE - 1) / G::TILE;
-        if (a.whole) last = n = tiles_of(count, nodes);
+        if (by_unit) last = n = tiles_of(count, nodes);
 
         RowsOfWave<G, F16, PARTS> rows;
         rows.start(wk, a.sm_scale);
@@ -266,7 +279,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         }
         const bool whole = first == 0 && last == n;
         const int64_t slot = share + unit;
-        if (first == 0 && tid == 0 && !o.whole) o.parts[unit] = make_int2(share, line.of(tiles_at + n - 1));
+        if (first == 0 && tid == 0 && !o.whole) o.parts[unit] = make_int2(share, by_unit ? share : line.of(tiles_at + n - 1));
         emit_rows<G>(smem, [&](int c, const Joined &j, int e) {
             const int qr = block * G::QROWS + c;
             if (qr >= queries) return;
