@@ -538,7 +538,7 @@ typedef struct specattn_pages_args {
     const int32_t *seq_lens, *new_lens;                      /* [B] */
     int32_t *lens_out;           /* out [B] */
     int32_t *token_starts;       /* out [B + 1], optional */
-    int32_t *slots;              /* out [token_capacity], optional (NULL: no limit on new tokens) */
+    int32_t *slots;              /* out [token_capacity], optional (NULL: 2^31 - 1 new tokens at most) */
     int32_t *positions, *owners; /* out [token_capacity], optional; with slots */
     int32_t token_capacity;
     uint32_t *row_flags;         /* out [B], optional */
@@ -578,13 +578,13 @@ specattn_status specattn_cache_store(const specattn_store_args *args, void *stre
  * infinities and NaN included; rows of out and lse that belong to no sequence are left as they were.
  * Accumulation and the softmax are fp32.  Where `out` is asked for the weights enter the second product in two parts of the element type
  * (16 significant bits with bf16, 22 with fp16), for out_lowp alone rounded to it.  Repeated calls give bit-identical results.
- * Starts ascend.  Lengths are cut to what there is (total_q, total_kv, the page table); a page number outside the pool reads the nearest page.
+ * Starts ascend.  The rows of a kv head lie within 64 GiB of its first one (packed: k and v as a whole; SPECATTN_ESHAPE).  Lengths are cut to what there is (total_q, total_kv, the page table); a page number outside the pool reads the nearest page.
  */
 typedef struct specattn_prompt_args {
     const void *q;               /* [total_q][H_q][d] */
     const void *k, *v;           /* packed [total_kv][H_kv][d], or pools [num_pages][H_kv][page_size][d] */
     specattn_dtype dtype;        /* SPECATTN_BF16 or SPECATTN_F16 */
-    int32_t B, H_q, H_kv, d;     /* H_q a multiple of H_kv; d: 64 or 128 */
+    int32_t B, H_q, H_kv, d;     /* H_q a multiple of H_kv; d: 64 or 128; B * H_kv <= 2^21 */
     int32_t total_q, total_kv;   /* rows of q, and of packed k and v; total_q * H_q <= 2^30 */
     float sm_scale;              /* <= 0 selects 1/sqrt(d) */
     int64_t q_stride_t, q_stride_h;                          /* elements; last dim contiguous; 16-byte multiples */
@@ -612,7 +612,8 @@ size_t specattn_prompt_workspace_size(const specattn_prompt_args *args);   /* 0 
  * seq_lens[b].  Nodes from node_counts[b] on are not there: their rows give out = 0 and lse = -inf, as does a row with nothing to attend to; their
  * bits, queries, keys and values have no effect.  Keys and values that a row's mask hides have none either, infinities and NaN included.
  * Weights and results as for specattn_prompt_attn.  A list entry outside the cache is read as the nearest slot inside it, a page number outside the
- * pool as the nearest page.  Any number of query heads per kv head up to 65536 query rows G*T; a row attends to 2^24 positions at most.
+ * pool as the nearest page.  Any number of query heads per kv head up to 65536 query rows G*T; a row attends to 2^24
+ * positions at most, and the rows of a kv head lie within 64 GiB of its first one (SPECATTN_ESHAPE otherwise).
  */
 typedef struct specattn_tree_args {
     const void *q;               /* [B][H_q][T][d] */

@@ -86,7 +86,8 @@ specattn_status check_prompt(const specattn_prompt_args *p)
     specattn_status st = check_heads(p->H_q, p->H_kv, p->d, p->dtype);
     if (st != SPECATTN_OK) return st;
     if ((int64_t)p->total_q * p->H_q > (1 << 30)) { set_error("more than 2^30 query rows"); return SPECATTN_ESHAPE; }
-    if ((int64_t)p->B * p->H_kv > (1 << 24)) { set_error("too many sequences"); return SPECATTN_ESHAPE; }
+    // (a launch has fewer than 2^32 threads along an axis: 512 for every 256 query rows, and for what is left of each sequence and kv head)
+    if ((int64_t)p->B * p->H_kv > (1 << 21)) { set_error("too many sequences"); return SPECATTN_ESHAPE; }
     if (p->page_table) {
         if (!p->seq_lens) { set_error("keys and values in pages need seq_lens"); return SPECATTN_EINVAL; }
         if (p->kv_starts) { set_error("kv_starts is for packed keys and values"); return SPECATTN_EINVAL; }

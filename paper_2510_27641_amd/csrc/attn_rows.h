@@ -603,7 +603,8 @@ template <int D> __device__ __forceinline__ void leave_slot(float *rows, float *
     }
 }
 
-constexpr int MERGE_ROWS = 4;                                 // query rows that a wave joins where they come from few slots
+// Query rows that a wave of a merge kernel joins: four, whose loads go together, where units are so many that each is in few parts; one otherwise.
+constexpr int MERGE_ROWS = 4;
 
 // Query rows of partial results in slots slot .. slot + n - 1 ([slot][qrows][D] unnormalised, references and sums [slot][2][qrows]), joined by one
 // wave: D / 8 lanes take a slot's row, eight elements each, and 512 / D slots go side by side; the order of all sums is fixed.  Every lane gets the
@@ -693,23 +694,21 @@ template <int D> struct Slots {
         together(j);
         return j;
     }
-    // What wave `w` of as many as there are rows does: the row of its number, or, where so few slots are joined that loads are short, MERGE_ROWS of
-    // them (and the last waves none).  done(row, Joined) is called for each.
-    template <typename DONE> __device__ __forceinline__ void join(int w, int all, DONE &&done) const
+    // Rows c0 .. c0 + N - 1 of at most `all`; done(row, Joined) is called for each.
+    template <int N, typename DONE> __device__ __forceinline__ void join(int c0, int all, DONE &&done) const
     {
+        if (c0 >= all) return;
         if (n > SIDE) {
-            if (w < all) done(w, many(w));
+            for (int k = 0; k < N && c0 + k < all; ++k) done(c0 + k, many(c0 + k));
             return;
         }
-        const int c0 = w * MERGE_ROWS;
-        if (c0 >= all) return;
-        int c[MERGE_ROWS];
-        Joined j[MERGE_ROWS];
+        int c[N];
+        Joined j[N];
 #pragma unroll
-        for (int k = 0; k < MERGE_ROWS; ++k) c[k] = min(c0 + k, all - 1);
+        for (int k = 0; k < N; ++k) c[k] = min(c0 + k, all - 1);
         few(c, j);
 #pragma unroll
-        for (int k = 0; k < MERGE_ROWS; ++k)
+        for (int k = 0; k < N; ++k)
             if (c0 + k < all) done(c0 + k, j[k]);
     }
 };

@@ -15,6 +15,7 @@ namespace {
 constexpr int PLAN_THREADS = 1024;
 constexpr int PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int MAP_THREADS = 256;
+constexpr int MAP_STARTS = 4096;
 constexpr int ONE_WORKGROUP = 1024;                           // sequences that it holds in LDS
 
 struct PagesArgs {
@@ -51,23 +52,30 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t v)
     v = add(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
     return v;
 }
-// Sum of v over the threads ahead of this one, and over all.
-__device__ __forceinline__ uint32_t block_sums(uint32_t v, uint32_t &all, uint32_t *lds)
+// Sums of N values over the threads ahead of this one, and over all.
+template <int N> struct Sums { uint32_t ahead[N], all[N]; };
+template <int N> __device__ __forceinline__ Sums<N> block_sums(const uint32_t (&v)[N], uint32_t *lds)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t up = wave_sums(v);
+    Sums<N> s;
     __syncthreads();
-    if (lane == 63) lds[wave] = up;
-    __syncthreads();
-    uint32_t ahead = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)up, 0x138, 0xf, 0xf, true);   // of the lane before (0 in the first)
-    all = 0;
 #pragma unroll
-    for (int w = 0; w < PLAN_WAVES; ++w) {
-        const uint32_t s = lds[w];
-        ahead = w < wave ? add(ahead, s) : ahead;
-        all = add(all, s);
+    for (int k = 0; k < N; ++k) {
+        const uint32_t up = wave_sums(v[k]);
+        if (lane == 63) lds[k * PLAN_WAVES + wave] = up;
+        s.ahead[k] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)up, 0x138, 0xf, 0xf, true);       // of the lane before (0 in the first)
+        s.all[k] = 0;
     }
-    return ahead;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int w = 0; w < PLAN_WAVES; ++w) {
+            const uint32_t x = lds[k * PLAN_WAVES + w];
+            s.ahead[k] = w < wave ? add(s.ahead[k], x) : s.ahead[k];
+            s.all[k] = add(s.all[k], x);
+        }
+    return s;
 }
 
 __device__ __forceinline__ int pages_of(const PagesArgs &a, int len) { return (int)(((uint32_t)len + (1u << a.page_shift) - 1) >> a.page_shift); }
@@ -82,52 +90,57 @@ __device__ void plan(const PagesArgs &a, Record *records, int *starts, Totals *t
         then = a.new_lens[b];
         flag = now < 0 || now > reach || then < 0 ? SPECATTN_ROW_INVALID : then > reach ? SPECATTN_ROW_OVERFLOW : 0;
     };
+    // what is returned in all comes first; of up to PLAN_THREADS sequences it is known when it is needed
     uint32_t given_all = 0;
-    for (int b0 = 0; b0 < a.B; b0 += PLAN_THREADS) {
+    for (int b0 = 0; a.B > PLAN_THREADS && b0 < a.B; b0 += PLAN_THREADS) {
         const int b = b0 + tid;
         int now, then;
-        uint32_t flag, all, gives = 0;
+        uint32_t flag, gives[1] = {0};
         if (b < a.B) {
             read(b, now, then, flag);
-            if (!flag && then < now) gives = (uint32_t)(pages_of(a, now) - pages_of(a, then));
+            if (!flag && then < now) gives[0] = (uint32_t)(pages_of(a, now) - pages_of(a, then));
         }
-        block_sums(gives, all, lds);
-        given_all = add(given_all, all);
+        given_all = add(given_all, block_sums(gives, lds).all[0]);
     }
-    const int stack = (int)min((uint64_t)count + given_all, (uint64_t)a.num_pages);
     uint32_t given = 0, asked = 0, came = 0;                  // ahead of these sequences
-    int taken_all = 0, tokens_all = 0;
+    int taken_all = 0, tokens_all = 0, stack = 0;
     for (int b0 = 0; b0 < a.B; b0 += PLAN_THREADS) {
         const int b = b0 + tid;
         int now = 0, then = 0;
-        uint32_t flag = SPECATTN_ROW_INVALID, gives = 0, asks = 0, tokens = 0, all;
+        uint32_t flag = SPECATTN_ROW_INVALID, gives = 0, asks = 0, tokens = 0;
         if (b < a.B) read(b, now, then, flag);
         if (!flag) {
             gives = then < now ? (uint32_t)(pages_of(a, now) - pages_of(a, then)) : 0;
             asks = then > now ? (uint32_t)(pages_of(a, then) - pages_of(a, now)) : 0;
         }
-        const uint32_t given_before = add(given, block_sums(gives, all, lds));
-        given = add(given, all);
-        const uint32_t asked_before = add(asked, block_sums(asks, all, lds));
-        asked = add(asked, all);
+        const uint32_t pages[2] = {gives, asks};
+        const Sums<2> p = block_sums(pages, lds);
+        if (a.B <= PLAN_THREADS) given_all = p.all[0];
+        stack = (int)min((uint64_t)count + given_all, (uint64_t)a.num_pages);
+        const uint32_t given_before = add(given, p.ahead[0]), asked_before = add(asked, p.ahead[1]);
+        given = add(given, p.all[0]);
+        asked = add(asked, p.all[1]);
         if (asks && add(asked_before, asks) > (uint32_t)stack) flag |= SPECATTN_ROW_OVERFLOW;
         if (!flag && then > now) tokens = (uint32_t)(then - now);
-        const uint32_t came_before = add(came, block_sums(tokens, all, lds));
-        came = add(came, all);
-        if (tokens && add(came_before, tokens) > (uint32_t)a.capacity) flag |= SPECATTN_ROW_OVERFLOW;
-        const bool grows = !flag && then > now;
+        const uint32_t coming[1] = {tokens};
+        const Sums<1> c = block_sums(coming, lds);
+        if (tokens && add(add(came, c.ahead[0]), tokens) > (uint32_t)a.capacity) flag |= SPECATTN_ROW_OVERFLOW;
+        came = add(came, c.all[0]);
         // (sequences are refused from one on, as far as they ask for anything, so that what is granted lies without gaps)
-        const uint32_t granted = block_sums(grows ? (uint32_t)(then - now) : 0, all, lds) + (uint32_t)tokens_all;
+        const bool grows = !flag && then > now;
+        const uint32_t grants[2] = {grows ? (uint32_t)(then - now) : 0, grows ? asks : 0};
+        Sums<2> g = {{c.ahead[0], 0}, {c.all[0], p.all[1]}};
+        if (__syncthreads_or(flag == SPECATTN_ROW_OVERFLOW)) g = block_sums(grants, lds);
         if (b < a.B) {
+            const int start = tokens_all + (int)g.ahead[0];
             records[b] = Record{now, flag ? now : then, (int)given_before, (int)asked_before};
-            starts[b] = (int)granted;
-            if (a.token_starts) a.token_starts[b] = (int)granted;
+            starts[b] = start;
+            if (a.token_starts) a.token_starts[b] = start;
             a.lens_out[b] = flag ? now : then;
             if (a.flags) a.flags[b] = flag;
         }
-        tokens_all += (int)all;
-        block_sums(grows ? asks : 0, all, lds);
-        taken_all += (int)all;
+        tokens_all += (int)g.all[0];
+        taken_all += (int)g.all[1];
     }
     if (tid == 0) {
         totals->count = count;
@@ -159,40 +172,58 @@ __device__ __forceinline__ int stack_entry(const PagesArgs &a, const Plan &p, in
     return a.table[(int64_t)b * a.max_pages + pages_of(a, r.then) + rank - r.given];
 }
 
-// Table entries and returned pages of sequences first, first + step, ...: a wave each.
-__device__ __forceinline__ void write_pages(const PagesArgs &a, const Plan &p, int first, int step)
+// Table entries and returned pages, LANES threads to a sequence.
+template <int LANES> __device__ __forceinline__ void write_pages(const PagesArgs &a, const Plan &p, int64_t thread, int64_t threads)
 {
-    const int lane = threadIdx.x & 63;
-    for (int b = first; b < a.B; b += step) {
+    const int lane = (int)(thread % LANES);
+    for (int64_t b = thread / LANES; b < a.B; b += threads / LANES) {
         const Record r = p.records[b];
         const int have = pages_of(a, r.now), need = pages_of(a, r.then);
-        int32_t *row = a.table + (int64_t)b * a.max_pages;
-        for (int k = lane; k < need - have; k += 64) row[have + k] = stack_entry(a, p, p.totals->stack - 1 - r.taken - k);
-        for (int k = lane; k < have - need; k += 64) {
+        int32_t *row = a.table + b * a.max_pages;
+        for (int k = lane; k < need - have; k += LANES) row[have + k] = stack_entry(a, p, p.totals->stack - 1 - r.taken - k);
+        for (int k = lane; k < have - need; k += LANES) {
             const int64_t to = (int64_t)p.totals->count + r.given + k;
             if (to < a.num_pages) a.free_pages[to] = row[need + k];
         }
     }
 }
 
-// Slots of new tokens first, first + step, ...; -1 behind the last one.
-__device__ __forceinline__ void write_tokens(const PagesArgs &a, const Plan &p, int64_t first, int64_t step)
+// Slots of new tokens; -1 behind the last one.  A thread takes four tokens at a time, so that their lookups are under way together.
+__device__ __forceinline__ void write_tokens(const PagesArgs &a, const Plan &p, int64_t thread, int64_t threads)
 {
+    constexpr int U = 4;
     const Record last = p.records[a.B - 1];
     const int tokens = p.starts[a.B - 1] + max(last.then - last.now, 0);
-    for (int64_t i = first; i < a.capacity; i += step) {
-        int slot = -1, place = -1, b = -1;
-        if (i < tokens) {
-            b = last_not_above(a.B, (int)i, [&](int x) { return p.starts[x]; });
-            const Record r = p.records[b];
-            place = r.now + (int)i - p.starts[b];
-            const int have = pages_of(a, r.now), at = place >> a.page_shift;
-            const int page = at < have ? a.table[(int64_t)b * a.max_pages + at] : stack_entry(a, p, p.totals->stack - 1 - r.taken - (at - have));
-            if (page >= 0 && page < a.num_pages) slot = (int)(((uint32_t)page << a.page_shift) | ((uint32_t)place & ((1u << a.page_shift) - 1)));
+    const int stack = p.totals->stack;
+    for (int64_t i0 = thread; i0 < a.capacity; i0 += U * threads) {
+        int b[U], place[U], page[U];
+        Record r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + u * threads;
+            b[u] = i < tokens ? last_not_above(a.B, (int)i, [&](int x) { return p.starts[x]; }) : -1;
         }
-        a.slots[i] = slot;
-        if (a.positions) a.positions[i] = place;
-        if (a.owners) a.owners[i] = b;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            r[u] = p.records[max(b[u], 0)];
+            place[u] = b[u] < 0 ? -1 : r[u].now + (int)(i0 + u * threads) - p.starts[b[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            page[u] = -1;
+            if (b[u] < 0) continue;
+            const int have = pages_of(a, r[u].now), at = place[u] >> a.page_shift;
+            page[u] = at < have ? a.table[(int64_t)b[u] * a.max_pages + at] : stack_entry(a, p, stack - 1 - r[u].taken - (at - have));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = i0 + u * threads;
+            if (i >= a.capacity) continue;
+            const bool some = page[u] >= 0 && page[u] < a.num_pages;
+            a.slots[i] = some ? (int)(((uint32_t)page[u] << a.page_shift) | ((uint32_t)place[u] & ((1u << a.page_shift) - 1))) : -1;
+            if (a.positions) a.positions[i] = place[u];
+            if (a.owners) a.owners[i] = b[u];
+        }
     }
 }
 
@@ -201,24 +232,31 @@ __global__ __launch_bounds__(PLAN_THREADS) void pages_kernel(PagesArgs a)
     __shared__ Record records[ONE_WORKGROUP];
     __shared__ int starts[ONE_WORKGROUP];
     __shared__ Totals totals;
-    __shared__ uint32_t lds[PLAN_WAVES];
+    __shared__ uint32_t lds[2 * PLAN_WAVES];
     plan(a, records, starts, &totals, lds);
     __syncthreads();
     const Plan p = {records, starts, &totals};
-    write_pages(a, p, threadIdx.x >> 6, PLAN_WAVES);
+    write_pages<16>(a, p, threadIdx.x, PLAN_THREADS);
     if (a.slots) write_tokens(a, p, threadIdx.x, PLAN_THREADS);
 }
 
 __global__ __launch_bounds__(PLAN_THREADS) void pages_plan_kernel(PagesArgs a, Record *records, int *starts, Totals *totals)
 {
-    __shared__ uint32_t lds[PLAN_WAVES];
+    __shared__ uint32_t lds[2 * PLAN_WAVES];
     plan(a, records, starts, totals, lds);
 }
 
+// (the tokens' sequences are found in LDS, as far as they fit there: every step of halving the starts in memory is a trip to L2)
 __global__ __launch_bounds__(MAP_THREADS) void pages_map_kernel(PagesArgs a, Plan p)
 {
+    __shared__ int starts[MAP_STARTS];
+    if (a.B <= MAP_STARTS) {
+        for (int i = threadIdx.x; i < a.B; i += MAP_THREADS) starts[i] = p.starts[i];
+        __syncthreads();
+        p.starts = starts;
+    }
     const int64_t thread = (int64_t)blockIdx.x * MAP_THREADS + threadIdx.x, threads = (int64_t)gridDim.x * MAP_THREADS;
-    write_pages(a, p, (int)(thread >> 6), (int)(threads >> 6));
+    write_pages<64>(a, p, thread, threads);
     if (a.slots) write_tokens(a, p, thread, threads);
 }
 

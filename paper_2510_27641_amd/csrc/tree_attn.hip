@@ -291,7 +291,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
 }
 
 // Units that several shares worked on: their partial results joined, in the order of the shares.
-template <int D, bool F16> __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int qrows)
+template <int D, bool F16, int N> __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int qrows)
 {
     const int unit = blockIdx.x;
     const int2 parts = a.parts[unit];
@@ -300,7 +300,7 @@ template <int D, bool F16> __global__ __launch_bounds__(256) void tree_merge_ker
     const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
     const int lane = threadIdx.x & 63, nodes = nodes_of(a, b), queries = a.G * a.T;
     const Slots<D> slots = {a.slots, a.slots_ml, (int64_t)parts.x + unit, parts.y - parts.x + 1, qrows};
-    slots.join(blockIdx.y * 4 + (threadIdx.x >> 6), min(qrows, queries - block * qrows), [&](int c, const Joined &j) {
+    slots.template join<N>((blockIdx.y * 4 + (threadIdx.x >> 6)) * N, min(qrows, queries - block * qrows), [&](int c, const Joined &j) {
         if (lane < D / 8) finish_row<D, F16>(a, j, b, h, block * qrows + c, nodes, lane);
     });
 }
@@ -319,6 +319,12 @@ TreeKernel variant(int d, bool f16, int parts, int qrows)
 {
     return d == 128 ? (f16 ? by_parts<128, true>(parts, qrows) : by_parts<128, false>(parts, qrows))
                     : (f16 ? by_parts<64, true>(parts, qrows) : by_parts<64, false>(parts, qrows));
+}
+typedef void (*MergeKernel)(TreeArgs, int);
+template <int D, bool F16> MergeKernel merge_by_rows(int per) { return per == 1 ? tree_merge_kernel<D, F16, 1> : tree_merge_kernel<D, F16, MERGE_ROWS>; }
+MergeKernel merge_variant(int d, bool f16, int per)
+{
+    return d == 128 ? (f16 ? merge_by_rows<128, true>(per) : merge_by_rows<128, false>(per)) : (f16 ? merge_by_rows<64, true>(per) : merge_by_rows<64, false>(per));
 }
 template <int D> size_t lds_of(int qrows) { return qrows == 64 ? Geo<D, 4, 2, 128>::LDS_BYTES : Geo<D, 8, 8, 128>::LDS_BYTES; }
 size_t lds_size(int d, int qrows, int rows) { return (d == 128 ? lds_of<128>(qrows) : lds_of<64>(qrows)) + (size_t)(rows + 1) * 4; }
@@ -411,8 +417,8 @@ specattn_status launch_tree(const specattn_tree_args *t, hipStream_t stream)
         st = check_launch("tree_kernel");
         if (st != SPECATTN_OK) return st;
         if (a.whole) continue;
-        const auto merge = t->d == 128 ? (f16 ? tree_merge_kernel<128, true> : tree_merge_kernel<128, false>) : (f16 ? tree_merge_kernel<64, true> : tree_merge_kernel<64, false>);
-        merge<<<dim3(a.rows * a.blocks, (std::min(queries, qrows) + 3) / 4), 256, 0, stream>>>(a, qrows);
+        const int per = units * 4 >= cu_count() ? MERGE_ROWS : 1;
+        merge_variant(t->d, f16, per)<<<dim3(units, (std::min(queries, qrows) + 4 * per - 1) / (4 * per)), 256, 0, stream>>>(a, qrows);
         st = check_launch("tree_merge_kernel");
         if (st != SPECATTN_OK) return st;
     }

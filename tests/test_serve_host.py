@@ -87,7 +87,8 @@ def test_store_refusals(kw, status):
     (False, dict(total_q=0), sa.EINVAL), (False, dict(total_kv=0), sa.EINVAL), (False, dict(dtype=sa.F32), sa.EUNSUPPORTED), (False, dict(H_q=30), sa.ESHAPE),
     (False, dict(d=96), sa.ESHAPE), (False, dict(kv_stride_n=64), sa.ESHAPE), (False, dict(q_stride_t=4100), sa.EALIGN), (False, dict(v=0x30008), sa.EALIGN),
     (False, dict(out=0x8), sa.EALIGN), (False, dict(total_q=1 << 26), sa.ESHAPE), (False, dict(total_kv=(1 << 30) + 1), sa.ESHAPE),
-    (False, dict(seq_lens=0x1000), sa.EINVAL), (False, dict(B=1 << 22), sa.ESHAPE),
+    (False, dict(seq_lens=0x1000), sa.EINVAL), (False, dict(B=1 << 22), sa.ESHAPE), (False, dict(B=(1 << 18) + 1), sa.ESHAPE),
+    (False, dict(kv_stride_n=1 << 23), sa.ESHAPE), (True, dict(kv_stride_page=1 << 27), sa.ESHAPE),
     (True, dict(seq_lens=None), sa.EINVAL), (True, dict(kv_starts=0x1000), sa.EINVAL), (True, dict(page_size=24), sa.ESHAPE), (True, dict(num_pages=0), sa.EINVAL),
     (True, dict(kv_stride_page=0), sa.ESHAPE), (True, dict(kv_stride_page=12), sa.EALIGN), (True, dict(max_pages_per_seq=0), sa.ESHAPE),
     (True, dict(max_pages_per_seq=1 << 27), sa.ESHAPE), (True, dict(total_q=100), sa.EWORKSPACE),
@@ -106,6 +107,7 @@ def test_prompt_refusals(paged, kw, status):
     (False, dict(H_q=1 << 13, T=64, H_kv=4), sa.ESHAPE), (False, dict(idx_capacity=0), sa.ESHAPE), (False, dict(idx_stride_row=5), sa.ESHAPE),
     (False, dict(chunk_size=12), sa.ESHAPE), (False, dict(chunk_size=16, indices=None, counts=None), sa.EUNSUPPORTED),
     (False, dict(idx_capacity=1 << 22, idx_stride_row=1 << 22, chunk_size=16), sa.ESHAPE), (False, dict(num_pages=3), sa.EINVAL),
+    (False, dict(kv_stride_n=1 << 27), sa.ESHAPE), (True, dict(kv_stride_page=1 << 29), sa.ESHAPE),
     (False, dict(kv_stride_n=32), sa.ESHAPE), (False, dict(kv_stride_b=4), sa.EALIGN), (False, dict(k_new=0x40004), sa.EALIGN), (False, dict(q_stride_t=65), sa.EALIGN),
     (True, dict(chunk_size=16, indices_are_physical=1), sa.EUNSUPPORTED), (True, dict(page_size=10), sa.ESHAPE), (True, dict(max_pages_per_seq=8), sa.ESHAPE),
     (True, dict(num_pages=0), sa.EINVAL), (True, dict(kv_stride_page=-8), sa.ESHAPE), (True, {}, sa.EWORKSPACE), (False, {}, sa.EWORKSPACE),
