@@ -805,6 +805,6 @@ specattn_status specattn_init(void)
 
 const char *specattn_last_error(void) { return g_error; }
 
-int specattn_version(void) { return 1010; }
+int specattn_version(void) { return 1020; }
 
 }  // extern "C"

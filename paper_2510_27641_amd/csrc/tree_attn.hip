@@ -305,14 +305,14 @@ template <int D, bool F16, int N> __global__ __launch_bounds__(256) void tree_me
     });
 }
 
-// Query rows of a unit: 64 for four waves, two of which share rows, or 256 for eight.  (us with 8 x 32 tokens over 7500 of 32768 positions, 128
-// rows to a kv head: two workgroups of four waves with 128 rows each 91, one of eight waves, half of which only fetch, 80.)
-int rows_per_unit(int queries) { return queries <= 64 ? 64 : 256; }
+// Query rows of a unit: 64 for four waves or 128 for eight, two of which share rows, or 256 for eight.  (us of calls with 65 to 128 rows to a kv
+// head, units of 128 / 256: 8 x 32 nodes over 7500 of 32768 positions 79 / 83, 32 x 26 over 1640 of 4096 59 / 65.)
+int rows_per_unit(int queries) { return queries <= 64 ? 64 : queries <= 128 ? 128 : 256; }
 
 typedef void (*TreeKernel)(TreeArgs);
 template <int D, bool F16, int PARTS> TreeKernel by_rows(int qrows)
 {
-    return qrows == 64 ? tree_kernel<D, F16, 4, 2, PARTS> : tree_kernel<D, F16, 8, 8, PARTS>;
+    return qrows == 64 ? tree_kernel<D, F16, 4, 2, PARTS> : qrows == 128 ? tree_kernel<D, F16, 8, 4, PARTS> : tree_kernel<D, F16, 8, 8, PARTS>;
 }
 template <int D, bool F16> TreeKernel by_parts(int parts, int qrows) { return parts == 1 ? by_rows<D, F16, 1>(qrows) : by_rows<D, F16, 2>(qrows); }
 TreeKernel variant(int d, bool f16, int parts, int qrows)
@@ -359,8 +359,8 @@ specattn_status tree_configure()
     }
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return SPECATTN_OK;
-    for (int k = 0; k < 16; ++k) {
-        const int d = k & 1 ? 128 : 64, qrows = k & 8 ? 256 : 64;
+    for (int k = 0; k < 24; ++k) {
+        const int d = k & 1 ? 128 : 64, qrows = 64 << (k >> 3);
         const size_t bytes = lds_size(d, qrows, MAX_UNITS);
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(variant(d, k & 2, k & 4 ? 2 : 1, qrows)), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
             (void)hipGetLastError();
@@ -413,7 +413,7 @@ specattn_status launch_tree(const specattn_tree_args *t, hipStream_t stream)
         a.whole = tiles <= WHOLE_TILES;
         const int units = a.rows * a.blocks;
         const int grid = a.whole ? units : (int)std::min<int64_t>(cu_count(), (units * tiles + MIN_TILES - 1) / MIN_TILES);
-        variant(t->d, f16, t->out ? 2 : 1, qrows)<<<grid, qrows == 256 ? 512 : 256, lds_size(t->d, qrows, a.rows), stream>>>(a);
+        variant(t->d, f16, t->out ? 2 : 1, qrows)<<<grid, qrows == 64 ? 256 : 512, lds_size(t->d, qrows, a.rows), stream>>>(a);
         st = check_launch("tree_kernel");
         if (st != SPECATTN_OK) return st;
         if (a.whole) continue;
