@@ -119,7 +119,7 @@ struct Line {
         const int before = r == rows ? tiles : prefix ? __builtin_amdgcn_readfirstlane(prefix[r]) : __builtin_amdgcn_readlane(ahead, r);
         return before + setup * r * blocks;
     }
-    __device__ __forceinline__ int row_of(int place) const
+    __device__ __forceinline__ int row_of(int place) const     // (as all below: by a whole wave)
     {
         const int lane = threadIdx.x & 63;
         if (!prefix) return __popcll(__ballot(lane < rows && ahead + setup * lane * blocks <= place)) - 1;
@@ -279,7 +279,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         }
         const bool whole = first == 0 && last == n;
         const int64_t slot = share + unit;
-        if (first == 0 && tid == 0 && !o.whole) o.parts[unit] = make_int2(share, by_unit ? share : line.of(tiles_at + n - 1));
+        if (first == 0 && wave == 0 && !o.whole) {            // (all of the wave: it looks the share up together)
+            const int2 parts = make_int2(share, by_unit ? share : line.of(tiles_at + n - 1));
+            if (lane == 0) o.parts[unit] = parts;
+        }
         emit_rows<G>(smem, [&](int c, const Joined &j, int e) {
             const int qr = block * G::QROWS + c;
             if (qr >= queries) return;

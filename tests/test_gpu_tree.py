@@ -253,6 +253,14 @@ def test_long_rows_are_cut_and_joined_in_order():
         assert torch.equal(c.out, first)
 
 
+@pytest.mark.parametrize("B,H_q,T,n,seed", [(30, 2, 3, 3000, 4), (30, 2, 3, 3000, 5), (48, 2, 3, 2500, 6), (48, 2, 3, 2500, 11), (12, 16, 33, 2000, 1)])
+def test_cuts_in_many_ragged_rows(B, H_q, T, n, seed):
+    """Cuts that are moved to a unit's ends in one place and left in another: the joining takes every share of a unit, and no other unit's."""
+    lens = np.random.default_rng(seed).integers(1, n, B).astype(np.int32)
+    c = Case(B, H_q, 2, T, 64, n, seed=seed)
+    c.check([[np.arange(x)] * 2 for x in lens], seq_lens=lens)
+
+
 def test_a_chain_is_the_causal_decode_attention():
     """Masks 0 .. t: what specattn_sparse_decode_attn computes with new tokens."""
     c = Case(2, 16, 4, 5, 128, 700, seed=14)
