@@ -18,7 +18,9 @@ constexpr int MAX_UNITS = 2048;                               // rows (b, h) per
 constexpr int MIN_TILES = 4;                                  // of a share
 constexpr int FEW = 64;                                       // rows that a wave scans by itself
 constexpr int WHOLE_TILES = 8;                                // units of up to so many are not cut: joining them takes a second launch
-constexpr int SETUP = 4;                                      // what a unit costs beside its tiles
+// Tiles that a unit costs beside its own: 10 us or so for finding its rows, first fetches and putting its result down.  (us with 4 / 8 / 10 / 14: 16
+// trees of 64 nodes over 256 to 16384 positions 131 / 131 / 122 / 134, 64 of 8 over 64 to 4096 72 / 66 / 65 / 65, 8 of 64 over 8192 65 / 64 / 59 / 60.)
+constexpr int SETUP = 10;
 
 struct TreeArgs {
     const uint16_t *q;
@@ -106,8 +108,8 @@ struct Line {
         : prefix(prefix_), ahead(ahead_), rows(rows_), blocks(blocks_), tiles(tiles_)
     {
         n = min(most, max(tiles / MIN_TILES, 1));
-        setup = min(SETUP, (int)((uint32_t)tiles / (uint32_t)n) / 4);
-        direct = rows * blocks <= most && largest <= (int)((uint32_t)tiles / (uint32_t)n) + 2 * SETUP;
+        setup = min(SETUP, (int)((uint32_t)tiles / (uint32_t)n) / 2);
+        direct = rows * blocks <= most && largest <= (int)((uint32_t)tiles / (uint32_t)n) + SETUP;
         if (direct) n = rows * blocks;
         const int total = tiles + setup * rows * blocks;
         each = (int)((uint32_t)total / (uint32_t)n);
