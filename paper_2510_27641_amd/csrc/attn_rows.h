@@ -147,6 +147,9 @@ __device__ __forceinline__ int wave_largest(int v)
 // The low `n` bits (none below 1, all from 64 on).
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
+// The reference of a part as it is put down: minus infinity says that nothing was attended to, which is not so where a score was NaN.
+__device__ __forceinline__ float reference(float ref, float sum) { return sum == sum ? ref : sum; }
+
 // One wave's 32 query rows.
 // PARTS: parts of the element type that a weight enters the second product in.  Where the result is asked for in that type alone, one:
 // its rounding (half a step, averaged over the row) is below the result's own.  Where it is asked for in fp32, two.
@@ -327,7 +330,7 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
             }
         if (half == 0) {
             float *ml = reinterpret_cast<float *>(smem + G::OFF_ML);
-            ml[wave * 32 + row] = ref;
+            ml[wave * 32 + row] = reference(ref, sum);
             ml[G::NW * 32 + wave * 32 + row] = sum;
         }
     }
@@ -602,7 +605,7 @@ template <int D> __device__ __forceinline__ void leave_slot(float *rows, float *
     *reinterpret_cast<f32x4 *>(x) = f32x4{j.o[0], j.o[1], j.o[2], j.o[3]};
     *reinterpret_cast<f32x4 *>(x + 4) = f32x4{j.o[4], j.o[5], j.o[6], j.o[7]};
     if (e == 0) {
-        ml[slot * 2 * qrows + c] = j.ref;
+        ml[slot * 2 * qrows + c] = reference(j.ref, j.sum);
         ml[slot * 2 * qrows + qrows + c] = j.sum;
     }
 }

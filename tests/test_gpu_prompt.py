@@ -174,6 +174,18 @@ def test_hidden_values_have_no_effect(bad, dtype, d):
         assert (np.abs(got[2][rows, h] - lse) <= tol_lse)[some].all()
 
 
+@pytest.mark.parametrize("q_lens,H_q,kv_lens", [([5], 2, None), ([70, 3], 2, None), ([9], 2, [1200]), ([300], 8, None)])
+def test_a_key_that_is_no_number_shows(q_lens, H_q, kv_lens):
+    """Queries that see it are NaN, the first of which may see nothing else."""
+    c = Case(q_lens, H_q, 2, 64, "bf16", kv_lens=kv_lens, seed=13)
+    c.k[0] = float("nan")
+    sa.specattn_prompt_attn(c.args())
+    torch.cuda.synchronize()
+    n = q_lens[0]
+    for x in (c.out, c.low, c.lse):
+        assert torch.isnan(x[:n]).all() and torch.isfinite(x[n:]).all()
+
+
 def test_large_values_and_scores():
     """Values whose unnormalised sums pass fp32, and scores far apart."""
     c = Case([80], 2, 1, 128, seed=7)

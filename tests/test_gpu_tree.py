@@ -200,6 +200,25 @@ def test_hidden_nodes_have_no_effect(bad, G, T):
     assert not np.isfinite(c.out.cpu().numpy()[0][:, below]).all(axis=2).any()
 
 
+@pytest.mark.parametrize("cached", [0, 40, 2000])
+@pytest.mark.parametrize("G,T", [(1, 7), (4, 20), (8, 30)])
+def test_a_key_that_is_no_number_shows(cached, G, T):
+    """Rows that see the node are NaN, also where its score is the only one of a wave or of a share; the others have nothing of it."""
+    c = Case(1, 2 * G, 2, T, 64, max(cached, 1), seed=12)
+    c.k_new[0, :, 0] = float("nan")
+    c.masks[0, 2] = np.uint64(4)                              # a second root
+    for t in range(3, T):
+        c.masks[0, t] = np.uint64(1) << np.uint64(t) | np.uint64(t % 2) | np.uint64(2) * np.uint64(t % 3 == 0)
+    a = c.args(seq_lens=np.array([cached], dtype=np.int32))
+    sa.specattn_tree_attn(a)
+    torch.cuda.synchronize()
+    sees = np.array([bool(int(c.masks[0, t]) & 1) for t in range(T)])
+    assert sees[:2].all() and not sees[2]
+    c.compare([[np.arange(cached)] * 2], skip=sees)
+    for x in (c.out, c.low, c.lse):
+        assert torch.isnan(x[0][:, torch.from_numpy(sees).cuda()]).all()
+
+
 def test_many_rows():
     """More rows of sequences and kv heads than a launch takes."""
     c = Case(300, 8, 8, 2, 64, 40, "f16", seed=11)
