@@ -13,7 +13,7 @@
 // With fewer query rows than the waves have room for, two waves share rows and take one half of a tile each; their results are joined in LDS at the end.
 //
 // A tile costs a wave 32 matrix instructions (d = 128; 1024 cycles of its SIMD's matrix unit) and about 185 vector ones, 32 of them exponentials.
-// One causal prompt of 32768 positions, 32 heads over 8, bf16: 8.1 ms, 1.09 PFLOP/s (a library product of 8192^3 reaches 1.20), the matrix units busy for 51 %
+// One causal prompt of 32768 positions, 32 heads over 8, bf16: 8.1 to 8.8 ms, 1.00 to 1.09 PFLOP/s (a library product of 8192^3 reaches 1.20), the matrix units busy for 51 %
 // of the cycles at 1.94 GHz.  Two groups of waves that take turns between products and softmax, and fetches spread between the products, took the same time.
 #pragma once
 
