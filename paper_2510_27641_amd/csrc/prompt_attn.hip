@@ -142,13 +142,17 @@ __device__ __forceinline__ CacheRows cache_rows(const PromptArgs &a, const Seque
     return src;
 }
 
-// A finished row: query row qr of a sequence's kv head h, elements 8 e .. 8 e + 7.
+// A finished row: query row qr of a sequence's kv head h, elements 8 e .. 8 e + 7.  (A row that sees nothing is zeros, whatever it holds: an infinity or NaN
+// that rows beside it see has come into it as 0 * infinity.)
 template <int D, bool F16> __device__ __forceinline__ void finish_row(const PromptArgs &a, const Joined &j, int q0, int h, int qr, int e)
 {
     const bool none = j.sum == 0.0f;
     const int t = a.per_g.divide(qr);
     const int64_t to = (int64_t)(q0 + t) * a.H_q + h * a.G + qr - t * a.G;
-    store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, j.o, none ? 0.0f : 1.0f / j.sum);
+    float o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = none ? 0.0f : j.o[i];
+    store_row<F16>(a.out, a.out_lowp, to * D + 8 * e, o, none ? 0.0f : 1.0f / j.sum);
     if (a.lse && e == 0) a.lse[to] = none ? -INFINITY : log_sum<F16>(j.ref, j.sum);
 }
 
