@@ -347,6 +347,21 @@ struct Joined {
     float ref, sum;
     float o[8];
 };
+// Parts of a row that are finite each may pass fp32 together (values near its end; a sum of weights is 1 or more).  Whether a row's elements, which LANES lanes
+// hold, are not finite although its scores were: it is then joined once more in units of 2^scale, in which its weights add up to less than 1.
+template <int LANES> __device__ __forceinline__ bool passed_fp32(const Joined &j)
+{
+    float x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x = fmaf(j.o[i], 0.0f, x);
+    const uint64_t some = __ballot(!(x == 0.0f) && j.sum - j.sum == 0.0f && j.ref > -INFINITY && j.ref < INFINITY);
+    return ((some >> (threadIdx.x & 63 & ~(LANES - 1))) & ((1ull << LANES) - 1)) != 0;
+}
+struct Units {
+    float by;
+    int scale;
+    __device__ __forceinline__ explicit Units(float sum) : scale(__builtin_amdgcn_frexp_expf(sum)) { by = __builtin_ldexpf(1.0f, -scale); }
+};
 template <typename G> __device__ __forceinline__ Joined joined(const char *smem, int row, int at)
 {
     constexpr int D = G::D, WQ = G::WQ;
@@ -367,22 +382,30 @@ template <typename G> __device__ __forceinline__ Joined joined(const char *smem,
     j.ref = -INFINITY;
 #pragma unroll
     for (int k = 0; k < G::WK; ++k) j.ref = fmaxf(j.ref, ml[(k * WQ + wq) * 32 + in]);
-    j.sum = 0.0f;
+    auto add = [&](float by) {
+        j.sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
+        for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < G::WK; ++k) {
-        const int wave = k * WQ + wq;
-        const float m = ml[wave * 32 + in];
-        if (m == -INFINITY) continue;                         // nothing was attended to (its values are zeros)
-        const float f = __builtin_amdgcn_exp2f(m - j.ref);    // (NaN where scores were)
-        j.sum = fmaf(f, ml[G::NW * 32 + wave * 32 + in], j.sum);
-        const f32x4 a = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at), b = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at + 1);
+        for (int k = 0; k < G::WK; ++k) {
+            const int wave = k * WQ + wq;
+            const float m = ml[wave * 32 + in];
+            if (m == -INFINITY) continue;                     // nothing was attended to (its values are zeros)
+            const float f = __builtin_amdgcn_exp2f(m - j.ref) * by;       // (NaN where scores were)
+            j.sum = fmaf(f, ml[G::NW * 32 + wave * 32 + in], j.sum);
+            const f32x4 a = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at), b = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at + 1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            j.o[i] = fmaf(f, a[i], j.o[i]);
-            j.o[4 + i] = fmaf(f, b[i], j.o[4 + i]);
+            for (int i = 0; i < 4; ++i) {
+                j.o[i] = fmaf(f, a[i], j.o[i]);
+                j.o[4 + i] = fmaf(f, b[i], j.o[4 + i]);
+            }
         }
+    };
+    add(1.0f);
+    if (passed_fp32<D / 8>(j)) {
+        const Units u(j.sum);
+        add(u.by);
+        j.ref += u.scale;
     }
     return j;
 }
@@ -651,15 +674,23 @@ template <int D> struct Slots {
             j[k].ref = mine;
 #pragma unroll
             for (int step = LANES; step < 64; step *= 2) j[k].ref = fmaxf(j[k].ref, __shfl_xor(j[k].ref, step));
-            const float f = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - j[k].ref);
-            const bool some = mine != -INFINITY;              // (nothing attended to: zeros)
-            j[k].sum = some ? f * l[k] : 0.0f;
+            auto add = [&](float by) {
+                const float f = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - j[k].ref) * by;
+                const bool some = mine != -INFINITY;          // (nothing attended to: zeros)
+                j[k].sum = some ? f * l[k] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                j[k].o[i] = some ? f * x[k][i] : 0.0f;
-                j[k].o[4 + i] = some ? f * y[k][i] : 0.0f;
+                for (int i = 0; i < 4; ++i) {
+                    j[k].o[i] = some ? f * x[k][i] : 0.0f;
+                    j[k].o[4 + i] = some ? f * y[k][i] : 0.0f;
+                }
+                together(j[k]);
+            };
+            add(1.0f);
+            if (passed_fp32<LANES>(j[k])) {                   // (of all lanes alike)
+                const Units u(j[k].sum);
+                add(u.by);
+                j[k].ref += u.scale;
             }
-            together(j[k]);
         }
     }
     __device__ __forceinline__ Joined many(int c) const
@@ -670,35 +701,43 @@ template <int D> struct Slots {
         for (int i = lane; i < n; i += 64) j.ref = fmaxf(j.ref, ml[(slot + i) * 2 * qrows + c]);
 #pragma unroll
         for (int step = 32; step; step >>= 1) j.ref = fmaxf(j.ref, __shfl_xor(j.ref, step));
-        j.sum = 0.0f;
+        auto add = [&](float by) {
+            j.sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
-        constexpr int U = 4;                                  // slots that a lane asks for together
-        for (int i0 = side; i0 < n; i0 += U * SIDE) {
-            f32x4 x[U], y[U];
-            float m[U], l[U];
+            for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
+            constexpr int U = 4;                              // slots that a lane asks for together
+            for (int i0 = side; i0 < n; i0 += U * SIDE) {
+                f32x4 x[U], y[U];
+                float m[U], l[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t at = slot + min(i0 + u * SIDE, n - 1);
-                const float *p = rows + (at * qrows + c) * D + 8 * e;
-                m[u] = ml[at * 2 * qrows + c];
-                l[u] = ml[at * 2 * qrows + qrows + c];
-                x[u] = *reinterpret_cast<const f32x4 *>(p);
-                y[u] = *reinterpret_cast<const f32x4 *>(p + 4);
-            }
+                for (int u = 0; u < U; ++u) {
+                    const int64_t at = slot + min(i0 + u * SIDE, n - 1);
+                    const float *p = rows + (at * qrows + c) * D + 8 * e;
+                    m[u] = ml[at * 2 * qrows + c];
+                    l[u] = ml[at * 2 * qrows + qrows + c];
+                    x[u] = *reinterpret_cast<const f32x4 *>(p);
+                    y[u] = *reinterpret_cast<const f32x4 *>(p + 4);
+                }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (i0 + u * SIDE >= n || m[u] == -INFINITY) continue;
-                const float f = __builtin_amdgcn_exp2f(m[u] - j.ref);
-                j.sum = fmaf(f, l[u], j.sum);
+                for (int u = 0; u < U; ++u) {
+                    if (i0 + u * SIDE >= n || m[u] == -INFINITY) continue;
+                    const float f = __builtin_amdgcn_exp2f(m[u] - j.ref) * by;
+                    j.sum = fmaf(f, l[u], j.sum);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    j.o[i] = fmaf(f, x[u][i], j.o[i]);
-                    j.o[4 + i] = fmaf(f, y[u][i], j.o[4 + i]);
+                    for (int i = 0; i < 4; ++i) {
+                        j.o[i] = fmaf(f, x[u][i], j.o[i]);
+                        j.o[4 + i] = fmaf(f, y[u][i], j.o[4 + i]);
+                    }
                 }
             }
+            together(j);
+        };
+        add(1.0f);
+        if (passed_fp32<LANES>(j)) {
+            const Units u(j.sum);
+            add(u.by);
+            j.ref += u.scale;
         }
-        together(j);
         return j;
     }
     // Rows c0 .. c0 + N - 1 of at most `all`; done(row, Joined) is called for each.

@@ -5,6 +5,8 @@ import pytest
 import torch
 
 import serve_reference as ref
+import test_gpu_prompt as prompts
+import test_gpu_tree as trees
 from paper_2510_27641_amd import binding as sa
 
 pytestmark = pytest.mark.gpu
@@ -32,3 +34,21 @@ def test_a_query_that_sees_nothing_beside_values_that_are_not_finite(rows, bad):
     for h in (0, 301):
         want, _, tol32, tol_low, _ = ref.attend(*(x[:n, i].double().cpu().numpy() for x, n, i in ((q, 100, h), (k, 90, h // 2), (v, 90, h // 2))), seen, d ** -0.5, "bf16")
         assert (np.abs(out[:15, h].cpu().numpy() - want[:15]) <= tol32[:15]).all() and (np.abs(low[:15, h].double().cpu().numpy() - want[:15]) <= tol_low[:15]).all()
+
+
+@pytest.mark.parametrize("q_lens,kv_lens", [([3], [700]), ([3], [4100]), ([40], [4100]), ([200], [1000])])
+def test_prompts_with_values_at_the_end_of_fp32(q_lens, kv_lens):
+    """3e38 in every row, in one part or several, waves that share rows or not: an average stays what it is however the call is cut."""
+    c = prompts.Case(q_lens, 4, 2, 128, kv_lens=kv_lens, page=16, seed=21)
+    c.v[:] = (c.v.float().sign() * 3e38).to(c.v.dtype)
+    c.v[:, :, :32] = 3e38
+    c.check()
+
+
+@pytest.mark.parametrize("G,T,n", [(1, 5, 300), (1, 5, 5000), (4, 26, 5000), (8, 30, 3000)])
+def test_trees_with_values_at_the_end_of_fp32(G, T, n):
+    c = trees.Case(1, 2 * G, 2, T, 128, n, seed=22)
+    for x in (c.v, c.v_new):
+        x[:] = (x.float().sign() * 3e38).to(x.dtype)
+        x[..., :32] = 3e38
+    c.check([[np.arange(n)] * 2])
