@@ -147,6 +147,12 @@ __device__ __forceinline__ int wave_largest(int v)
 // The low `n` bits (none below 1, all from 64 on).
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
+// Values near the end of fp32 (with bf16; with fp16 no sum comes close): rows whose unnormalised values times LARGE pass it are computed once more, with weights that add up to
+// SMALL = 2^-MORE, so that 2^MORE parts of a row (the GPU's workgroups are fewer) can be joined as they are.
+constexpr float LARGE = 262144.0f;                            // 2^18
+constexpr int MORE = 12;
+constexpr float SMALL = 1.0f / (1 << MORE);
+
 // The reference of a part as it is put down: minus infinity says that nothing was attended to, which is not so where a score was NaN.
 __device__ __forceinline__ float reference(float ref, float sum) { return sum == sum ? ref : sum; }
 
@@ -303,16 +309,16 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
         }
     }
 
-    // Whether a row with finite scores holds a value that is not finite: an infinity or NaN behind its mask came in as 0 * infinity, or
-    // large values passed fp32 ahead of the division.
+    // Whether a row with finite scores holds a value that is not finite, or so large that parts of a row could pass fp32 together: an infinity or NaN
+    // behind its mask came in as 0 * infinity, or values are near the end of fp32 (never so with sums below 2^104, always from 2^111 on).
     __device__ __forceinline__ bool spoiled() const
     {
         float x = 0.0f;
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x = fmaf(o[t][i], 0.0f, x);
-        return !(x == 0.0f) && sum - sum == 0.0f && ref > -INFINITY && ref < INFINITY;
+            for (int i = 0; i < 16; ++i) x = fmaf(o[t][i], LARGE, x);
+        return !(x - x == 0.0f) && sum - sum == 0.0f && ref > -INFINITY && ref < INFINITY;
     }
 
     // Result of this wave into its part of the LDS: unnormalised rows (16-byte chunks in a swizzled order), references and sums.
@@ -347,21 +353,6 @@ struct Joined {
     float ref, sum;
     float o[8];
 };
-// Parts of a row that are finite each may pass fp32 together (values near its end; a sum of weights is 1 or more).  Whether a row's elements, which LANES lanes
-// hold, are not finite although its scores were: it is then joined once more in units of 2^scale, in which its weights add up to less than 1.
-template <int LANES> __device__ __forceinline__ bool passed_fp32(const Joined &j)
-{
-    float x = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x = fmaf(j.o[i], 0.0f, x);
-    const uint64_t some = __ballot(!(x == 0.0f) && j.sum - j.sum == 0.0f && j.ref > -INFINITY && j.ref < INFINITY);
-    return ((some >> (threadIdx.x & 63 & ~(LANES - 1))) & ((1ull << LANES) - 1)) != 0;
-}
-struct Units {
-    float by;
-    int scale;
-    __device__ __forceinline__ explicit Units(float sum) : scale(__builtin_amdgcn_frexp_expf(sum)) { by = __builtin_ldexpf(1.0f, -scale); }
-};
 template <typename G> __device__ __forceinline__ Joined joined(const char *smem, int row, int at)
 {
     constexpr int D = G::D, WQ = G::WQ;
@@ -382,30 +373,22 @@ template <typename G> __device__ __forceinline__ Joined joined(const char *smem,
     j.ref = -INFINITY;
 #pragma unroll
     for (int k = 0; k < G::WK; ++k) j.ref = fmaxf(j.ref, ml[(k * WQ + wq) * 32 + in]);
-    auto add = [&](float by) {
-        j.sum = 0.0f;
+    j.sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
+    for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < G::WK; ++k) {
-            const int wave = k * WQ + wq;
-            const float m = ml[wave * 32 + in];
-            if (m == -INFINITY) continue;                     // nothing was attended to (its values are zeros)
-            const float f = __builtin_amdgcn_exp2f(m - j.ref) * by;       // (NaN where scores were)
-            j.sum = fmaf(f, ml[G::NW * 32 + wave * 32 + in], j.sum);
-            const f32x4 a = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at), b = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at + 1);
+    for (int k = 0; k < G::WK; ++k) {
+        const int wave = k * WQ + wq;
+        const float m = ml[wave * 32 + in];
+        if (m == -INFINITY) continue;                         // nothing was attended to (its values are zeros)
+        const float f = __builtin_amdgcn_exp2f(m - j.ref);    // (NaN where scores were)
+        j.sum = fmaf(f, ml[G::NW * 32 + wave * 32 + in], j.sum);
+        const f32x4 a = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at), b = left_row<D>(smem + wave * 32 * D * 4, in, 2 * at + 1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                j.o[i] = fmaf(f, a[i], j.o[i]);
-                j.o[4 + i] = fmaf(f, b[i], j.o[4 + i]);
-            }
+        for (int i = 0; i < 4; ++i) {
+            j.o[i] = fmaf(f, a[i], j.o[i]);
+            j.o[4 + i] = fmaf(f, b[i], j.o[4 + i]);
         }
-    };
-    add(1.0f);
-    if (passed_fp32<D / 8>(j)) {
-        const Units u(j.sum);
-        add(u.by);
-        j.ref += u.scale;
     }
     return j;
 }
@@ -564,8 +547,8 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, WHERE
     }
 }
 
-// Rows of this wave that an infinity or NaN in a place that their mask hides has spoiled (0 * infinity), or whose unnormalised values passed fp32: once
-// more, one row after the other, from what they attend to alone and with weights that add up to 1.  Runs behind leave(), over the same tiles.
+// Rows of this wave that an infinity or NaN in a place that their mask hides has spoiled (0 * infinity), or whose unnormalised values came close to the end of fp32: once
+// more, one row after the other, from what they attend to alone and with weights that add up to SMALL.  Runs behind leave(), over the same tiles.
 // `query(row)`: the row's query; `seen(tile, row)`: the positions that a row of the wave sees.
 template <typename G, bool F16, typename QUERY, typename SEEN>
 __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const CacheRows &src, int first, int last, int cached, int wk, char *smem, QUERY query, SEEN seen)
@@ -604,7 +587,7 @@ __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const Cac
                 for (int i = 0; i < D / 64; ++i) s = fmaf(x[i], Half<F16>::widen(k[64 * i + lane]), s);
 #pragma unroll
                 for (int step = 32; step; step >>= 1) s += __shfl_xor(s, step);
-                const float w = __builtin_amdgcn_exp2f(fmaf(s, scale, Half<F16>::HEAD - ref)) / sum;
+                const float w = __builtin_amdgcn_exp2f(fmaf(s, scale, Half<F16>::HEAD - ref)) / sum * SMALL;
 #pragma unroll
                 for (int i = 0; i < D / 64; ++i) acc[i] = fmaf(w, Half<F16>::widen(v[64 * i + lane]), acc[i]);
             }
@@ -615,8 +598,8 @@ __device__ __forceinline__ void mend_rows(uint64_t which, float scale, const Cac
             *reinterpret_cast<float *>(mine + row * D * 4 + (((e >> 2) ^ (row & (D / 4 - 1))) << 4) + 4 * (e & 3)) = acc[i];
         }
         if (lane == 0) {
-            ml[row] = ref + __builtin_amdgcn_logf(sum);
-            ml[G::NW * 32 + row] = 1.0f;
+            ml[row] = ref + __builtin_amdgcn_logf(sum) + MORE;
+            ml[G::NW * 32 + row] = SMALL;
         }
     }
 }
@@ -674,23 +657,15 @@ template <int D> struct Slots {
             j[k].ref = mine;
 #pragma unroll
             for (int step = LANES; step < 64; step *= 2) j[k].ref = fmaxf(j[k].ref, __shfl_xor(j[k].ref, step));
-            auto add = [&](float by) {
-                const float f = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - j[k].ref) * by;
-                const bool some = mine != -INFINITY;          // (nothing attended to: zeros)
-                j[k].sum = some ? f * l[k] : 0.0f;
+            const float f = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - j[k].ref);
+            const bool some = mine != -INFINITY;              // (nothing attended to: zeros)
+            j[k].sum = some ? f * l[k] : 0.0f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    j[k].o[i] = some ? f * x[k][i] : 0.0f;
-                    j[k].o[4 + i] = some ? f * y[k][i] : 0.0f;
-                }
-                together(j[k]);
-            };
-            add(1.0f);
-            if (passed_fp32<LANES>(j[k])) {                   // (of all lanes alike)
-                const Units u(j[k].sum);
-                add(u.by);
-                j[k].ref += u.scale;
+            for (int i = 0; i < 4; ++i) {
+                j[k].o[i] = some ? f * x[k][i] : 0.0f;
+                j[k].o[4 + i] = some ? f * y[k][i] : 0.0f;
             }
+            together(j[k]);
         }
     }
     __device__ __forceinline__ Joined many(int c) const
@@ -701,43 +676,35 @@ template <int D> struct Slots {
         for (int i = lane; i < n; i += 64) j.ref = fmaxf(j.ref, ml[(slot + i) * 2 * qrows + c]);
 #pragma unroll
         for (int step = 32; step; step >>= 1) j.ref = fmaxf(j.ref, __shfl_xor(j.ref, step));
-        auto add = [&](float by) {
-            j.sum = 0.0f;
+        j.sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
-            constexpr int U = 4;                              // slots that a lane asks for together
-            for (int i0 = side; i0 < n; i0 += U * SIDE) {
-                f32x4 x[U], y[U];
-                float m[U], l[U];
+        for (int i = 0; i < 8; ++i) j.o[i] = 0.0f;
+        constexpr int U = 4;                                  // slots that a lane asks for together
+        for (int i0 = side; i0 < n; i0 += U * SIDE) {
+            f32x4 x[U], y[U];
+            float m[U], l[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int64_t at = slot + min(i0 + u * SIDE, n - 1);
-                    const float *p = rows + (at * qrows + c) * D + 8 * e;
-                    m[u] = ml[at * 2 * qrows + c];
-                    l[u] = ml[at * 2 * qrows + qrows + c];
-                    x[u] = *reinterpret_cast<const f32x4 *>(p);
-                    y[u] = *reinterpret_cast<const f32x4 *>(p + 4);
-                }
+            for (int u = 0; u < U; ++u) {
+                const int64_t at = slot + min(i0 + u * SIDE, n - 1);
+                const float *p = rows + (at * qrows + c) * D + 8 * e;
+                m[u] = ml[at * 2 * qrows + c];
+                l[u] = ml[at * 2 * qrows + qrows + c];
+                x[u] = *reinterpret_cast<const f32x4 *>(p);
+                y[u] = *reinterpret_cast<const f32x4 *>(p + 4);
+            }
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (i0 + u * SIDE >= n || m[u] == -INFINITY) continue;
-                    const float f = __builtin_amdgcn_exp2f(m[u] - j.ref) * by;
-                    j.sum = fmaf(f, l[u], j.sum);
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * SIDE >= n || m[u] == -INFINITY) continue;
+                const float f = __builtin_amdgcn_exp2f(m[u] - j.ref);
+                j.sum = fmaf(f, l[u], j.sum);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        j.o[i] = fmaf(f, x[u][i], j.o[i]);
-                        j.o[4 + i] = fmaf(f, y[u][i], j.o[4 + i]);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    j.o[i] = fmaf(f, x[u][i], j.o[i]);
+                    j.o[4 + i] = fmaf(f, y[u][i], j.o[4 + i]);
                 }
             }
-            together(j);
-        };
-        add(1.0f);
-        if (passed_fp32<LANES>(j)) {
-            const Units u(j.sum);
-            add(u.by);
-            j.ref += u.scale;
         }
+        together(j);
         return j;
     }
     // Rows c0 .. c0 + N - 1 of at most `all`; done(row, Joined) is called for each.
