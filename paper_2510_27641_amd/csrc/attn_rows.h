@@ -148,10 +148,9 @@ __device__ __forceinline__ int wave_largest(int v)
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
 // Values near the end of fp32 (with bf16; with fp16 no sum comes close): rows whose unnormalised values times LARGE pass it are computed once more, with weights that add up to
-// SMALL = 2^-MORE, so that 2^MORE parts of a row (the GPU's workgroups are fewer) can be joined as they are.
+// less than 2^-MORE, so that 2^MORE parts of a row (the GPU's workgroups are fewer) can be joined as they are.
 constexpr float LARGE = 262144.0f;                            // 2^18
 constexpr int MORE = 12;
-constexpr float SMALL = 1.0f / (1 << MORE);
 
 // The reference of a part as it is put down: minus infinity says that nothing was attended to, which is not so where a score was NaN.
 __device__ __forceinline__ float reference(float ref, float sum) { return sum == sum ? ref : sum; }
@@ -310,7 +309,7 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
     }
 
     // Whether a row with finite scores holds a value that is not finite, or so large that parts of a row could pass fp32 together: an infinity or NaN
-    // behind its mask came in as 0 * infinity, or values are near the end of fp32 (never so with sums below 2^104, always from 2^111 on).
+    // came in, as 0 * infinity from behind its mask or as what the row sees, or values are near the end of fp32 (never so with sums below 2^104, always from 2^111 on).
     __device__ __forceinline__ bool spoiled() const
     {
         float x = 0.0f;
@@ -547,60 +546,110 @@ __device__ __forceinline__ void run_tiles(RowsOfWave<G, F16, PARTS> &rows, WHERE
     }
 }
 
-// Rows of this wave that an infinity or NaN in a place that their mask hides has spoiled (0 * infinity), or whose unnormalised values came close to the end of fp32: once
-// more, one row after the other, from what they attend to alone and with weights that add up to SMALL.  Runs behind leave(), over the same tiles.
-// `query(row)`: the row's query; `seen(tile, row)`: the positions that a row of the wave sees.
-template <typename G, bool F16, typename QUERY, typename SEEN>
-__device__ __forceinline__ void mend_rows(uint64_t which, float scale, const CacheRows &src, int first, int last, int cached, int wk, char *smem, QUERY query, SEEN seen)
+// Rows of this wave that an infinity or NaN among the values has come into, from a place that their mask hides (0 * infinity) or one that they see, or whose
+// unnormalised values came close to the end of fp32: once more, all of them together, from what they attend to alone.  Runs behind leave(), over the same tiles, for one wave by
+// itself: fragments come straight from memory, 32 elements at a time.  In the product, values that are not finite count as 0; beside it, plus and minus count those that
+// a row gives a weight to (a NaN as both, and so anything of weight 0 that is seen, as 0 * infinity is NaN).  bf16 weights are taken in units in which a row's add up to
+// less than 2^-MORE; with fp16 no sum comes near the end of fp32.
+// `seen(tile, row)`: the positions that a row of the wave sees.
+// With an infinity in the first value of one causal prompt, which sends every row here: 2048 tokens, 8 heads over 2, bf16 150 us (42 without it), 32768 tokens, 32
+// heads over 8 73 ms (8.2).
+template <typename G, bool F16, int PARTS, typename SEEN>
+__device__ __forceinline__ void mend_rows(uint64_t which, const RowsOfWave<G, F16, PARTS> &rows, const CacheRows &src, int first, int last, int cached, int wk, char *smem, SEEN seen)
 {
     constexpr int D = G::D;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr uint32_t INF = F16 ? 0x7c00 : 0x7f80, ONE = F16 ? 0x3c00 : 0x3f80, SIGN = 0x8000;
+    typedef typename Half<F16>::x8 x8;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                             // (what follows from it is not computed ahead, for rows that are not mended)
+    const int lane = tid & 63, wave = tid >> 6, row = lane & 31, half = lane >> 5;
     float *ml = reinterpret_cast<float *>(smem + G::OFF_ML) + wave * 32;
     char *mine = smem + wave * 32 * D * 4;
-    uint32_t left = (uint32_t)which | (uint32_t)(which >> 32);
-    while (left) {
-        const int row = __ffs(left) - 1;
-        left &= left - 1;
-        const float ref = ml[row], sum = ml[G::NW * 32 + row];
-        const uint16_t *q = query(row);
-        float x[D / 64], acc[D / 64];
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            x[i] = Half<F16>::widen(q[64 * i + lane]);
-            acc[i] = 0.0f;
-        }
+    const bool bad = (((uint32_t)which | (uint32_t)(which >> 32)) >> row) & 1;
+    const float ref = ml[row], sum = ml[G::NW * 32 + row];
+    const int scale = F16 ? 0 : __builtin_amdgcn_frexp_expf(sum) + MORE;
+    const float from = Half<F16>::HEAD - ref, by = __builtin_ldexpf(1.0f, -scale);
+#pragma unroll 1
+    for (int e = 0; e < D / 32; ++e) {
+        f32x16 o{}, plus{}, minus{};
+#pragma unroll 1
         for (int t = first; t < last; ++t) {
-            const uint64_t word = seen(t, row);
-            for (int r = 0; r < G::SPAN; ++r) {
-                if (!((word >> r) & 1)) continue;
-                const int in = wk * G::SPAN + r;
-                int64_t off;
-                if (t < cached) {
+            const uint64_t word = bad ? seen(t, row) : 0;
+            const bool old = t < cached;
+#pragma unroll 1
+            for (int u = 0; u < G::SUBS; ++u) {
+                const uint32_t bits = (uint32_t)(word >> (32 * u));
+                if (!__any(bits != 0)) continue;
+                const int in = wk * G::SPAN + 32 * u + row;
+                uint32_t unit;                                // where the row of position `row` of these 32 lies
+                if (old) {
                     const int rank = min(t * G::TILE + in, src.count - 1);
                     const int pos = src.position(rank, src.word(rank));
-                    off = (int64_t)src.unit(pos, src.page(pos)) * 16;
-                } else off = (int64_t)min(in, src.nodes - 1) * G::ROW_BYTES;
-                const uint16_t *k = reinterpret_cast<const uint16_t *>((t < cached ? src.k : src.k_new) + off);
-                const uint16_t *v = reinterpret_cast<const uint16_t *>((t < cached ? src.v : src.v_new) + off);
-                float s = 0.0f;
+                    unit = src.unit(pos, src.page(pos));
+                } else unit = (uint32_t)min(in, max(src.nodes, 1) - 1) * (G::ROW_BYTES / 16);
+                const char *k = (old ? src.k : src.k_new) + ((uint64_t)unit * 16 + half * 16), *v = (old ? src.v : src.v_new) + (32 * e + row) * 2;
+                f32x16 s{};
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) s = fmaf(x[i], Half<F16>::widen(k[64 * i + lane]), s);
+                for (int c = 0; c < D / 16; ++c) s = Half<F16>::mfma(*reinterpret_cast<const x8 *>(k + 32 * c), rows.q[c], s);
 #pragma unroll
-                for (int step = 32; step; step >>= 1) s += __shfl_xor(s, step);
-                const float w = __builtin_amdgcn_exp2f(fmaf(s, scale, Half<F16>::HEAD - ref)) / sum * SMALL;
+                for (int b = 0; b < 2; ++b) {                 // 16 positions
+                    uint32_t x[8], odd = 0;
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) acc[i] = fmaf(w, Half<F16>::widen(v[64 * i + lane]), acc[i]);
+                    for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const uint16_t *>(v + (uint64_t)(uint32_t)__shfl((int)unit, 16 * b + 8 * (i / 4) + 4 * half + i % 4) * 16);
+                    u32x4 value, more, less, hi, lo, live, dead;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float w[2];
+                        uint32_t f[2], m[2], l[2], on[2], off[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int n = 8 * b + 2 * i + j;
+                            const bool sees = (bits >> (8 * (n / 4) + 4 * half + n % 4)) & 1;
+                            w[j] = sees ? __builtin_amdgcn_exp2f(fmaf(s[n], rows.scale, from)) * by : 0.0f;
+                            const uint32_t y = x[2 * i + j];
+                            const bool wild = (y & INF) == INF;
+                            odd |= wild;
+                            f[j] = wild ? 0 : y;
+                            m[j] = wild && y != (SIGN | INF) ? ONE : 0;
+                            l[j] = wild && y != INF ? ONE : 0;
+                            on[j] = w[j] > 0.0f ? ONE : 0;
+                            off[j] = sees && !(w[j] > 0.0f) ? ONE : 0;
+                        }
+                        value[i] = f[0] | f[1] << 16;
+                        more[i] = m[0] | m[1] << 16;
+                        less[i] = l[0] | l[1] << 16;
+                        live[i] = on[0] | on[1] << 16;
+                        dead[i] = off[0] | off[1] << 16;
+                        hi[i] = pack2<F16>(w[0], w[1]);
+                        lo[i] = pack2<F16>(w[0] - Half<F16>::widen((uint16_t)hi[i]), w[1] - Half<F16>::widen((uint16_t)(hi[i] >> 16)));
+                    }
+                    o = Half<F16>::mfma(__builtin_bit_cast(x8, value), __builtin_bit_cast(x8, hi), o);
+                    o = Half<F16>::mfma(__builtin_bit_cast(x8, value), __builtin_bit_cast(x8, lo), o);
+                    if (__any(odd)) {
+                        const x8 any = __builtin_bit_cast(x8, more | less);
+                        plus = Half<F16>::mfma(__builtin_bit_cast(x8, more), __builtin_bit_cast(x8, live), plus);
+                        minus = Half<F16>::mfma(__builtin_bit_cast(x8, less), __builtin_bit_cast(x8, live), minus);
+                        plus = Half<F16>::mfma(any, __builtin_bit_cast(x8, dead), plus);
+                        minus = Half<F16>::mfma(any, __builtin_bit_cast(x8, dead), minus);
+                    }
+                }
             }
         }
+        if (!bad) continue;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            const int e = 64 * i + lane;
-            *reinterpret_cast<float *>(mine + row * D * 4 + (((e >> 2) ^ (row & (D / 4 - 1))) << 4) + 4 * (e & 3)) = acc[i];
+        for (int j = 0; j < 4; ++j) {
+            f32x4 x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int n = 4 * j + i;
+                x[i] = o[n] + (plus[n] > 0.0f ? INFINITY : 0.0f) + (minus[n] > 0.0f ? -INFINITY : 0.0f);
+            }
+            *reinterpret_cast<f32x4 *>(mine + row * D * 4 + (((8 * e + 2 * j + half) ^ (row & (D / 4 - 1))) << 4)) = x;
         }
-        if (lane == 0) {
-            ml[row] = ref + __builtin_amdgcn_logf(sum) + MORE;
-            ml[G::NW * 32 + row] = SMALL;
-        }
+    }
+    if (!F16 && bad && half == 0) {
+        ml[row] = ref + scale;
+        ml[G::NW * 32 + row] = sum * by;
     }
 }
 

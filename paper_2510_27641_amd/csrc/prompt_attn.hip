@@ -202,7 +202,7 @@ __global__ __launch_bounds__(NW * 64, WQ == 2 ? 1 : 2) void prompt_kernel(Prompt
     const PromptArgs &o = arguments_again<PromptArgs>();
     if (bad) {
         const CacheRows old = cache_rows(o, s, b, h);
-        mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, n, wk, smem, [&](int i) { return query(o, i); }, [&](int t, int i) {
+        mend_rows(bad, rows, old, first, last, n, wk, smem, [&](int t, int i) {
             return low_bits(max(token(o, i) + ahead + 1, 0) - t * G::TILE - wk * G::SPAN);
         });
     }

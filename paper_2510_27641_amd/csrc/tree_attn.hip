@@ -279,7 +279,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
         const TreeArgs &o = arguments_again<TreeArgs>();
         if (bad) {
             const CacheRows old = where();
-            mend_rows<G, F16>(bad, o.sm_scale * LOG2E, old, first, last, cached, wk, smem, [&](int i) { return query(o, i); }, [&](int t, int i) {
+            mend_rows(bad, rows, old, first, last, cached, wk, smem, [&](int t, int i) {
                 return t >= cached ? node_seen(o, old.nodes, i) >> (wk * G::SPAN) : low_bits(old.count - t * G::TILE - wk * G::SPAN);
             });
         }

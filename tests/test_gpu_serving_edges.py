@@ -52,3 +52,89 @@ def test_trees_with_values_at_the_end_of_fp32(G, T, n):
         x[:] = (x.float().sign() * 3e38).to(x.dtype)
         x[..., :32] = 3e38
     c.check([[np.arange(n)] * 2])
+
+
+def not_finite(v, at, d):
+    """Infinities of either sign, both in one column, and a NaN, in the rows `at` of v [..., rows, d]."""
+    inf = float("inf")
+    for i, (row, column, x) in enumerate(zip(at * 2, (3, d - 3, 17, 17, 40, 3), (inf, -inf, inf, -inf, float("nan"), inf))):
+        v[..., row, column] = x
+
+
+def compare_not_finite(got, q, k, v, seen, scale, dtype, low):
+    """Elements that are infinite or NaN where they have to be, and as near as others elsewhere."""
+    out, _, tol32, tol_low, _ = ref.attend(q, k, np.where(np.isfinite(v), v, 0.0), seen, scale, dtype)
+    for i in range(seen.shape[0]):
+        rows = v[seen[i]]
+        plus, minus, nan = ((x[:, None] if x.ndim == 1 else x).any(0) for x in (rows == np.inf, rows == -np.inf, np.isnan(rows)))
+        out[i] = np.where(nan | (plus & minus), np.nan, np.where(plus, np.inf, np.where(minus, -np.inf, out[i])))
+    finite = np.isfinite(out)
+    assert np.array_equal(np.isnan(got), np.isnan(out)) and np.array_equal(got[np.isinf(out)], out[np.isinf(out)])
+    assert (np.abs(got - out)[finite] <= (tol_low if low else tol32)[finite]).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f16", 128)])
+@pytest.mark.parametrize("q_lens,kv_lens,page", [([90], [90], 0), ([300, 7], [400, 64], 16), ([4, 2], [900, 130], 16), ([30], [2000], 0), ([130], [3000], 0)])
+def test_prompts_over_values_that_are_not_finite(q_lens, kv_lens, page, dtype, d):
+    """Seen by some queries, hidden from others of the same tile, and far behind them all."""
+    c = prompts.Case(q_lens, 8, 2, d, dtype, kv_lens=kv_lens, page=page, seed=23)
+    n, m = kv_lens[0], q_lens[0]
+    not_finite(c.v.transpose(0, 1), [n // 3, n - m // 2 - 1, n - 1], d)
+    for want in (("out",), ("low",)):
+        sa.specattn_prompt_attn(c.args(want))
+        torch.cuda.synchronize()
+        got = (c.out if want == ("out",) else c.low).double().cpu().numpy()
+        for b in range(len(q_lens)):
+            k, v = (x.double().numpy() for x in c.kv(b))
+            rows = slice(c.starts[b], c.starts[b + 1])
+            seen = np.arange(kv_lens[b])[None] < (kv_lens[b] - q_lens[b] + np.arange(q_lens[b])[:, None] + 1)
+            for h in range(8):
+                compare_not_finite(got[rows, h], c.q[rows, h].double().numpy(), k[:, h // 4], v[:, h // 4], seen, d ** -0.5, dtype, want == ("low",))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("G,T,n", [(1, 6, 200), (4, 20, 90), (4, 20, 3000), (8, 33, 900)])
+def test_trees_over_values_that_are_not_finite(G, T, n, dtype, d):
+    c = trees.Case(1, 2 * G, 2, T, d, n, dtype, page=16, seed=24)
+    not_finite(c.v_new, [1, T // 2, T - 1], d)
+    for column, at in ((5, n // 4), (d - 1, n - 1)):
+        c.v[c.table[0][at // 16], :, at % 16, column] = float("inf")
+    bits = np.array([[bool((int(c.masks[0, t]) >> u) & 1) for u in range(T)] for t in range(T)])
+    seen = np.concatenate((np.ones((T, n), dtype=bool), bits), 1)
+    for want in (("out",), ("low",)):
+        sa.specattn_tree_attn(c.args(want=want))
+        torch.cuda.synchronize()
+        got = (c.out if want == ("out",) else c.low).double().cpu().numpy()
+        for h in range(2 * G):
+            key, val = c.rows(0, h // G, np.arange(n))
+            k, v = np.concatenate((key, c.k_new[0, h // G].double().numpy())), np.concatenate((val, c.v_new[0, h // G].double().numpy()))
+            compare_not_finite(got[0, h], c.q[0, h].double().numpy(), k, v, seen, d ** -0.5, dtype, want == ("low",))
+
+
+def test_an_infinity_that_every_query_sees_costs_no_multiple_of_the_rows():
+    """What is computed once more is computed for all rows of a wave together: a row after the other took 200 times the plain call."""
+    n = 2048
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v = (torch.randn((n, h, 128), generator=g, device="cuda").bfloat16() for h in (8, 2, 2))
+    starts, out = torch.tensor([0, n], dtype=torch.int32, device="cuda"), torch.empty_like(q)
+    a = sa.prompt_args(q, k, v, starts, out_lowp=out)
+    ws = sa.alloc_workspace(sa.specattn_prompt_workspace_size(a))
+    sa.set_workspace(a, ws)
+
+    def took():
+        least = float("inf")
+        for _ in range(4):
+            one, two = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            one.record()
+            sa.specattn_prompt_attn(a)
+            two.record()
+            torch.cuda.synchronize()
+            least = min(least, one.elapsed_time(two))
+        return least
+
+    plain = took()
+    v[0, :, 9] = float("inf")
+    spoiled = took()
+    print("plain", plain, "ms, with an infinity", spoiled, "ms")
+    assert (out[..., 9] == float("inf")).all() and torch.isfinite(out[..., :9]).all() and torch.isfinite(out[..., 10:]).all()
+    assert spoiled < 30 * plain
