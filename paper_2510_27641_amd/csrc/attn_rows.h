@@ -166,6 +166,7 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
     f32x16 s[G::SUBS];                                        // scores of a tile
     u32x4 p[G::SUBS][2][PARTS];                               // weights of a tile, in the element type
     float ref, sum;                                           // in powers of two; of this lane's positions alone
+    float over;                                               // what rounding has put into the sum beyond its terms
     float scale;                                              // of the scores, log2(e) in it
     uint32_t key_at, value_at;                                // where this lane's first fragments lie in a tile
 
@@ -174,7 +175,7 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
 #pragma unroll
         for (int t = 0; t < D / 32; ++t) o[t] = f32x16{};
         ref = -INFINITY;
-        sum = 0.0f;
+        sum = over = 0.0f;
         scale = sm_scale * LOG2E;
         const int lane = threadIdx.x & 63, half = lane >> 5;
         const int krow = lane & 31;
@@ -282,19 +283,21 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
             const float by = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
             ref = next;
             sum *= by;
+            over *= by;
 #pragma unroll
             for (int t = 0; t < D / 32; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[t][i] *= by;
         }
         const float from = ref == -INFINITY ? 0.0f : Half<F16>::HEAD - ref;
+        float part[4] = {};                                   // a tile's weights by themselves, in four sums
 #pragma unroll
         for (int u = 0; u < G::SUBS; ++u) {
             float w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 w[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], scale, from));
-                sum += w[i];
+                part[i & 3] += w[i];
             }
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -306,6 +309,10 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
                         p[u][b][PARTS - 1][i] = pack2<F16>(x - Half<F16>::widen((uint16_t)p[u][b][0][i]), y - Half<F16>::widen((uint16_t)(p[u][b][0][i] >> 16)));
                 }
         }
+        // (compensated, W. Kahan 1965: equal weights added to a long sum one by one are all rounded the same way)
+        const float tile = ((part[0] + part[1]) + (part[2] + part[3])) - over, next = sum + tile;
+        over = (next - sum) - tile;
+        sum = next;
     }
 
     // Whether a row with finite scores holds a value that is not finite, or so large that parts of a row could pass fp32 together: an infinity or NaN
@@ -325,7 +332,7 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 31, half = lane >> 5;
         char *mine = smem + wave * 32 * D * 4;
-        sum = pair_sum(sum);
+        sum = pair_sum(sum - over);
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
 #pragma unroll

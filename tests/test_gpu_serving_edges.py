@@ -138,3 +138,38 @@ def test_an_infinity_that_every_query_sees_costs_no_multiple_of_the_rows():
     print("plain", plain, "ms, with an infinity", spoiled, "ms")
     assert (out[..., 9] == float("inf")).all() and torch.isfinite(out[..., :9]).all() and torch.isfinite(out[..., 10:]).all()
     assert spoiled < 30 * plain
+
+
+@pytest.mark.parametrize("n", [5000, 1 << 18])
+@pytest.mark.parametrize("tree", [False, True])
+def test_long_sums_of_equal_weights(tree, n):
+    """A first key and n - 1 equal ones behind it, in one part (256 kv heads): the total is off by what its weights are (2^-21 of them, and as much for the
+    argument), not by a step of itself for each of them; 2^-22 of the result for the logarithm."""
+    H, d, scale = 256, 64, float(np.log(2.0))
+    k, v = torch.zeros((n, 1, d), device="cuda").bfloat16(), torch.ones((n, 1, d), device="cuda").bfloat16()
+    k[1:, :, 0] = -0.5
+    lse = torch.empty((1, H), device="cuda")
+    if tree:
+        q = torch.zeros((1, H, 1, d), device="cuda").bfloat16()
+        q[..., 0] = 1
+        out, new = torch.empty((1, H, 1, d), device="cuda"), torch.zeros((1, H, 1, d), device="cuda").bfloat16()
+        k, v = (x.transpose(0, 1)[None].expand(1, H, n, d) for x in (k, v))
+        a = sa.tree_args(q, k, v, new, new, torch.zeros((1, 1), dtype=torch.int64, device="cuda"), out=out, lse=lse[..., None], sm_scale=scale)
+        ws = sa.alloc_workspace(sa.specattn_tree_workspace_size(a))
+        sa.set_workspace(a, ws)
+        sa.specattn_tree_attn(a)
+    else:
+        q = torch.zeros((1, H, d), device="cuda").bfloat16()
+        q[..., 0] = 1
+        out = torch.empty((1, H, d), device="cuda")
+        kw = dict(kv_starts=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+        a = sa.prompt_args(q, k.expand(n, H, d), v.expand(n, H, d), torch.tensor([0, 1], dtype=torch.int32, device="cuda"), out=out, lse=lse, sm_scale=scale, **kw)
+        assert sa.specattn_prompt_workspace_size(a) == 0
+        sa.specattn_prompt_attn(a)
+    torch.cuda.synchronize()
+    want = np.log(1 + (n - 1) * np.exp(-0.5 * np.float64(np.float32(scale))))
+    off = (lse.double().cpu() - want).abs().max().item()
+    print("lse", want, "off by", off, "out off by", (out.double() - 1).abs().max().item())
+    assert off <= 2.0 ** -20 + 2.0 ** -22 * want
+    # (products are added up sixteen positions at a time: half a step of the sum for each sixteen)
+    assert (out.double() - 1).abs().max().item() <= 2 * (n / 16 + 32) * 2.0 ** -24 + 2.0 ** -16
