@@ -278,10 +278,10 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
         top = pair_max(top) * scale;
-        if (__any(top > ref + Half<F16>::SLACK)) {
-            const float next = fmaxf(ref, top);
-            const float by = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
-            ref = next;
+        const bool far = top > ref + Half<F16>::SLACK;
+        if (__any(far)) {                                     // (each row for itself: what its neighbours see has no part in its rounding)
+            const float by = far ? __builtin_amdgcn_exp2f(ref - top) : 1.0f;
+            ref = far ? top : ref;
             sum *= by;
             over *= by;
 #pragma unroll

@@ -173,3 +173,47 @@ def test_long_sums_of_equal_weights(tree, n):
     assert off <= 2.0 ** -20 + 2.0 ** -22 * want
     # (products are added up sixteen positions at a time: half a step of the sum for each sixteen)
     assert (out.double() - 1).abs().max().item() <= 2 * (n / 16 + 32) * 2.0 ** -24 + 2.0 ** -16
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 128), ("f16", 64)])
+@pytest.mark.parametrize("q_len,H_q,kv_len", [(100, 2, 100), (300, 8, 700), (20, 2, 1500)])
+def test_prompts_do_not_depend_on_what_they_do_not_see(q_len, H_q, kv_len, dtype, d):
+    """Other keys, values and queries behind a place: the queries ahead of it keep their bits."""
+    c = prompts.Case([q_len], H_q, 1, d, dtype, kv_lens=[kv_len], seed=25)
+    c.k *= 4
+    sa.specattn_prompt_attn(c.args())
+    torch.cuda.synchronize()
+    first = c.out.clone(), c.low.clone(), c.lse.clone()
+    for cut in (q_len // 2, q_len // 5):
+        x = prompts.Case([q_len], H_q, 1, d, dtype, kv_lens=[kv_len], seed=26)
+        for name in ("q", "k", "v"):
+            at = cut + (kv_len - q_len if name != "q" else 0)
+            getattr(x, name)[:at] = getattr(c, name)[:at]
+            getattr(x, name)[at:] *= 6
+        sa.specattn_prompt_attn(x.args())
+        torch.cuda.synchronize()
+        for got, was in zip((x.out, x.low, x.lse), first):
+            assert torch.equal(got[:cut], was[:cut])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 128), ("f16", 64)])
+@pytest.mark.parametrize("G,T,n", [(1, 9, 100), (4, 20, 3000), (8, 33, 300)])
+def test_trees_do_not_depend_on_what_they_do_not_see(G, T, n, dtype, d):
+    """Nodes that are not there, and nodes that others do not descend from: their queries, keys and values leave the others' bits alone."""
+    c = trees.Case(1, 2 * G, 2, T, d, n, dtype, seed=27)
+    for x in (c.k, c.k_new):
+        x *= 4
+    c.masks[0] = [np.uint64(1) << np.uint64(t) | np.uint64(1) << np.uint64(t % 2) for t in range(T)]      # two roots, leaves of either
+    nodes = np.array([T - 2], dtype=np.int32)
+    sa.specattn_tree_attn(c.args(nodes=nodes))
+    torch.cuda.synchronize()
+    first = c.out.clone(), c.low.clone(), c.lse.clone()
+    odd = torch.arange(T) % 2 == 1
+    odd[T - 2:] = True
+    g = torch.Generator().manual_seed(28)
+    for x in (c.q, c.k_new, c.v_new):
+        x[:, :, odd] = (torch.randn(x[:, :, odd].shape, generator=g) * 6).to(x.dtype)
+    sa.specattn_tree_attn(c.args(nodes=nodes))
+    torch.cuda.synchronize()
+    for got, was in zip((c.out, c.low, c.lse), first):
+        assert torch.equal(got[:, :, ~odd.cuda()], was[:, :, ~odd.cuda()])
