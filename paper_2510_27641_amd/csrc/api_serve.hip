@@ -148,7 +148,7 @@ extern "C" {
 
 size_t specattn_pages_workspace_size(const specattn_pages_args *args)
 {
-    if (!args || args->B <= 0) return 0;
+    if (check_pages_args(args) != SPECATTN_OK) { clear_error(); return 0; }
     return pages_workspace_bytes(args);
 }
 
