@@ -86,7 +86,6 @@ template <int DIM, int NW_, int WQ_, int RING> struct Geo {
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;        // keys, values
     static constexpr int STAGES = RING * 1024 / STAGE_BYTES;  // tiles under way or in use
     static constexpr int BATCH = RING / 2;                    // tiles whose rows are looked up at a time
-    static constexpr int PER_CU = RING > 64 ? 1 : 2;          // workgroups that share a CU and its LDS
     static constexpr int OFF_TABLE = STAGES * STAGE_BYTES;    // uint32[BATCH * TILE] where the rows lie, in units of 16 bytes
     static constexpr int OFF_ML = OFF_TABLE + BATCH * TILE * 4;       // float[2][NW][32]: references and sums of the waves' rows
     static constexpr int LDS_BYTES = OFF_ML + 2 * NW * 32 * 4;
@@ -109,8 +108,6 @@ __device__ __forceinline__ void load_to_lds(const void *src, uint32_t to)
 }
 // All but the last N loads of this wave have arrived, LDS is read and written, and the other waves are here.
 template <int N> __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
-// The other waves are here; loads under way stay so.
-__device__ __forceinline__ void tile_barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 // As tile_barrier with the loads of `tiles` tiles of N left under way (at most MOST).
 template <int N, int MOST> __device__ __forceinline__ void tile_barrier_behind(int tiles)
 {
