@@ -638,12 +638,12 @@ typedef struct specattn_tree_args {
     float *out;                  /* [B][H_q][T][d] fp32, contiguous; optional if out_lowp is given */
     void *out_lowp;              /* [B][H_q][T][d] in dtype, contiguous; optional if out is given */
     float *lse;                  /* [B][H_q][T]; optional */
-    void *workspace;             /* specattn_tree_workspace_size(args) bytes, 256-byte aligned */
+    void *workspace;             /* specattn_tree_workspace_size(args) bytes (0: none), 256-byte aligned */
     size_t workspace_bytes;
 } specattn_tree_args;
 
 specattn_status specattn_tree_attn(const specattn_tree_args *args, void *stream);
-size_t specattn_tree_workspace_size(const specattn_tree_args *args);       /* 0 for invalid arguments */
+size_t specattn_tree_workspace_size(const specattn_tree_args *args);       /* 0 for invalid arguments too */
 
 /* Text of the calling thread's last error ("" if none).  Never NULL. */
 const char *specattn_last_error(void);

@@ -672,15 +672,16 @@ template <int D> __device__ __forceinline__ void leave_slot(float *rows, float *
 // Query rows that a wave of a merge kernel joins: four, whose loads go together, where units are so many that each is in few parts; one otherwise.
 constexpr int MERGE_ROWS = 4;
 
-// Query rows of partial results in slots slot .. slot + n - 1 ([slot][qrows][D] unnormalised, references and sums [slot][2][qrows]), joined by one
+// Query rows of n partial results, the first in slot `head`, part i in slot base + i * step ([slot][qrows][D] unnormalised, references and sums [slot][2][qrows]), joined by one
 // wave: D / 8 lanes take a slot's row, eight elements each, and 512 / D slots go side by side; the order of all sums is fixed.  Every lane gets the
 // total and the elements of its place.
 template <int D> struct Slots {
     static constexpr int LANES = D / 8, SIDE = 64 / LANES;
     const float *rows, *ml;
-    int64_t slot;
-    int n, qrows;
+    int64_t head, base;
+    int step, n, qrows;
 
+    __device__ __forceinline__ int64_t slot(int i) const { return i == 0 ? head : base + i * step; }
     __device__ __forceinline__ void together(Joined &j) const // over the slots that lie side by side
     {
 #pragma unroll
@@ -694,7 +695,7 @@ template <int D> struct Slots {
     template <int N> __device__ __forceinline__ void few(const int (&c)[N], Joined (&j)[N]) const
     {
         const int lane = threadIdx.x & 63, e = lane % LANES, side = lane / LANES;
-        const int64_t at = slot + min(side, n - 1);
+        const int64_t at = slot(min(side, n - 1));
         f32x4 x[N], y[N];
         float m[N], l[N];
 #pragma unroll
@@ -726,7 +727,7 @@ template <int D> struct Slots {
         const int lane = threadIdx.x & 63, e = lane % LANES, side = lane / LANES;
         Joined j;
         j.ref = -INFINITY;
-        for (int i = lane; i < n; i += 64) j.ref = fmaxf(j.ref, ml[(slot + i) * 2 * qrows + c]);
+        for (int i = lane; i < n; i += 64) j.ref = fmaxf(j.ref, ml[slot(i) * 2 * qrows + c]);
 #pragma unroll
         for (int step = 32; step; step >>= 1) j.ref = fmaxf(j.ref, __shfl_xor(j.ref, step));
         j.sum = 0.0f;
@@ -738,7 +739,7 @@ template <int D> struct Slots {
             float m[U], l[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int64_t at = slot + min(i0 + u * SIDE, n - 1);
+                const int64_t at = slot(min(i0 + u * SIDE, n - 1));
                 const float *p = rows + (at * qrows + c) * D + 8 * e;
                 m[u] = ml[at * 2 * qrows + c];
                 l[u] = ml[at * 2 * qrows + qrows + c];

@@ -224,7 +224,8 @@ template <int D, bool F16, int QROWS> __global__ __launch_bounds__(256) void pro
     Sequence s;
     if (!find_unit<QROWS, 256>(a, index, b, tile, s, lds)) return;
     const int lane = threadIdx.x & 63, queries = s.q_len * a.G;
-    const Slots<D> slots = {a.slots, a.slots_ml, (int64_t)blockIdx.x * a.parts, a.parts, QROWS};
+    const int64_t slot = (int64_t)blockIdx.x * a.parts;
+    const Slots<D> slots = {a.slots, a.slots_ml, slot, slot, 1, a.parts, QROWS};
     slots.template join<1>(blockIdx.y * 4 + (threadIdx.x >> 6), min(QROWS, queries - tile * QROWS), [&](int c, const Joined &j) {
         if (lane < D / 8) finish_row<D, F16>(a, j, s.q0, h, tile * QROWS + c, lane);
     });

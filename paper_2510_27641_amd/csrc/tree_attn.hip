@@ -284,7 +284,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void tree_kernel(TreeArgs a)
             });
         }
         const bool whole = first == 0 && last == n;
-        const int64_t slot = share + unit;
+        const int64_t slot = 2 * share + (first == 0);       // (a share has two partial results at most: of its first unit's end, and of its last unit's beginning)
         if (first == 0 && wave == 0 && !o.whole) {            // (all of the wave: it looks the share up together)
             const int2 parts = make_int2(share, by_unit ? share : line.of(tiles_at + n - 1));
             if (lane == 0) o.parts[unit] = parts;
@@ -308,7 +308,7 @@ template <int D, bool F16, int N> __global__ __launch_bounds__(256) void tree_me
     const int r = unit / a.blocks, block = unit - r * a.blocks;
     const int row = a.row0 + r, b = a.per_h.divide(row), h = row - b * a.H_kv;
     const int lane = threadIdx.x & 63, nodes = nodes_of(a, b), queries = a.G * a.T;
-    const Slots<D> slots = {a.slots, a.slots_ml, (int64_t)parts.x + unit, parts.y - parts.x + 1, qrows};
+    const Slots<D> slots = {a.slots, a.slots_ml, 2 * (int64_t)parts.x + 1, 2 * (int64_t)parts.x, 2, parts.y - parts.x + 1, qrows};
     slots.template join<N>((blockIdx.y * 4 + (threadIdx.x >> 6)) * N, min(qrows, queries - block * qrows), [&](int c, const Joined &j) {
         if (lane < D / 8) finish_row<D, F16>(a, j, b, h, block * qrows + c, nodes, lane);
     });
@@ -339,19 +339,39 @@ template <int D> size_t lds_of(int qrows) { return qrows == 64 ? Geo<D, 4, 2, 12
 size_t lds_size(int d, int qrows, int rows) { return (d == 128 ? lds_of<128>(qrows) : lds_of<64>(qrows)) + (size_t)(rows + 1) * 4; }
 size_t a256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-struct Layout { size_t parts, rows, ml; };
-Layout layout(int d, int qrows, int units)
+// How a call is cut: query rows of a unit, units to a row (b, h), rows to a launch, tiles of a unit at most, whether each unit has a workgroup, and workgroups
+// of a launch of so many rows.
+struct Cut {
+    int qrows, blocks, rows;
+    int64_t tiles;
+    bool whole;
+    int grid(int rows) const { return whole ? rows * blocks : (int)std::min<int64_t>(cu_count(), (rows * blocks * tiles + MIN_TILES - 1) / MIN_TILES); }
+};
+Cut cut(const specattn_tree_args *t)
 {
-    const size_t slots = (size_t)cu_count() + units;
-    return {a256((size_t)units * sizeof(int2)), slots * qrows * d * sizeof(float), a256(slots * 2 * qrows * sizeof(float))};
+    Cut c;
+    const int queries = t->H_q / t->H_kv * t->T;
+    c.qrows = rows_per_unit(queries);
+    c.blocks = (queries + c.qrows - 1) / c.qrows;
+    const int64_t most = t->indices ? (int64_t)t->idx_capacity << (t->chunk_size > 1 ? log2i(t->chunk_size) : 0) : t->n_max;
+    c.tiles = (most + 63) / 64 + 1;
+    c.rows = (int)std::min<int64_t>({(int64_t)t->B * t->H_kv, MAX_UNITS, (int64_t)(1 << 30) / (c.blocks * (most / 64 + 2))});      // tiles are counted in 31 bits
+    c.whole = c.tiles <= WHOLE_TILES;
+    return c;
+}
+struct Layout { size_t parts, rows, ml; };
+Layout layout(int d, const Cut &c)
+{
+    if (c.whole) return {0, 0, 0};                            // (every unit is finished where it is computed)
+    const size_t units = (size_t)c.rows * c.blocks, slots = 2 * (size_t)c.grid(c.rows);
+    return {a256(units * sizeof(int2)), slots * c.qrows * d * sizeof(float), a256(slots * 2 * c.qrows * sizeof(float))};
 }
 
 }  // namespace
 
 size_t tree_workspace_bytes(const specattn_tree_args *t)
 {
-    const int queries = t->H_q / t->H_kv * t->T, qrows = rows_per_unit(queries), blocks = (queries + qrows - 1) / qrows;
-    const Layout l = layout(t->d, qrows, (int)std::min<int64_t>((int64_t)t->B * t->H_kv, MAX_UNITS) * blocks);
+    const Layout l = layout(t->d, cut(t));
     return l.parts + l.rows + l.ml;
 }
 
@@ -407,27 +427,25 @@ specattn_status launch_tree(const specattn_tree_args *t, hipStream_t stream)
     a.chunk_shift = t->chunk_size > 1 ? log2i(t->chunk_size) : 0;
     a.capacity = t->idx_capacity;
     a.sm_scale = t->sm_scale > 0.0f ? t->sm_scale : 1.0f / std::sqrt((float)t->d);
-    const int queries = a.G * a.T, qrows = rows_per_unit(queries), rows = t->B * t->H_kv;
-    a.blocks = (queries + qrows - 1) / qrows;
+    const Cut c = cut(t);
+    const int rows = t->B * t->H_kv;
+    a.blocks = c.blocks;
+    a.whole = c.whole;
     const bool f16 = t->dtype == SPECATTN_F16;
-    const Layout l = layout(t->d, qrows, std::min(rows, MAX_UNITS) * a.blocks);
+    const Layout l = layout(t->d, c);
     char *ws = static_cast<char *>(t->workspace);
     a.parts = reinterpret_cast<int2 *>(ws);
     a.slots = reinterpret_cast<float *>(ws + l.parts);
     a.slots_ml = reinterpret_cast<float *>(ws + l.parts + l.rows);
-    const int64_t most = t->indices ? (int64_t)t->idx_capacity << a.chunk_shift : t->n_max;
     for (a.row0 = 0; a.row0 < rows; a.row0 += a.rows) {
-        a.rows = (int)std::min<int64_t>({rows - a.row0, MAX_UNITS, (int64_t)(1 << 30) / (a.blocks * (most / 64 + 2))});     // tiles are counted in 31 bits
-        const int64_t tiles = (most + 63) / 64 + 1;           // of a unit, at most
-        a.whole = tiles <= WHOLE_TILES;
+        a.rows = std::min(rows - a.row0, c.rows);
         const int units = a.rows * a.blocks;
-        const int grid = a.whole ? units : (int)std::min<int64_t>(cu_count(), (units * tiles + MIN_TILES - 1) / MIN_TILES);
-        variant(t->d, f16, t->out ? 2 : 1, qrows)<<<grid, qrows == 64 ? 256 : 512, lds_size(t->d, qrows, a.rows), stream>>>(a);
+        variant(t->d, f16, t->out ? 2 : 1, c.qrows)<<<c.grid(a.rows), c.qrows == 64 ? 256 : 512, lds_size(t->d, c.qrows, a.rows), stream>>>(a);
         st = check_launch("tree_kernel");
         if (st != SPECATTN_OK) return st;
         if (a.whole) continue;
         const int per = units * 4 >= cu_count() ? MERGE_ROWS : 1;
-        merge_variant(t->d, f16, per)<<<dim3(units, (std::min(queries, qrows) + 4 * per - 1) / (4 * per)), 256, 0, stream>>>(a, qrows);
+        merge_variant(t->d, f16, per)<<<dim3(units, (std::min(a.G * a.T, c.qrows) + 4 * per - 1) / (4 * per)), 256, 0, stream>>>(a, c.qrows);
         st = check_launch("tree_merge_kernel");
         if (st != SPECATTN_OK) return st;
     }

@@ -56,3 +56,23 @@ def test_updates_of_many_sequences(B, capacity):
         pick = rng.random(B)
         new = np.where(pick < 0.7, s.lens + rng.integers(0, 7, B), np.where(pick < 0.85, s.lens // 2, 0))
         s.update(np.minimum(new, width * page), capacity)
+
+
+def test_trees_stay_inside_their_workspace():
+    """Cut and joined in exactly the bytes that the size asks for; a call that is not cut runs without any."""
+    c = trees.Case(30, 8, 2, 16, 64, 3000, seed=5)
+    lens = np.random.default_rng(5).integers(1, 3000, 30).astype(np.int32)
+    a = c.args(seq_lens=lens)
+    need = sa.specattn_tree_workspace_size(a)
+    ws = torch.full((need + (1 << 16),), 0xab, dtype=torch.uint8, device="cuda")
+    sa.set_workspace(a, ws[:need])
+    sa.specattn_tree_attn(a)
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xab).all() and not (ws[:need] == 0xab).all()
+    c.compare([[np.arange(x)] * 2 for x in lens])
+    c = trees.Case(3, 8, 2, 16, 64, 448, seed=6)
+    a = c.args()
+    a.workspace, a.workspace_bytes = None, 0
+    sa.specattn_tree_attn(a)
+    torch.cuda.synchronize()
+    c.compare([[np.arange(448)] * 2] * 3)
