@@ -575,7 +575,7 @@ specattn_status specattn_cache_store(const specattn_store_args *args, void *stre
  * Sequence b has query rows q_starts[b] .. q_starts[b + 1] - 1 and L keys and values: those of the same rows of k and v, rows kv_starts[b] .. of them
  * where kv_starts is given, or positions 0 .. seq_lens[b] - 1 of its pages.  Its last query sees all L, the one before one less: query i of m
  * sees the first L - m + i + 1.  A query that sees nothing gives out = 0 and lse = -inf.  What a query does not see has no effect on it,
- * infinities and NaN included; rows of out and lse that belong to no sequence are left as they were.
+ * infinities and NaN included (among values: on its last bits at most); rows of out and lse that belong to no sequence are left as they were.
  * Accumulation and the softmax are fp32.  Where `out` is asked for the weights enter the second product in two parts of the element type
  * (16 significant bits with bf16, 22 with fp16), for out_lowp alone rounded to it.  Repeated calls give bit-identical results.
  * Starts ascend.  The rows of a kv head lie within 64 GiB of its first one (packed: k and v as a whole; SPECATTN_ESHAPE).  Lengths are cut to what there is (total_q, total_kv, the page table); a page number outside the pool reads the nearest page.
@@ -610,7 +610,8 @@ size_t specattn_prompt_workspace_size(const specattn_prompt_args *args);   /* 0 
  * tree_masks[b][t] - those it descends from and itself, in a tree; any set will do - in place of nodes 0 .. t.
  * Lists of positions, lists of chunks (chunk_size), pool slots (indices_are_physical) or, with indices == counts == NULL, every position below
  * seq_lens[b].  Nodes from node_counts[b] on are not there: their rows give out = 0 and lse = -inf, as does a row with nothing to attend to; their
- * bits, queries, keys and values have no effect.  Keys and values that a row's mask hides have none either, infinities and NaN included.
+ * bits, queries, keys and values have no effect.  Keys and values that a row's mask hides have none either, infinities and NaN included (as for
+ * specattn_prompt_attn).
  * Weights and results as for specattn_prompt_attn.  A list entry outside the cache is read as the nearest slot inside it, a page number outside the
  * pool as the nearest page.  Any number of query heads per kv head up to 65536 query rows G*T; a row attends to 2^24
  * positions at most, and the rows of a kv head lie within 64 GiB of its first one (SPECATTN_ESHAPE otherwise).

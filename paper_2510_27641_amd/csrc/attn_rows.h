@@ -12,8 +12,8 @@
 // way (slot 8 h + j of 16 stands for position 8 (j / 4) + 4 h + j % 4), so weights never leave their lane.
 // With fewer query rows than the waves have room for, two waves share rows and take one half of a tile each; their results are joined in LDS at the end.
 //
-// A tile costs a wave 32 matrix instructions (d = 128; 1024 cycles of its SIMD's matrix unit) and about 185 vector ones, 32 of them exponentials.
-// One causal prompt of 32768 positions, 32 heads over 8, bf16: 8.1 to 8.8 ms, 1.00 to 1.09 PFLOP/s (a library product of 8192^3 reaches 1.20), the matrix units busy for 51 %
+// A tile costs a wave 32 matrix instructions (d = 128; 1024 cycles of its SIMD's matrix unit) and about 190 vector ones, 32 of them exponentials.
+// One causal prompt of 32768 positions, 32 heads over 8, bf16: 7.9 to 8.6 ms, 1.03 to 1.11 PFLOP/s (a library product of 8192^3 reaches 1.20), the matrix units busy for 51 %
 // of the cycles at 1.94 GHz.  Two groups of waves that take turns between products and softmax, and fetches spread between the products, took the same time.
 #pragma once
 
@@ -154,7 +154,8 @@ __device__ __forceinline__ float reference(float ref, float sum) { return sum ==
 
 // One wave's 32 query rows.
 // PARTS: parts of the element type that a weight enters the second product in.  Where the result is asked for in that type alone, one:
-// its rounding (half a step, averaged over the row) is below the result's own.  Where it is asked for in fp32, two.
+// its rounding (half a step, averaged over the row) is below the result's own.  Where it is asked for in fp32, two.  (One part / two: a causal prompt of 32768 tokens
+// 8.0 / 11.1 ms, 4 x 512 tokens behind 4096 to 15872 in pages 667 / 910 us, 8 trees of 16 nodes over 7536 of 32768 positions 62 / 68, 16 of 64 over 3276 of 8192 138 / 180.)
 template <typename G, bool F16, int PARTS> struct RowsOfWave {
     static constexpr int D = G::D;
     typedef typename Half<F16>::x8 x8;
@@ -257,7 +258,7 @@ template <typename G, bool F16, int PARTS> struct RowsOfWave {
         }
     }
 
-    // Scores of tile t into weights.
+    // Scores of tile t into weights.  (The total is compensated; the products add up in fp32, sixteen positions at a time.)
     template <typename SEEN> __device__ __forceinline__ void weigh(SEEN &&seen, int t)
     {
         uint64_t word = 0;

@@ -4,7 +4,7 @@
 // such pieces that it asks for together.
 //
 // 131072 rows of 8 heads by 128 in fp16 (537 MB of keys and values read and as much written): 108 us, 4.95 TB/s, where a copy of 1 GiB reaches 5.17.  The
-// accepted nodes of 64 trees, 1.8 MB: 4.3 us, a launch and two dependent trips to memory.
+// accepted nodes of 64 trees, 1.8 MB: 4.2 to 4.7 us, a launch and two dependent trips to memory.
 #include "serve.h"
 
 #include <algorithm>

@@ -5,8 +5,8 @@
 // are entries, each finding its sequence by halving.  A new page may be one that another sequence has just returned: it is looked up where that
 // sequence's table still holds it, so that no thread waits for another's store.  Small calls do both in one workgroup and one launch.
 //
-// 64 sequences that gain or lose up to 8 tokens: 6.8 to 7.8 us, a launch and a chain of four dependent trips to memory.  256 prompts of up to 4096 tokens,
-// 12.6 MB of slots, positions and owners: 11.5 us in two launches (3.6 and 7.5; a copy of as many bytes would take 2.5).
+// 64 sequences that gain or lose up to 8 tokens: 7.2 to 8.5 us, a launch and a chain of four dependent trips to memory.  256 prompts of up to 4096 tokens,
+// 12.6 MB of slots, positions and owners: 11.5 to 12 us in two launches (3.6 and 8; a copy of as many bytes would take 2.5).
 #include "checks.h"
 #include "serve.h"
 

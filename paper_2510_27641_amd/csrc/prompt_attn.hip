@@ -8,8 +8,9 @@
 // prompt_merge_kernel joins their partial results in order.
 //
 // Bound by the tile loop's products and exponentials (attn_rows.h), in short prompts by the setup and the write-out of a unit beside few tiles: 32768 tokens
-// 8.1 to 8.8 ms (1.00 to 1.09 PFLOP/s, from card to card), 4 pieces of 512 tokens behind 16384 cached positions, 64 heads over 8 in fp16 690 to 735 us (0.96 to 1.02), 24 prompts of 32 to 2048 tokens
-// 167 to 176 us (0.65), 37 tokens by 8 heads at d = 64 5.1 us (a launch).
+// 7.9 to 8.6 ms (1.03 to 1.11 PFLOP/s, from card to card), 4 pieces of 512 tokens behind 16384 cached positions, 64 heads over 8 in fp16 676 to 728 us (0.97 to 1.04), 24 prompts of 32 to 2048 tokens
+// 165 to 172 us (0.67), 37 tokens by 8 heads at d = 64 5.1 to 5.4 us (a launch).  Single tokens, 32 heads over 8 and 8192 positions in pages: 64 sequences 375 us, 16 (a workgroup to each kv head, half
+// of the CUs without any) 160.
 #include "attn_rows.h"
 #include "checks.h"
 

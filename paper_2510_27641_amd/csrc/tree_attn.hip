@@ -2,12 +2,12 @@
 //
 // A unit is a kv head of a sequence with up to 256 of its G * T query rows; its tiles are those of the kept positions and one of the tree's
 // nodes behind them.  The tiles of all units form one line that is cut into equal shares, one per workgroup, whatever the counts are.  A unit
-// that lies in one share is finished there; of the others every share leaves a partial result (reference, sum, unnormalised rows), and
+// that lies in one share is finished there; of the others every share leaves a partial result (reference, sum, unnormalised rows; two at most to a share), and
 // tree_merge_kernel joins them in the order of the shares, so that repeated calls give the same bits.
 //
 // Few rows: bound by memory and by what a share spends ahead of and behind its tiles (finding its rows, the first fetches, partial results: 10 to 15 us, the joining 5 to
-// 9): 8 trees of 16 nodes, 32 heads over 8, a quarter of 32768 positions 69 to 71 us, 252 MB (3.6 TB/s); one tree of 26 over a third of 8192 24 us.  Many rows: by the tile
-// loop's products: 16 trees of 64 nodes, 64 heads over 8 in fp16, 40 % of 256 to 16384 positions in pages 122 us (0.48 PFLOP/s), 17 of them the joining.
+// 9): 8 trees of 16 nodes, 32 heads over 8, a quarter of 32768 positions 70 to 72 us, 252 MB (3.5 TB/s); one tree of 26 over a third of 8192 24 to 25 us.  Many rows: by the tile
+// loop's products: 16 trees of 64 nodes, 64 heads over 8 in fp16, 40 % of 256 to 16384 positions in pages 113 to 124 us (0.47 to 0.52 PFLOP/s), 14 to 17 of them the joining.
 #include "attn_rows.h"
 #include "checks.h"
 
@@ -33,7 +33,7 @@ struct TreeArgs {
     const int32_t *node_counts, *seq_lens, *indices, *counts, *page_table;
     float *out, *lse;
     void *out_lowp;
-    float *slots;                                             // partial results: [slot][rows][d], then references and sums [slot][2][rows]
+    float *slots;                                             // partial results: [slot][rows][d], then references and sums [slot][2][rows]; two slots to a share
     float *slots_ml;
     int2 *parts;                                              // [unit] first and last share of the unit
     int64_t q_b, q_h, q_t;                                    // elements
