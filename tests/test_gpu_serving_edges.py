@@ -217,3 +217,17 @@ def test_trees_do_not_depend_on_what_they_do_not_see(G, T, n, dtype, d):
     torch.cuda.synchronize()
     for got, was in zip((c.out, c.low, c.lse), first):
         assert torch.equal(got[:, :, ~odd.cuda()], was[:, :, ~odd.cuda()])
+
+
+@pytest.mark.parametrize("size", [1e30, 1e31, 1e32, 1e33, 1e34, 1e36])
+def test_values_on_either_side_of_where_rows_are_mended(size):
+    """Unnormalised sums from 2^100 on: as they are, mended in some parts of a row or in some rows, mended in all."""
+    c = prompts.Case([3, 40], 4, 2, 128, kv_lens=[4100, 900], page=16, seed=29)
+    c.v[:] = (c.v.float() * size).to(c.v.dtype)
+    c.v[:2000] *= 0.01
+    c.check()
+    c = trees.Case(2, 8, 2, 20, 128, 3000, seed=30)
+    c.v[:] = (c.v.float() * size).to(c.v.dtype)
+    c.v[:, :, 1000:] *= 0.01
+    c.v_new[:] = (c.v_new.float() * size).to(c.v_new.dtype)
+    c.check([[np.arange(3000)] * 2] * 2)
